@@ -3,7 +3,10 @@ budget-aware queues, vectorised over independent serving pools).
 
 The compute path is libinframind.so (HIP kernels for gfx950 behind the C ABI of
 include/inframind.h); this package only marshals arguments. Importing it does
-not load the library; the first call does, and fails loudly if it is missing."""
+not load the library; the first call does, and fails loudly if it is missing.
+
+learn.py binds libinframind_learn.so (include/inframind_learn.h): the policy's
+layers, softmax head and AdamW step for training on the rollouts."""
 from __future__ import annotations
 
 import numpy as np
@@ -21,6 +24,8 @@ from ._lib import (EXPORTED, IMError, im_clear_error, im_destroy, im_dual_update
                    im_write_state,
                    make_arrivals,
                    make_desc)
+from .learn import (LEARN_EXPORTED, AdamW, im_head_backward, im_head_forward,  # noqa: F401
+                    im_learn_last_error, im_linear_backward, im_linear_forward)
 
 
 def device_arrivals(arr: dict, device="cuda"):

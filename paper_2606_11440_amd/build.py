@@ -1,4 +1,5 @@
-"""Build libinframind.so (all HIP sources, gfx950) in-tree with hipcc."""
+"""Build libinframind.so and libinframind_learn.so (all HIP sources, gfx950)
+in-tree with hipcc."""
 from __future__ import annotations
 
 import concurrent.futures as cf
@@ -11,6 +12,9 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libinframind.so")
 SOURCES = ["route.hip", "schedule.hip", "rows.hip", "pool.hip"]
+# the learner's operators: a library of their own
+LEARN_LIB = os.path.join(HERE, "libinframind_learn.so")
+LEARN_SOURCES = ["learn.hip", "learn_rows.hip", "learn_sums.hip", "learn_adamw.hip"]
 # measurement probe used by the benchmark only (not part of the tick's library)
 PROBE_LIB = os.path.join(HERE, "libimprobe.so")
 PROBE_SOURCES = ["peak_probe.hip"]
@@ -22,8 +26,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 
 
-def build(jobs: int = 3) -> str:
-    """Compile every source and link the shared library; returns its path."""
+def build(jobs: int = 6) -> str:
+    """Compile every source and link the shared libraries; returns libinframind.so's path."""
     os.makedirs(BUILD, exist_ok=True)
 
     def compile_one(src):
@@ -35,8 +39,8 @@ def build(jobs: int = 3) -> str:
         return obj
 
     with cf.ThreadPoolExecutor(max_workers=jobs) as ex:
-        objs = list(ex.map(compile_one, SOURCES + PROBE_SOURCES))
-    for lib, srcs in ((LIB, SOURCES), (PROBE_LIB, PROBE_SOURCES)):
+        objs = list(ex.map(compile_one, SOURCES + LEARN_SOURCES + PROBE_SOURCES))
+    for lib, srcs in ((LIB, SOURCES), (LEARN_LIB, LEARN_SOURCES), (PROBE_LIB, PROBE_SOURCES)):
         tmp = lib + ".tmp"
         mine = [os.path.join(BUILD, s + ".o") for s in srcs]
         r = subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *mine],

@@ -1,0 +1,598 @@
+// C ABI of the learner's operators: checks of arguments, workspaces, launches.
+#include <cstdarg>
+#include <cstdio>
+#include <new>
+#include <vector>
+
+#include "learn_adamw.h"
+#include "learn_internal.h"
+
+using namespace im::learn;
+
+struct im_adamw {
+  int device = 0;
+  int bits = 32, grad_dtype = IM_F32;
+  int64_t runs = 0;
+  AdamwRun* table = nullptr;
+  im_adamw_tensor* tensors = nullptr;
+  uint32_t* done = nullptr;
+};
+
+namespace {
+
+thread_local char t_error[256] = "no error";
+
+__attribute__((format(printf, 2, 3))) im_status fail(im_status s, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  std::vsnprintf(t_error, sizeof(t_error), fmt, ap);
+  va_end(ap);
+  return s;
+}
+
+#define LEARN_HIP(call)                                                                              \
+  do {                                                                                               \
+    const hipError_t _e = (call);                                                                    \
+    if (_e != hipSuccess)                                                                            \
+      return fail(_e == hipErrorOutOfMemory ? IM_ENOMEM : IM_EHIP, "%s: %s", #call, hipGetErrorString(_e)); \
+  } while (0)
+
+#define LEARN_CHECK(cond, ...)                       \
+  do {                                               \
+    if (!(cond)) return fail(IM_EINVAL, __VA_ARGS__); \
+  } while (0)
+
+// Compute units of the current device (256 where the query fails).
+int compute_units() {
+  static int known[64];   // each device's is written once it is known, always with the same value
+  int dev = 0, n = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return 256;
+  if (dev >= 0 && dev < 64 && __atomic_load_n(&known[dev], __ATOMIC_RELAXED) > 0)
+    return __atomic_load_n(&known[dev], __ATOMIC_RELAXED);
+  if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) return 256;
+  if (dev >= 0 && dev < 64) __atomic_store_n(&known[dev], n, __ATOMIC_RELAXED);
+  return n;
+}
+
+// Sections of a workspace, each 256-byte aligned.
+struct Sections {
+  char* base;
+  int64_t used = 0;
+  explicit Sections(void* p) : base(static_cast<char*>(p)) {}
+  template <typename T>
+  T* take(int64_t count) {
+    T* p = base ? reinterpret_cast<T*>(base + used) : nullptr;
+    used += (count * (int64_t)sizeof(T) + 255) & ~(int64_t)255;
+    return p;
+  }
+};
+
+int64_t size_of(int dtype) { return dtype == IM_BF16 ? 2 : 4; }
+bool aligned(const void* p, int64_t a) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(a - 1)) == 0; }
+
+im_status check_groups(int32_t G, const int32_t* offsets) {
+  LEARN_CHECK(offsets || G == 1, "offsets NULL needs n_groups = 1");
+  LEARN_CHECK(aligned(offsets, 4), "offsets is not 4-byte aligned");
+  return IM_OK;
+}
+im_status check_work(const void* ws, int64_t have, int64_t need) {
+  LEARN_CHECK(have >= need && (need == 0 || ws), "workspace of %lld bytes, %lld needed", (long long)have, (long long)need);
+  LEARN_CHECK(need == 0 || aligned(ws, 256), "workspace is not 256-byte aligned");
+  return IM_OK;
+}
+im_status check_launch(int64_t tiles) {
+  if (tiles > 0x7fffffff) return fail(IM_EUNSUPPORTED, "more than 2^31 - 1 tiles");
+  return IM_OK;
+}
+#define LEARN_OK(call)                       \
+  do {                                       \
+    const im_status _s = (call);             \
+    if (_s != IM_OK) return _s;              \
+  } while (0)
+
+// ---- layers ------------------------------------------------------------------
+
+im_status check_linear(const im_linear_desc* d) {
+  LEARN_CHECK(d, "desc is NULL");
+  LEARN_CHECK(d->n_groups >= 1 && d->n_groups <= IM_MAX_GROUPS, "n_groups out of range");
+  LEARN_CHECK(d->n_rows >= 0, "n_rows out of range");
+  LEARN_CHECK(d->in_dim >= 1 && d->in_dim <= IM_MAX_DIM, "in_dim out of range");
+  LEARN_CHECK(d->out_dim >= 1 && d->out_dim <= IM_MAX_DIM, "out_dim out of range");
+  LEARN_CHECK(d->dtype == IM_F32 || d->dtype == IM_BF16, "dtype out of range");
+  LEARN_CHECK((d->relu | d->relu_in) == 0 || (d->relu | d->relu_in) == 1, "relu and relu_in are 0 or 1");
+  return IM_OK;
+}
+
+struct LinearWork {
+  SumPlan sums;
+  float* part;
+  int64_t part_width, db_at, bytes;
+};
+// Plan and workspace of the weight and bias gradients.
+LinearWork linear_work(int dtype, int64_t n, int64_t G, int64_t M, int64_t N, void* ws) {
+  LinearWork w;
+  w.sums = plan_sums(dtype, n, G, M, N, compute_units());
+  w.db_at = (M * N + 3) & ~(int64_t)3;
+  w.part_width = w.db_at + ((M + 3) & ~(int64_t)3);
+  Sections s(ws);
+  // one group of one chunk stores its gradient at once
+  w.part = s.take<float>(w.sums.chunks > 1 ? w.sums.chunks * w.part_width : 0);
+  w.bytes = s.used;
+  return w;
+}
+
+RowArgs row_args(const int32_t* offsets, int32_t G, int32_t n, const RowPlan& p, int32_t* error) {
+  RowArgs a = {};
+  a.offsets = offsets;
+  a.G = G;
+  a.n = n;
+  a.row_tiles = (int32_t)p.row_tiles;
+  a.col_tiles = (int32_t)p.col_tiles;
+  a.error = error;
+  return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+const char* im_learn_last_error(void) { return t_error; }
+
+im_status im_linear_workspace(const im_linear_desc* d, int32_t backward, int64_t* bytes) {
+  LEARN_OK(check_linear(d));
+  LEARN_CHECK(bytes, "bytes is NULL");
+  LEARN_CHECK(backward == 0 || backward == 1, "backward is 0 or 1");
+  *bytes = backward ? linear_work(d->dtype, d->n_rows, d->n_groups, d->out_dim, d->in_dim, nullptr).bytes : 0;
+  return IM_OK;
+}
+
+im_status im_linear_forward(const im_linear_desc* d, const int32_t* offsets, const void* x, const void* W,
+                            const float* b, void* y, void* ws, int64_t ws_bytes, int32_t* error, void* stream) {
+  LEARN_OK(check_linear(d));
+  LEARN_OK(check_groups(d->n_groups, offsets));
+  const int64_t e = size_of(d->dtype);
+  LEARN_CHECK(d->ld_x >= d->in_dim && d->ld_y >= d->out_dim, "ld_x or ld_y is less than the row");
+  LEARN_CHECK(W && (d->n_rows == 0 || (x && y)), "x, W or y is NULL");
+  LEARN_CHECK(aligned(x, e) && aligned(W, e) && aligned(y, e) && aligned(b, 4) && aligned(error, 4),
+              "a pointer is not aligned to its elements");
+  LEARN_OK(check_work(ws, ws_bytes, 0));
+  if (d->n_rows == 0) return IM_OK;
+  const RowPlan p = plan_rows(d->dtype, d->n_rows, d->n_groups, d->out_dim, compute_units());
+  LEARN_OK(check_launch(p.row_tiles * p.col_tiles));
+  RowArgs a = row_args(offsets, d->n_groups, d->n_rows, p, error);
+  a.K = d->in_dim;
+  a.N = d->out_dim;
+  a.A = x;
+  a.lda = d->ld_x;
+  a.B = W;
+  a.ldb = d->in_dim;
+  a.b_group = (int64_t)d->in_dim * d->out_dim;
+  a.bias = b;
+  a.bias_group = d->out_dim;
+  a.C = y;
+  a.ldc = d->ld_y;
+  a.relu = d->relu;
+  LEARN_HIP(launch_rows_product(a, d->dtype, p.shape, kStore, (hipStream_t)stream));
+  return IM_OK;
+}
+
+im_status im_linear_backward(const im_linear_desc* d, const int32_t* offsets, const void* dy, const void* x,
+                             const void* W, void* dx, void* dW, float* db, void* ws, int64_t ws_bytes, int32_t* error,
+                             void* stream) {
+  LEARN_OK(check_linear(d));
+  LEARN_OK(check_groups(d->n_groups, offsets));
+  const int64_t e = size_of(d->dtype);
+  const bool some = d->n_rows > 0;
+  LEARN_CHECK(!some || dy, "dy is NULL");
+  LEARN_CHECK(d->ld_y >= d->out_dim, "ld_y is less than the row");
+  LEARN_CHECK(!dx || !some || (W && d->ld_dx >= d->in_dim), "dx needs W and ld_dx >= in_dim");
+  LEARN_CHECK(!some || !(dW || (dx && d->relu_in)) || (x && d->ld_x >= d->in_dim),
+              "dW, and dx with relu_in, need x and ld_x >= in_dim");
+  LEARN_CHECK(aligned(dy, e) && aligned(x, e) && aligned(W, e) && aligned(dx, e) && aligned(dW, e) && aligned(db, 4) &&
+                  aligned(error, 4),
+              "a pointer is not aligned to its elements");
+  const LinearWork w = linear_work(d->dtype, d->n_rows, d->n_groups, d->out_dim, d->in_dim, ws);
+  LEARN_OK(check_work(ws, ws_bytes, w.bytes));
+  const RowPlan p = plan_rows(d->dtype, d->n_rows, d->n_groups, d->in_dim, compute_units());
+  LEARN_OK(check_launch(p.row_tiles * p.col_tiles));
+  LEARN_OK(check_launch(w.sums.chunks * w.sums.row_tiles * w.sums.col_tiles));
+  if (dx && some) {
+    RowArgs a = row_args(offsets, d->n_groups, d->n_rows, p, error);
+    a.K = d->out_dim;
+    a.N = d->in_dim;
+    a.A = dy;
+    a.lda = d->ld_y;
+    a.B = W;
+    a.ldb = d->in_dim;
+    a.b_group = (int64_t)d->in_dim * d->out_dim;
+    a.C = dx;
+    a.ldc = d->ld_dx;
+    a.X = d->relu_in ? x : nullptr;
+    a.ldx = d->ld_x;
+    a.first = a.last = 1;
+    LEARN_HIP(launch_rows_product(a, d->dtype, p.shape, kStoreInput, (hipStream_t)stream));
+  }
+  if (dW || db) {
+    SumArgs a = {};
+    a.offsets = offsets;
+    a.G = d->n_groups;
+    a.n = d->n_rows;
+    a.M = d->out_dim;
+    a.N = dW ? d->in_dim : 1;   // db alone: a column of dy in place of x
+    a.P = dy;
+    a.ldp = d->ld_y;
+    a.Q = dW ? x : dy;
+    a.ldq = dW ? d->ld_x : d->ld_y;
+    a.dW = dW;
+    a.w_group = (int64_t)d->in_dim * d->out_dim;
+    a.db = db;
+    a.part = w.part;
+    a.part_width = w.part_width;
+    a.db_at = w.db_at;
+    a.chunk = (int32_t)w.sums.chunk;
+    a.chunks = (int32_t)w.sums.chunks;
+    a.row_tiles = (int32_t)w.sums.row_tiles;
+    a.col_tiles = dW ? (int32_t)w.sums.col_tiles : 1;
+    a.error = error;
+    LEARN_HIP(launch_sums(a, d->dtype, w.sums.shape, (hipStream_t)stream));
+  }
+  return IM_OK;
+}
+
+// ---- softmax head ----------------------------------------------------------------
+
+}  // extern "C"
+
+namespace {
+
+im_status check_head(const im_head_desc* d) {
+  LEARN_CHECK(d, "desc is NULL");
+  LEARN_CHECK(d->n_groups >= 1 && d->n_groups <= IM_MAX_GROUPS, "n_groups out of range");
+  LEARN_CHECK(d->n_rows >= 0, "n_rows out of range");
+  LEARN_CHECK(d->dim >= 1 && d->dim <= IM_MAX_DIM, "dim out of range");
+  LEARN_CHECK(d->n_classes >= 1 && d->n_classes <= IM_MAX_CLASSES, "n_classes out of range");
+  LEARN_CHECK(d->dtype == IM_F32 || d->dtype == IM_BF16, "dtype out of range");
+  LEARN_CHECK(d->relu_in == 0 || d->relu_in == 1, "relu_in is 0 or 1");
+  return IM_OK;
+}
+
+struct HeadForward {
+  RowPlan plan;
+  float *stats, *taken;
+  int64_t bytes;
+};
+HeadForward head_forward(const im_head_desc& d, void* ws) {
+  HeadForward w;
+  w.plan = plan_rows(d.dtype, d.n_rows, d.n_groups, d.n_classes, compute_units());
+  Sections s(ws);
+  const bool split = w.plan.col_tiles > 1;
+  w.stats = s.take<float>(split ? w.plan.col_tiles * d.n_rows * 3 : 0);
+  w.taken = s.take<float>(split ? d.n_rows : 0);
+  w.bytes = s.used;
+  return w;
+}
+
+// The gradient's pieces: dz of `width` classes at a time.
+struct HeadBackward {
+  int64_t width, pieces;
+  RowPlan logits, input;
+  LinearWork sums;
+  void* dz;
+  float *sum, *db_part;
+  uint8_t* live;
+  void* sums_ws;
+  int64_t bytes;
+};
+HeadBackward head_backward(const im_head_desc& d, void* ws) {
+  HeadBackward w;
+  const int64_t n = d.n_rows, G = d.n_groups, V = d.n_classes;
+  const int cus = compute_units();
+  // dz of a piece stays within 2^27 elements, and a piece is 1024 classes at least
+  int64_t width = n > 0 ? ((int64_t)1 << 27) / n : V;
+  width = width < 1024 ? 1024 : width / 1024 * 1024;
+  w.pieces = (V + width - 1) / width;
+  w.width = w.pieces > 1 ? width : (V + 7) / 8 * 8;
+  w.logits = plan_rows(d.dtype, n, G, w.pieces > 1 ? width : V, cus);
+  w.input = plan_rows(d.dtype, n, G, d.dim, cus);
+  Sections s(ws);
+  w.dz = s.take<char>(n * w.width * size_of(d.dtype));
+  w.sum = s.take<float>(w.pieces > 1 ? n * d.dim : 0);
+  w.db_part = s.take<float>(w.logits.row_tiles * V);
+  w.live = s.take<uint8_t>(n);
+  w.sums_ws = s.base ? s.base + s.used : nullptr;
+  w.sums = linear_work(d.dtype, n, G, w.pieces > 1 ? width : V, d.dim, w.sums_ws);
+  w.bytes = s.used + w.sums.bytes;
+  return w;
+}
+
+}  // namespace
+
+extern "C" {
+
+im_status im_head_workspace(const im_head_desc* d, int32_t backward, int64_t* bytes) {
+  LEARN_OK(check_head(d));
+  LEARN_CHECK(bytes, "bytes is NULL");
+  LEARN_CHECK(backward == 0 || backward == 1, "backward is 0 or 1");
+  *bytes = d->n_rows == 0 && !backward ? 0 : (backward ? head_backward(*d, nullptr).bytes : head_forward(*d, nullptr).bytes);
+  return IM_OK;
+}
+
+im_status im_head_forward(const im_head_desc* d, const int32_t* offsets, const void* h, const void* W, const float* b,
+                          const uint32_t* valid, const int32_t* target, float* logp, float* entropy, float* lse,
+                          void* ws, int64_t ws_bytes, int32_t* error, void* stream) {
+  LEARN_OK(check_head(d));
+  LEARN_OK(check_groups(d->n_groups, offsets));
+  const int64_t e = size_of(d->dtype);
+  LEARN_CHECK(d->ld_h >= d->dim, "ld_h is less than the row");
+  LEARN_CHECK(W && (d->n_rows == 0 || (h && target && logp)), "h, W, target or logp is NULL");
+  LEARN_CHECK(aligned(h, e) && aligned(W, e) && aligned(b, 4) && aligned(valid, 4) && aligned(target, 4) &&
+                  aligned(logp, 4) && aligned(entropy, 4) && aligned(lse, 4) && aligned(error, 4),
+              "a pointer is not aligned to its elements");
+  if (d->n_rows == 0) return IM_OK;
+  const HeadForward w = head_forward(*d, ws);
+  LEARN_OK(check_work(ws, ws_bytes, w.bytes));
+  LEARN_OK(check_launch(w.plan.row_tiles * w.plan.col_tiles));
+  RowArgs a = row_args(offsets, d->n_groups, d->n_rows, w.plan, error);
+  a.K = d->dim;
+  a.N = a.V = d->n_classes;
+  a.words = (d->n_classes + 31) / 32;
+  a.A = h;
+  a.lda = d->ld_h;
+  a.B = W;
+  a.ldb = d->dim;
+  a.b_group = (int64_t)d->dim * d->n_classes;
+  a.bias = b;
+  a.bias_group = d->n_classes;
+  a.valid = valid;
+  a.target = target;
+  a.stats = w.stats;
+  a.taken = w.taken;
+  a.logp = logp;
+  a.entropy = entropy;
+  a.lse = lse;
+  LEARN_HIP(launch_rows_product(a, d->dtype, w.plan.shape, kStats, (hipStream_t)stream));
+  return IM_OK;
+}
+
+im_status im_head_backward(const im_head_desc* d, const int32_t* offsets, const void* h, const void* W, const float* b,
+                           const uint32_t* valid, const int32_t* target, const float* lse, const float* entropy,
+                           const float* dlogp, const float* dentropy, void* dh, void* dW, float* db, void* ws,
+                           int64_t ws_bytes, int32_t* error, void* stream) {
+  LEARN_OK(check_head(d));
+  LEARN_OK(check_groups(d->n_groups, offsets));
+  const int64_t e = size_of(d->dtype);
+  const bool some = d->n_rows > 0;
+  LEARN_CHECK(d->ld_h >= d->dim && (!dh || d->ld_dh >= d->dim), "ld_h or ld_dh is less than the row");
+  LEARN_CHECK(!some || (h && W && target && lse && dlogp), "h, W, target, lse or dlogp is NULL");
+  LEARN_CHECK(!some || !dentropy || entropy, "dentropy needs entropy");
+  LEARN_CHECK(aligned(h, e) && aligned(W, e) && aligned(dh, e) && aligned(dW, e) && aligned(b, 4) && aligned(valid, 4) &&
+                  aligned(target, 4) && aligned(lse, 4) && aligned(entropy, 4) && aligned(dlogp, 4) &&
+                  aligned(dentropy, 4) && aligned(db, 4) && aligned(error, 4),
+              "a pointer is not aligned to its elements");
+  const HeadBackward w = head_backward(*d, ws);
+  LEARN_OK(check_work(ws, ws_bytes, w.bytes));
+  LEARN_OK(check_launch(w.logits.row_tiles * w.logits.col_tiles));
+  LEARN_OK(check_launch(w.input.row_tiles * w.input.col_tiles));
+  LEARN_OK(check_launch(w.sums.sums.chunks * w.sums.sums.row_tiles * w.sums.sums.col_tiles));
+  if (!dh && !dW && !db) return IM_OK;
+  const hipStream_t s = (hipStream_t)stream;
+  const int64_t V = d->n_classes;
+  for (int64_t piece = 0; piece < w.pieces; ++piece) {
+    const int64_t c0 = piece * w.width, width = V - c0 < w.width ? V - c0 : w.width;
+    const char* Wp = static_cast<const char*>(W) + c0 * d->dim * e;
+    if (some) {
+      RowArgs a = row_args(offsets, d->n_groups, d->n_rows, w.logits, error);
+      a.K = d->dim;
+      a.N = (int32_t)width;
+      a.V = d->n_classes;
+      a.col0 = (int32_t)c0;
+      a.words = (d->n_classes + 31) / 32;
+      a.A = h;
+      a.lda = d->ld_h;
+      a.B = Wp;
+      a.ldb = d->dim;
+      a.b_group = V * d->dim;
+      a.bias = b;
+      a.bias_group = V;
+      a.C = w.dz;
+      a.ldc = w.width;
+      a.valid = valid;
+      a.target = target;
+      a.lse = const_cast<float*>(lse);
+      a.entropy = const_cast<float*>(entropy);
+      a.dlogp = dlogp;
+      a.dentropy = dentropy;
+      a.db_part = db ? w.db_part : nullptr;
+      a.db_width = V;
+      a.live = w.live;
+      LEARN_HIP(launch_rows_product(a, d->dtype, w.logits.shape, kGradLogits, s));
+    }
+    if (dh && some) {
+      RowArgs a = row_args(offsets, d->n_groups, d->n_rows, w.input, error);
+      a.K = (int32_t)width;
+      a.N = d->dim;
+      a.A = w.dz;
+      a.lda = w.width;
+      a.B = Wp;
+      a.ldb = d->dim;
+      a.b_group = V * d->dim;
+      a.C = dh;
+      a.ldc = d->ld_dh;
+      a.X = d->relu_in ? h : nullptr;
+      a.ldx = d->ld_h;
+      a.sum = w.pieces > 1 ? w.sum : nullptr;
+      a.first = piece == 0;
+      a.last = piece == w.pieces - 1;
+      LEARN_HIP(launch_rows_product(a, d->dtype, w.input.shape, kStoreInput, s));
+    }
+    if (dW) {
+      SumArgs a = {};
+      a.offsets = offsets;
+      a.G = d->n_groups;
+      a.n = d->n_rows;
+      a.M = (int32_t)width;
+      a.N = d->dim;
+      a.P = w.dz;
+      a.ldp = w.width;
+      a.Q = h;
+      a.ldq = d->ld_h;
+      a.live = w.live;
+      a.dW = static_cast<char*>(dW) + c0 * d->dim * e;
+      a.w_group = V * d->dim;
+      a.part = w.sums.part;
+      a.part_width = w.sums.part_width;
+      a.db_at = (width * d->dim + 3) & ~(int64_t)3;
+      a.chunk = (int32_t)w.sums.sums.chunk;
+      a.chunks = (int32_t)w.sums.sums.chunks;
+      a.row_tiles = (int32_t)w.sums.sums.row_tiles;
+      a.col_tiles = (int32_t)w.sums.sums.col_tiles;
+      a.error = error;
+      LEARN_HIP(launch_sums(a, d->dtype, w.sums.sums.shape, s));
+    }
+  }
+  if (db)
+    LEARN_HIP(launch_bias_sum(offsets, d->n_groups, d->n_rows, rows_per_tile(w.logits.shape), w.db_part, V, db, s));
+  return IM_OK;
+}
+
+// ---- AdamW -------------------------------------------------------------------------
+
+}  // extern "C"
+
+namespace {
+
+im_status check_tensor(const im_adamw_tensor& t, int bits, int grad_dtype, int i) {
+  LEARN_CHECK(t.n >= 0, "tensor %d: n out of range", i);
+  LEARN_CHECK(t.decay == 0 || t.decay == 1, "tensor %d: decay is 0 or 1", i);
+  if (t.n == 0) return IM_OK;
+  LEARN_CHECK(t.param && t.grad && t.m && t.v, "tensor %d: param, grad, m or v is NULL", i);
+  LEARN_CHECK(bits == 32 || (t.m_scale && t.v_scale), "tensor %d: 8-bit states need m_scale and v_scale", i);
+  LEARN_CHECK(bits == 8 || (!t.m_scale && !t.v_scale), "tensor %d: 32-bit states have no scales", i);
+  LEARN_CHECK(aligned(t.param, 4) && aligned(t.grad, size_of(grad_dtype)) && aligned(t.copy, 2) &&
+                  (bits == 8 || (aligned(t.m, 4) && aligned(t.v, 4))) && aligned(t.m_scale, 4) && aligned(t.v_scale, 4),
+              "tensor %d: a pointer is not aligned to its elements", i);
+  return IM_OK;
+}
+
+template <typename T>
+hipError_t upload(T** out, const std::vector<T>& from, hipStream_t s) {
+  if (from.empty()) return hipSuccess;
+  hipError_t e = hipMalloc(reinterpret_cast<void**>(out), from.size() * sizeof(T));
+  if (e == hipSuccess) e = hipMemcpyAsync(*out, from.data(), from.size() * sizeof(T), hipMemcpyHostToDevice, s);
+  return e;
+}
+
+void free_adamw(im_adamw* o) {
+  (void)hipFree(o->table);
+  (void)hipFree(o->tensors);
+  (void)hipFree(o->done);
+  delete o;
+}
+
+// The plan's device as the current one within a call.
+class OnDevice {
+ public:
+  explicit OnDevice(int device) {
+    err = hipGetDevice(&was_);
+    if (err == hipSuccess && was_ != device) {
+      err = hipSetDevice(device);
+      moved_ = err == hipSuccess;
+    }
+  }
+  ~OnDevice() {
+    if (moved_) (void)hipSetDevice(was_);
+  }
+  OnDevice(const OnDevice&) = delete;
+  OnDevice& operator=(const OnDevice&) = delete;
+  hipError_t err;
+
+ private:
+  int was_ = 0;
+  bool moved_ = false;
+};
+
+}  // namespace
+
+extern "C" {
+
+im_status im_adamw_create(const im_adamw_tensor* tensors, int32_t n_tensors, int32_t state_bits, int32_t grad_dtype,
+                          void* stream, im_adamw** out) {
+  LEARN_CHECK(out, "out is NULL");
+  LEARN_CHECK(n_tensors >= 0 && n_tensors <= IM_MAX_TENSORS, "n_tensors out of range");
+  LEARN_CHECK(n_tensors == 0 || tensors, "tensors is NULL");
+  LEARN_CHECK(state_bits == 32 || state_bits == 8, "state_bits is 32 or 8");
+  LEARN_CHECK(grad_dtype == IM_F32 || grad_dtype == IM_BF16, "grad_dtype out of range");
+  for (int i = 0; i < n_tensors; ++i) LEARN_OK(check_tensor(tensors[i], state_bits, grad_dtype, i));
+  im_adamw* o = new (std::nothrow) im_adamw();
+  if (!o) return fail(IM_ENOMEM, "out of host memory");
+  hipError_t e = hipGetDevice(&o->device);
+  try {
+    std::vector<AdamwRun> runs;
+    std::vector<im_adamw_tensor> list(tensors, tensors + n_tensors);
+    for (int i = 0; i < n_tensors; ++i) {
+      const im_adamw_tensor& t = list[i];
+      const int64_t state = state_bits == 32 ? 16 : 4;
+      const bool al = aligned(t.param, 16) && aligned(t.grad, grad_dtype == IM_BF16 ? 8 : 16) && aligned(t.m, state) &&
+                      aligned(t.v, state) && aligned(t.copy, 8);
+      for (int64_t at = 0; at < t.n; at += kRun) runs.push_back(AdamwRun{at, i, al ? 1 : 0});
+    }
+    o->bits = state_bits;
+    o->grad_dtype = grad_dtype;
+    o->runs = (int64_t)runs.size();
+    const hipStream_t s = (hipStream_t)stream;
+    const std::vector<uint32_t> zero(1, 0);
+    if (e == hipSuccess && o->runs > 0x7fffffff) e = hipErrorInvalidValue;
+    if (e == hipSuccess) e = upload(&o->table, runs, s);
+    if (e == hipSuccess) e = upload(&o->tensors, list, s);
+    if (e == hipSuccess) e = upload(&o->done, zero, s);
+    const hipError_t w = hipStreamSynchronize(s);   // the host arrays end with this scope
+    if (e == hipSuccess) e = w;
+  } catch (const std::bad_alloc&) {
+    free_adamw(o);
+    return fail(IM_ENOMEM, "out of host memory");
+  }
+  if (e != hipSuccess) {
+    free_adamw(o);
+    return fail(e == hipErrorOutOfMemory ? IM_ENOMEM : IM_EHIP, "im_adamw_create: %s", hipGetErrorString(e));
+  }
+  *out = o;
+  return IM_OK;
+}
+
+im_status im_adamw_step(im_adamw* o, double lr, double beta1, double beta2, double eps, double weight_decay,
+                        int64_t* step, const float* scale, void* stream) {
+  LEARN_CHECK(o, "opt is NULL");
+  LEARN_CHECK(step, "step is NULL");
+  LEARN_CHECK(aligned(step, 8) && aligned(scale, 4), "a pointer is not aligned to its elements");
+  LEARN_CHECK(lr >= 0 && eps >= 0 && weight_decay >= 0, "lr, eps and weight_decay must be >= 0");
+  LEARN_CHECK(beta1 >= 0 && beta1 < 1 && beta2 >= 0 && beta2 < 1, "betas must be in [0, 1)");
+  AdamwArgs a = {};
+  a.table = o->table;
+  a.tensors = o->tensors;
+  a.runs = o->runs;
+  a.step = step;
+  a.scale = scale;
+  a.done = o->done;
+  a.beta1 = beta1;
+  a.beta2 = beta2;
+  a.lr = (float)lr;
+  a.beta1f = (float)beta1;
+  a.omb1 = (float)(1.0 - beta1);
+  a.beta2f = (float)beta2;
+  a.omb2 = (float)(1.0 - beta2);
+  a.eps = (float)eps;
+  a.keep = (float)(1.0 - lr * weight_decay);
+  const OnDevice on(o->device);
+  LEARN_HIP(on.err);
+  LEARN_HIP(launch_adamw(a, o->bits, o->grad_dtype, (hipStream_t)stream));
+  return IM_OK;
+}
+
+void im_adamw_destroy(im_adamw* o) {
+  if (!o) return;
+  const OnDevice on(o->device);
+  (void)hipDeviceSynchronize();
+  free_adamw(o);
+}
+
+}  // extern "C"

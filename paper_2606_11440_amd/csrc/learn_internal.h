@@ -1,0 +1,95 @@
+// Kernel argument blocks and launchers of the learner's operators.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "inframind_learn.h"
+
+namespace im {
+namespace learn {
+
+// What a row product does with its results.
+enum Epilogue {
+  kStore = 0,     // y = act(sum + b)
+  kStoreInput,    // dx = sum, zero where x <= 0 with relu_in
+  kStats,         // per row and column tile: largest logit, sum exp, sum exp (z - largest)
+  kGradLogits     // dz of a piece of the classes
+};
+
+// A product of the groups' rows with their weights: out[i][j] = sum_k A[i][k] B_g(j, k).
+struct RowArgs {
+  const int32_t* offsets;
+  int32_t G, n, K, N;         // N: output columns (of the piece, for a head)
+  const void* A;
+  int64_t lda;
+  const void* B;              // rows [N x K], or columns [K x N], per group
+  int64_t ldb, b_group;       // strides in elements
+  const float* bias;          // [G x bias_group] or NULL
+  int64_t bias_group;
+  void* C;
+  int64_t ldc;
+  int32_t relu;
+  int32_t* error;
+  int32_t row_tiles, col_tiles;   // of the launch
+  // kStoreInput
+  const void* X;              // relu_in: the layer's input
+  int64_t ldx;
+  float* sum;                 // fp32 running sums [n x N] over the pieces of a head, or NULL
+  int32_t first, last;        // piece of a head: the first starts the sums, the last stores C
+  // heads
+  int32_t V, words, col0;     // classes, mask words of a row, first class of the piece
+  const uint32_t* valid;
+  const int32_t* target;
+  float* stats;               // [col_tiles][n][3]
+  float* taken;               // [n] logit of the target
+  float* logp;
+  float* entropy;             // kStats: out; kGradLogits: in
+  float* lse;                 // kStats: out; kGradLogits: in
+  const float* dlogp;
+  const float* dentropy;
+  float* db_part;             // [row_tiles][db_width] column sums of dz
+  int64_t db_width;
+  uint8_t* live;              // [n] kGradLogits: 1 where the row adds to the gradient
+};
+
+// dW_g = sum over the group's rows of P[i][m] Q[i][n] (and db_g = sum P[i][m]).
+struct SumArgs {
+  const int32_t* offsets;
+  int32_t G, n, M, N;
+  const void* P;
+  int64_t ldp;
+  const void* Q;
+  int64_t ldq;
+  const uint8_t* live;        // rows of Q to take, or NULL (all)
+  void* dW;                   // [G x w_group], rows of N
+  int64_t w_group;
+  float* db;                  // [G x M] or NULL
+  float* part;                // [chunks][part_width] sums of groups of several chunks: M x N, then M at db_at
+  int64_t part_width, db_at;
+  int32_t chunk, chunks;      // rows of a chunk; chunks the launch covers
+  int32_t row_tiles, col_tiles;
+  int32_t* error;
+};
+
+// Tile shape of a row product of n rows in G groups with N columns, and its tiles
+// (row tiles: at most; the groups' sizes are known on the device only).
+struct RowPlan {
+  int shape;
+  int64_t row_tiles, col_tiles;
+};
+RowPlan plan_rows(int dtype, int64_t n, int64_t G, int64_t N, int cus);
+hipError_t launch_rows_product(const RowArgs& a, int dtype, int shape, int epilogue, hipStream_t s);
+
+struct SumPlan {
+  int shape;
+  int64_t row_tiles, col_tiles, chunk, chunks;
+};
+SumPlan plan_sums(int dtype, int64_t n, int64_t G, int64_t M, int64_t N, int cus);
+hipError_t launch_sums(const SumArgs& a, int dtype, int shape, hipStream_t s);
+// db_g = sum of the column sums of the group's row tiles (of `step` rows).
+hipError_t launch_bias_sum(const int32_t* offsets, int G, int n, int step, const float* part, int64_t width, float* db,
+                           hipStream_t s);
+int rows_per_tile(int shape);
+
+}  // namespace learn
+}  // namespace im

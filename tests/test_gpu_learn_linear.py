@@ -1,0 +1,213 @@
+"""GPU: grouped layers and their gradients against 64 bits (bounds: learn_util)."""
+import pytest
+
+import learn_util as U
+from gpu_util import need_gpu, note
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = "float32", "bfloat16"
+
+
+def make(n, k, m, sizes, dtype, seed=0, pad=0, relu_x=False):
+    torch = need_gpu()
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    dt = getattr(torch, dtype)
+    G = len(sizes) if sizes else 1
+
+    def normal(*s, scale=1.0, t=dt):
+        return (torch.randn(*s, device="cuda", generator=g) * scale).to(t)
+    x = normal(n, k + pad)[:, pad // 2:pad // 2 + k]
+    if relu_x:
+        x.relu_()
+    off = None
+    if sizes:
+        off = [0]
+        for s in sizes:
+            off.append(off[-1] + s)
+        assert off[-1] <= n
+    dev = None if off is None else torch.tensor(off, dtype=torch.int32, device="cuda")
+    return dict(torch=torch, x=x, W=normal(G, m, k, scale=k ** -0.5), b=normal(G, m, t=torch.float32),
+                dy=normal(n, m + pad)[:, :m], off=off, dev=dev, G=G, dt=dt)
+
+
+def run_forward(c, relu, b=True, pad=0):
+    import paper_2606_11440_amd as P
+    torch, n, m = c["torch"], c["x"].shape[0], c["W"].shape[1]
+    y = torch.full((n, m + pad), 77.0, dtype=c["dt"], device="cuda")
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    P.im_linear_forward(c["x"], c["W"], c["b"] if b else None, y[:, :m], offsets=c["dev"], relu=relu, error=err)
+    torch.cuda.synchronize()
+    assert int(err) == 0
+    if pad:
+        assert bool((y[:, m:] == 77.0).all())
+    return y[:, :m]
+
+
+def check_forward(c, relu, b=True, pad=0):
+    y = run_forward(c, relu, b, pad)
+    want, tol = U.linear(c["x"], c["W"], c["b"] if b else None, c["off"], relu)
+    end = c["off"][-1] if c["off"] else c["x"].shape[0]
+    U.close(y[:end], want[:end], tol[:end], "y")
+    assert bool((y[end:] == 77.0).all())
+
+
+def run_backward(c, relu_in, want=("dx", "dW", "db"), pad=0):
+    import paper_2606_11440_amd as P
+    torch, (n, k), (G, m, _) = c["torch"], c["x"].shape, c["W"].shape
+    o = dict(dx=torch.full((n, k + pad), 77.0, dtype=c["dt"], device="cuda")[:, :k],
+             dW=torch.full((G, m, k), 77.0, dtype=c["dt"], device="cuda"), db=torch.full((G, m), 77.0, device="cuda"))
+    o = {key: v if key in want else None for key, v in o.items()}
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    P.im_linear_backward(c["dy"], c["x"], c["W"], o["dx"], o["dW"], o["db"], offsets=c["dev"], relu_in=relu_in, error=err)
+    torch.cuda.synchronize()
+    assert int(err) == 0
+    return o
+
+
+def check_backward(c, relu_in, want=("dx", "dW", "db"), pad=0):
+    o = run_backward(c, relu_in, want, pad)
+    refs = dict(zip(("dx", "dW", "db"), U.linear_grad(c["dy"], c["x"], c["W"], c["off"], relu_in)))
+    end = c["off"][-1] if c["off"] else c["x"].shape[0]
+    for key in want:
+        ref, tol = refs[key]
+        if key == "dx":
+            assert bool((o["dx"][end:] == 77.0).all())
+            U.close(o["dx"][:end], ref[:end], tol[:end], key)
+        else:
+            U.close(o[key], ref, tol, key)
+
+
+SHAPES = [  # n, in, out, group sizes (None: no offsets)
+    (1, 1, 1, None), (1, 86, 256, None), (3, 7, 5, None), (48, 86, 256, None), (64, 64, 64, [64]), (65, 33, 65, [65]),
+    (130, 193, 129, [0, 130]), (200, 8, 8, [50, 0, 0, 149, 1]), (257, 256, 15, [100, 157]), (300, 104, 24, [7] * 40),
+    (513, 384, 128, [511]), (700, 72, 200, [0, 0, 0]), (1000, 513, 255, [1, 2, 997]),
+    (4096, 193, 512, [1000, 0, 3000, 50, 13]), (70000, 64, 48, [30000, 39000]), (900, 40, 24, [3] * 299 + [1]),
+    (40000, 520, 520, [39000, 1000]), (20000, 130, 300, None),
+]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,k,m,sizes", SHAPES)
+def test_layer(n, k, m, sizes, dtype):
+    note(f"[layer] n={n} k={k} m={m} groups={sizes and len(sizes)} {dtype}")
+    c = make(n, k, m, sizes, dtype, seed=n + k)
+    check_forward(c, relu=True)
+    check_forward(c, relu=False, b=False)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,k,m,sizes", SHAPES)
+def test_layer_gradient(n, k, m, sizes, dtype):
+    note(f"[layer gradient] n={n} k={k} m={m} groups={sizes and len(sizes)} {dtype}")
+    check_backward(make(n, k, m, sizes, dtype, seed=n + m), relu_in=False)
+    check_backward(make(n, k, m, sizes, dtype, seed=n + m + 1, relu_x=True), relu_in=True)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("pad", [1, 3, 8, 10])
+def test_strides(dtype, pad):
+    """Rows cut out of wider ones, at every alignment of 2 (4) bytes."""
+    note(f"[strides] pad={pad} {dtype}")
+    for n, k, m, sizes in ((77, 45, 33, [70]), (600, 200, 130, [300, 299])):
+        c = make(n, k, m, sizes, dtype, seed=pad, pad=pad)
+        check_forward(c, relu=True, pad=pad)
+        check_backward(c, relu_in=True, pad=pad)
+
+
+@pytest.mark.parametrize("want", [("dx",), ("dW",), ("db",), ("dW", "db")])
+def test_some_gradients(want):
+    note(f"[some gradients] {want}")
+    check_backward(make(500, 100, 70, [400, 90], BF16, seed=5), relu_in=False, want=want)
+    check_backward(make(500, 100, 70, None, F32, seed=6), relu_in=True, want=want)
+
+
+def test_no_rows():
+    c = make(0, 20, 30, None, BF16)
+    run_forward(c, True)
+    o = run_backward(c, False)
+    assert bool((o["dW"] == 0).all()) and bool((o["db"] == 0).all())
+    c = make(5, 20, 30, [0, 0], BF16)
+    assert bool((run_forward(c, True) == 77.0).all())
+    o = run_backward(c, False)
+    assert bool((o["dW"] == 0).all()) and bool((o["db"] == 0).all()) and bool((o["dx"] == 77.0).all())
+
+
+def test_what_is_not_read_does_not_matter():
+    """Not-a-numbers behind the last group's rows, between strided rows and in
+    other groups' weights stay where they are."""
+    note("[unread]")
+    c = make(400, 90, 60, [150, 0, 200], BF16, seed=8, pad=6)
+    torch = c["torch"]
+    nan = float("nan")
+    wide_x = torch.full((400, 96), nan, dtype=torch.bfloat16, device="cuda")
+    wide_x[:350, 3:93] = c["x"][:350]
+    wide_dy = torch.full((400, 61), nan, dtype=torch.bfloat16, device="cuda")
+    wide_dy[:350, 1:] = c["dy"][:350]
+    c["x"], c["dy"] = wide_x[:, 3:93], wide_dy[:, 1:]
+    c["W"][1] = nan
+    c["b"][1] = nan
+    y = run_forward(c, True)
+    assert bool(torch.isfinite(y).all())
+    o = run_backward(c, True)
+    assert all(bool(torch.isfinite(v).all()) for v in o.values())
+
+
+def test_values_that_are_not_finite_travel():
+    c = make(100, 40, 50, None, F32, seed=9)
+    torch = c["torch"]
+    c["x"][3, 5] = float("nan")
+    c["x"][4, 5] = float("inf")
+    y = run_forward(c, True)
+    assert bool(torch.isnan(y[3]).all()) and bool(torch.isfinite(y[:3]).all()) and bool(torch.isfinite(y[5:]).all())
+    assert bool(((y[4] == 0) | torch.isposinf(y[4])).all())
+
+
+@pytest.mark.parametrize("off", [[0, 50, 40, 100], [0, -1, 50, 100], [1, 10, 20, 30], [0, 10, 20, 101]])
+def test_broken_offsets(off):
+    """Nothing is computed and IM_ERR_COUNT is raised."""
+    import paper_2606_11440_amd as P
+    note(f"[broken offsets] {off}")
+    c = make(100, 40, 50, [30, 30, 40], BF16, seed=10)
+    torch = c["torch"]
+    dev = torch.tensor(off, dtype=torch.int32, device="cuda")
+    y = torch.full((100, 50), 77.0, dtype=torch.bfloat16, device="cuda")
+    dx, dW = torch.full_like(c["x"], 77.0), torch.full_like(c["W"], 77.0)
+    db = torch.full_like(c["b"], 77.0)
+    for i in range(2):
+        err = torch.zeros(1, dtype=torch.int32, device="cuda")
+        if i == 0:
+            P.im_linear_forward(c["x"], c["W"], c["b"], y, offsets=dev, error=err)
+        else:
+            P.im_linear_backward(c["dy"], c["x"], c["W"], dx, dW, db, offsets=dev, error=err)
+        torch.cuda.synchronize()
+        assert int(err) == P._lib.IM_ERR_COUNT
+    assert all(bool((t == 77.0).all()) for t in (y, dx, dW, db))
+
+
+def test_same_bits_each_time():
+    c = make(30000, 100, 90, [20000, 9000], BF16, seed=11)
+    torch = c["torch"]
+    a, b = run_backward(c, True), run_backward(c, True)
+    assert all(torch.equal(a[k], b[k]) for k in a)
+
+
+def test_refused_tensors():
+    import paper_2606_11440_amd as P
+    c = make(20, 16, 24, None, BF16)
+    torch = c["torch"]
+    x, W, b = c["x"], c["W"], c["b"]
+    y = torch.empty(20, 24, dtype=torch.bfloat16, device="cuda")
+    bad = [dict(x=x.float()), dict(x=x.T), dict(x=x[:, :8]), dict(W=W.float()), dict(W=W.transpose(1, 2)),
+           dict(b=b.bfloat16()), dict(b=b[:, :8]), dict(y=y.float()), dict(y=y[:10]), dict(y=y[:, ::2]),
+           dict(x=x[:1].expand(20, 16)), dict(W=W.expand(2, 24, 16).contiguous()), dict(b=b.cpu()), dict(y=y.cpu()),
+           dict(offsets=torch.zeros(2, dtype=torch.int64, device="cuda")),
+           dict(offsets=torch.zeros(3, dtype=torch.int32, device="cuda")), dict(error=torch.zeros(1, device="cuda"))]
+    for over in bad:
+        a = dict(x=x, W=W, b=b, y=y) | over
+        with pytest.raises(P.IMError) as e:
+            P.im_linear_forward(**a)
+        assert e.value.status == P._lib.IM_EINVAL
+    c = make(5000, 16, 24, [2000, 3000], BF16)
+    for ws in (torch.empty(16, dtype=torch.uint8, device="cuda"), torch.empty(1 << 24, dtype=torch.uint8)):
+        with pytest.raises(P.IMError):
+            P.im_linear_backward(c["dy"], c["x"], c["W"], dW=torch.empty_like(c["W"]), offsets=c["dev"], workspace=ws)

@@ -1,0 +1,161 @@
+"""The learner's C ABI on a machine without a GPU: exports, and every refusal
+that is decided before a device is touched."""
+import ctypes
+import os
+import re
+
+import pytest
+
+import paper_2606_11440_amd as P
+from paper_2606_11440_amd import learn
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+EINVAL = P._lib.IM_EINVAL
+A = ctypes.c_void_p(4096)   # an aligned address that is never dereferenced
+
+
+def L():
+    return learn.load_learn()
+
+
+def test_library_exports_every_declared_symbol():
+    with open(os.path.join(ROOT, "include", "inframind_learn.h")) as f:
+        names = set(re.findall(r"\b(im_[a-z_]+)\s*\(", f.read()))
+    lib = ctypes.CDLL(learn.LEARN_PATH)
+    assert not [n for n in names if not hasattr(lib, n)]
+    assert names == set(P.LEARN_EXPORTED)
+
+
+def linear_desc(**kw):
+    d = learn.ImLinearDesc(1, 8, 16, 24, 1, 0, 0, 0, 16, 24, 16)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+def head_desc(**kw):
+    d = learn.ImHeadDesc(1, 8, 16, 24, 1, 0, 0, 0, 16, 16)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+BAD_LINEAR = [dict(n_groups=0), dict(n_groups=1025), dict(n_rows=-1), dict(in_dim=0), dict(in_dim=65537),
+              dict(out_dim=0), dict(out_dim=65537), dict(dtype=2), dict(relu=2), dict(relu_in=-1)]
+BAD_HEAD = [dict(n_groups=0), dict(n_groups=1025), dict(n_rows=-1), dict(dim=0), dict(dim=65537), dict(n_classes=0),
+            dict(n_classes=(1 << 22) + 1), dict(dtype=-1), dict(relu_in=2)]
+
+
+@pytest.mark.parametrize("over", BAD_LINEAR)
+def test_bad_layers(over):
+    d, out = linear_desc(**over), ctypes.c_int64(7)
+    assert L().im_linear_workspace(ctypes.byref(d), 0, ctypes.byref(out)) == EINVAL and out.value == 7
+    assert L().im_linear_forward(ctypes.byref(d), A, A, A, A, A, None, 0, None, None) == EINVAL
+    assert L().im_linear_backward(ctypes.byref(d), A, A, A, A, A, A, A, A, 1 << 40, None, None) == EINVAL
+    assert P.im_learn_last_error() != "no error"
+
+
+@pytest.mark.parametrize("over", BAD_HEAD)
+def test_bad_heads(over):
+    d, out = head_desc(**over), ctypes.c_int64(7)
+    assert L().im_head_workspace(ctypes.byref(d), 1, ctypes.byref(out)) == EINVAL and out.value == 7
+    assert L().im_head_forward(ctypes.byref(d), A, A, A, A, None, A, A, A, A, A, 1 << 40, None, None) == EINVAL
+    assert L().im_head_backward(ctypes.byref(d), A, A, A, A, None, A, A, A, A, A, A, A, A, A, 1 << 40, None,
+                                None) == EINVAL
+
+
+def test_layer_arguments():
+    f = L().im_linear_forward
+    d = linear_desc()
+    R = ctypes.byref
+    odd = ctypes.c_void_p(4097)
+    for args in [(None, A, A, A, A, A, None, 0, None, None),
+                 (R(d), None, None, A, A, A, None, 0, None, None), (R(d), None, A, None, A, A, None, 0, None, None),
+                 (R(d), None, A, A, A, None, None, 0, None, None), (R(d), None, odd, A, A, A, None, 0, None, None),
+                 (R(d), None, A, A, odd, A, None, 0, None, None), (R(d), odd, A, A, A, A, None, 0, None, None),
+                 (R(linear_desc(n_groups=2)), None, A, A, A, A, None, 0, None, None),
+                 (R(linear_desc(ld_x=15)), None, A, A, A, A, None, 0, None, None),
+                 (R(linear_desc(ld_y=23)), None, A, A, A, A, None, 0, None, None)]:
+        assert f(*args) == EINVAL
+    b = L().im_linear_backward
+    d = linear_desc(n_groups=3, n_rows=5000)
+    need = ctypes.c_int64(0)
+    assert L().im_linear_workspace(R(d), 1, R(need)) == 0 and need.value > 0
+    assert L().im_linear_workspace(R(d), 2, R(need)) == EINVAL
+    assert L().im_linear_workspace(R(d), 1, None) == EINVAL
+    for args in [(R(d), A, A, A, A, A, A, A, None, 1 << 40, None, None),
+                 (R(d), A, A, A, A, A, A, A, A, need.value - 1, None, None),
+                 (R(d), A, A, A, A, A, A, A, ctypes.c_void_p(4096 + 128), 1 << 40, None, None),
+                 (R(d), A, None, A, A, A, A, A, A, 1 << 40, None, None),
+                 (R(d), A, A, None, A, A, A, A, A, 1 << 40, None, None),
+                 (R(d), A, A, A, None, A, A, A, A, 1 << 40, None, None),
+                 (R(linear_desc(n_groups=3, n_rows=5000, ld_dx=3)), A, A, A, A, A, A, A, A, 1 << 40, None, None)]:
+        assert b(*args) == EINVAL
+    # tiles beyond what a launch counts
+    big = linear_desc(n_rows=2 ** 31 - 1, in_dim=65536, out_dim=65536, ld_x=65536, ld_y=65536)
+    assert f(R(big), None, A, A, A, A, None, 0, None, None) == P._lib.IM_EUNSUPPORTED
+
+
+def test_head_arguments():
+    R = ctypes.byref
+    d = head_desc()
+    f = L().im_head_forward
+    for args in [(R(d), None, None, A, A, None, A, A, A, A, A, 1 << 40, None, None),
+                 (R(d), None, A, None, A, None, A, A, A, A, A, 1 << 40, None, None),
+                 (R(d), None, A, A, A, None, None, A, A, A, A, 1 << 40, None, None),
+                 (R(d), None, A, A, A, None, A, None, A, A, A, 1 << 40, None, None),
+                 (R(head_desc(ld_h=15)), None, A, A, A, None, A, A, A, A, A, 1 << 40, None, None),
+                 (R(head_desc(n_groups=2)), None, A, A, A, None, A, A, A, A, A, 1 << 40, None, None),
+                 (R(head_desc(n_classes=5000)), None, A, A, A, None, A, A, A, A, None, 0, None, None)]:
+        assert f(*args) == EINVAL
+    b = L().im_head_backward
+    need = ctypes.c_int64(0)
+    assert L().im_head_workspace(R(d), 1, R(need)) == 0 and need.value > 0
+    ok = [R(d), None, A, A, A, None, A, A, A, A, A, A, A, A, A, 1 << 40, None, None]
+    for i in (2, 3, 6, 7, 9):                      # h, W, target, lse, dlogp
+        assert b(*(ok[:i] + [None] + ok[i + 1:])) == EINVAL, i
+    assert b(*(ok[:8] + [None] + ok[9:])) == EINVAL           # dentropy without entropy
+    assert b(*(ok[:14] + [None] + ok[15:])) == EINVAL         # workspace
+    assert b(*(ok[:15] + [need.value - 1] + ok[16:])) == EINVAL
+    assert b(R(head_desc(ld_dh=2)), *ok[1:]) == EINVAL
+
+
+def tensor(**kw):
+    t = learn.ImAdamwTensor(4096, 4096, 4096, 4096, None, None, None, 10, 1, 0)
+    for k, v in kw.items():
+        setattr(t, k, v)
+    return t
+
+
+def test_adamw_arguments():
+    R = ctypes.byref
+    out = ctypes.c_void_p()
+
+    def create(t, bits=32, gd=0, n=1, o=R(out)):
+        return L().im_adamw_create(None if t is None else R(t), n, bits, gd, None, o)
+    for t in (tensor(param=None), tensor(grad=None), tensor(m=None), tensor(v=None), tensor(n=-1), tensor(decay=2),
+              tensor(param=4098), tensor(m=4098), tensor(copy=4097), tensor(m_scale=4096, v_scale=4096)):
+        assert create(t) == EINVAL
+    assert create(tensor(), bits=8) == EINVAL and create(tensor(m_scale=4096), bits=8) == EINVAL
+    assert create(tensor(), bits=16) == EINVAL and create(tensor(), gd=2) == EINVAL
+    assert create(tensor(), n=-1) == EINVAL and create(None) == EINVAL and create(tensor(), o=None) == EINVAL
+    assert create(tensor(), n=65537) == EINVAL
+    assert not out.value
+    step = L().im_adamw_step
+    assert step(None, 1e-3, 0.9, 0.99, 1e-8, 0.0, A, None, None) == EINVAL
+    L().im_adamw_destroy(None)
+
+
+def test_tensors_are_checked():
+    """The binding refuses what the library cannot see: types, devices, shapes."""
+    import torch
+    x = torch.zeros(4, 8)
+    with pytest.raises(P.IMError) as e:
+        P.im_linear_forward(x, torch.zeros(2, 8), None, torch.zeros(4, 2))
+    assert e.value.status == EINVAL and "GPU" in str(e.value)
+    with pytest.raises(P.IMError):
+        P.im_head_forward(x, torch.zeros(2, 8), None, torch.zeros(4, dtype=torch.int32), torch.zeros(4))
+    with pytest.raises(P.IMError):
+        P.AdamW([dict(param=x, grad=x, m=x, v=x)])
+    with pytest.raises(P.IMError):
+        P.AdamW([], bits=4)
