@@ -19,7 +19,7 @@
  *     caller-owned buffers must stay valid until the stream work that uses
  *     them has finished. Outputs must not overlap inputs or one another.
  *   - Matrices are row-major. ld_* are row strides in elements (at least the
- *     row's width); weights and their gradients are contiguous. 16-bit data
+ *     row's width, at most IM_MAX_LD); weights and their gradients are contiguous. 16-bit data
  *     needs 2-byte, 32-bit data 4-byte alignment, nothing more.
  *   - dtype IM_BF16: bf16 activations, weights and their gradients; IM_F32:
  *     fp32. Products are accumulated in fp32; biases, their gradients and the
@@ -47,6 +47,7 @@ extern "C" {
 
 #define IM_MAX_GROUPS 1024        /* n_groups                                          */
 #define IM_MAX_DIM    65536       /* in_dim, out_dim, dim                              */
+#define IM_MAX_LD     (1 << 22)   /* row strides (elements)                            */
 #define IM_MAX_CLASSES (1 << 22)  /* n_classes                                         */
 #define IM_MAX_TENSORS 65536      /* tensors of an im_adamw                            */
 #define IM_STATE_BLOCK 256        /* elements of an 8-bit state that share a scale     */

@@ -12,7 +12,7 @@ using namespace im::learn;
 struct im_adamw {
   int device = 0;
   int bits = 32, grad_dtype = IM_F32;
-  int64_t runs = 0;
+  int64_t runs = 0, blocks = 1;
   AdamwRun* table = nullptr;
   im_adamw_tensor* tensors = nullptr;
   uint32_t* done = nullptr;
@@ -69,6 +69,8 @@ struct Sections {
 
 int64_t size_of(int dtype) { return dtype == IM_BF16 ? 2 : 4; }
 bool aligned(const void* p, int64_t a) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(a - 1)) == 0; }
+
+bool stride_ok(int64_t ld, int64_t width) { return ld >= width && ld <= IM_MAX_LD; }
 
 im_status check_groups(int32_t G, const int32_t* offsets) {
   LEARN_CHECK(offsets || G == 1, "offsets NULL needs n_groups = 1");
@@ -151,7 +153,7 @@ im_status im_linear_forward(const im_linear_desc* d, const int32_t* offsets, con
   LEARN_OK(check_linear(d));
   LEARN_OK(check_groups(d->n_groups, offsets));
   const int64_t e = size_of(d->dtype);
-  LEARN_CHECK(d->ld_x >= d->in_dim && d->ld_y >= d->out_dim, "ld_x or ld_y is less than the row");
+  LEARN_CHECK(stride_ok(d->ld_x, d->in_dim) && stride_ok(d->ld_y, d->out_dim), "ld_x or ld_y out of range");
   LEARN_CHECK(W && (d->n_rows == 0 || (x && y)), "x, W or y is NULL");
   LEARN_CHECK(aligned(x, e) && aligned(W, e) && aligned(y, e) && aligned(b, 4) && aligned(error, 4),
               "a pointer is not aligned to its elements");
@@ -184,10 +186,10 @@ im_status im_linear_backward(const im_linear_desc* d, const int32_t* offsets, co
   const int64_t e = size_of(d->dtype);
   const bool some = d->n_rows > 0;
   LEARN_CHECK(!some || dy, "dy is NULL");
-  LEARN_CHECK(d->ld_y >= d->out_dim, "ld_y is less than the row");
-  LEARN_CHECK(!dx || !some || (W && d->ld_dx >= d->in_dim), "dx needs W and ld_dx >= in_dim");
-  LEARN_CHECK(!some || !(dW || (dx && d->relu_in)) || (x && d->ld_x >= d->in_dim),
-              "dW, and dx with relu_in, need x and ld_x >= in_dim");
+  LEARN_CHECK(stride_ok(d->ld_y, d->out_dim), "ld_y out of range");
+  LEARN_CHECK(!dx || !some || (W && stride_ok(d->ld_dx, d->in_dim)), "dx needs W and a valid ld_dx");
+  LEARN_CHECK(!some || !(dW || (dx && d->relu_in)) || (x && stride_ok(d->ld_x, d->in_dim)),
+              "dW, and dx with relu_in, need x and a valid ld_x");
   LEARN_CHECK(aligned(dy, e) && aligned(x, e) && aligned(W, e) && aligned(dx, e) && aligned(dW, e) && aligned(db, 4) &&
                   aligned(error, 4),
               "a pointer is not aligned to its elements");
@@ -323,7 +325,7 @@ im_status im_head_forward(const im_head_desc* d, const int32_t* offsets, const v
   LEARN_OK(check_head(d));
   LEARN_OK(check_groups(d->n_groups, offsets));
   const int64_t e = size_of(d->dtype);
-  LEARN_CHECK(d->ld_h >= d->dim, "ld_h is less than the row");
+  LEARN_CHECK(stride_ok(d->ld_h, d->dim), "ld_h out of range");
   LEARN_CHECK(W && (d->n_rows == 0 || (h && target && logp)), "h, W, target or logp is NULL");
   LEARN_CHECK(aligned(h, e) && aligned(W, e) && aligned(b, 4) && aligned(valid, 4) && aligned(target, 4) &&
                   aligned(logp, 4) && aligned(entropy, 4) && aligned(lse, 4) && aligned(error, 4),
@@ -362,7 +364,7 @@ im_status im_head_backward(const im_head_desc* d, const int32_t* offsets, const 
   LEARN_OK(check_groups(d->n_groups, offsets));
   const int64_t e = size_of(d->dtype);
   const bool some = d->n_rows > 0;
-  LEARN_CHECK(d->ld_h >= d->dim && (!dh || d->ld_dh >= d->dim), "ld_h or ld_dh is less than the row");
+  LEARN_CHECK(stride_ok(d->ld_h, d->dim) && (!dh || stride_ok(d->ld_dh, d->dim)), "ld_h or ld_dh out of range");
   LEARN_CHECK(!some || (h && W && target && lse && dlogp), "h, W, target, lse or dlogp is NULL");
   LEARN_CHECK(!some || !dentropy || entropy, "dentropy needs entropy");
   LEARN_CHECK(aligned(h, e) && aligned(W, e) && aligned(dh, e) && aligned(dW, e) && aligned(b, 4) && aligned(valid, 4) &&
@@ -382,6 +384,7 @@ im_status im_head_backward(const im_head_desc* d, const int32_t* offsets, const 
     const char* Wp = static_cast<const char*>(W) + c0 * d->dim * e;
     if (some) {
       RowArgs a = row_args(offsets, d->n_groups, d->n_rows, w.logits, error);
+      a.col_tiles = (int32_t)((width + cols_per_tile(w.logits.shape) - 1) / cols_per_tile(w.logits.shape));
       a.K = d->dim;
       a.N = (int32_t)width;
       a.V = d->n_classes;
@@ -444,7 +447,8 @@ im_status im_head_backward(const im_head_desc* d, const int32_t* offsets, const 
       a.db_at = (width * d->dim + 3) & ~(int64_t)3;
       a.chunk = (int32_t)w.sums.sums.chunk;
       a.chunks = (int32_t)w.sums.sums.chunks;
-      a.row_tiles = (int32_t)w.sums.sums.row_tiles;
+      const int64_t tile = rows_per_sum(w.sums.sums.shape);
+      a.row_tiles = (int32_t)((width + tile - 1) / tile);
       a.col_tiles = (int32_t)w.sums.sums.col_tiles;
       a.error = error;
       LEARN_HIP(launch_sums(a, d->dtype, w.sums.sums.shape, s));
@@ -539,6 +543,7 @@ im_status im_adamw_create(const im_adamw_tensor* tensors, int32_t n_tensors, int
     o->bits = state_bits;
     o->grad_dtype = grad_dtype;
     o->runs = (int64_t)runs.size();
+    o->blocks = 8 * (int64_t)compute_units();
     const hipStream_t s = (hipStream_t)stream;
     const std::vector<uint32_t> zero(1, 0);
     if (e == hipSuccess && o->runs > 0x7fffffff) e = hipErrorInvalidValue;
@@ -570,6 +575,7 @@ im_status im_adamw_step(im_adamw* o, double lr, double beta1, double beta2, doub
   a.table = o->table;
   a.tensors = o->tensors;
   a.runs = o->runs;
+  a.blocks = o->blocks;
   a.step = step;
   a.scale = scale;
   a.done = o->done;

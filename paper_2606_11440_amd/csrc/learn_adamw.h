@@ -20,6 +20,7 @@ struct AdamwArgs {
   const AdamwRun* table;
   const im_adamw_tensor* tensors;
   int64_t runs;
+  int64_t blocks;            // grid at most: blocks share the runs
   int64_t* step;
   const float* scale;
   uint32_t* done;

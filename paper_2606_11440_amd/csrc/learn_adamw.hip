@@ -109,95 +109,148 @@ __device__ __forceinline__ uint32_t encode(f32x4 y, bool least, float& scale) {
   return to_e4m3(x);
 }
 
-template <int BITS, bool HALF>
-__global__ __launch_bounds__(256) void adamw_kernel(const AdamwArgs a) {
-  __shared__ float rate[2];
-  if (threadIdx.x == 0) {
-    const double t = (double)(*a.step + 1);
-    rate[0] = (float)(1.0 / (1.0 - pow(a.beta1, t)));
-    rate[1] = (float)(1.0 / (1.0 - pow(a.beta2, t)));
+// x^t by squaring: relative error below t 2^-52, and t x^t is bounded.
+__device__ __forceinline__ double power(double x, int64_t t) {
+  double y = 1.0;
+  for (; t > 0; t >>= 1) {
+    if (t & 1) y *= x;
+    x *= x;
   }
-  __syncthreads();
-  const float r1 = rate[0], r2 = rate[1], scale = a.scale ? *a.scale : 1.f;
-  if (a.runs > 0) {
-    const AdamwRun run = a.table[blockIdx.x];
-    const im_adamw_tensor t = a.tensors[run.tensor];
-    const Global<float> param = global<float>(t.param), mf = global<float>(t.m), vf = global<float>(t.v);
-    const Global<float> m_scale = global<float>(t.m_scale), v_scale = global<float>(t.v_scale);
-    const Global<uint8_t> mb = global<uint8_t>(t.m), vb = global<uint8_t>(t.v);
-    const float keep = t.decay ? a.keep : 1.f;
-    const bool al = run.aligned;
-    const int64_t end = run.first + kRun < t.n ? run.first + kRun : t.n;
-    const int lane = threadIdx.x % 64;
-    for (int64_t at = run.first + (threadIdx.x / 64) * 256; at < end; at += 1024) {
-      const int64_t e = at + lane * 4;
-      const int left = end - e >= 4 ? 4 : (int)(end - e);
-      f32x4 p = load_f(param + e, left, al), m, v;
-      const f32x4 g0 = HALF ? load_h(global<const __bf16>(t.grad) + e, left, al)
-                            : load_f(global<const float>(t.grad) + e, left, al);
-      if constexpr (BITS == 32) {
-        m = load_f(mf + e, left, al);
-        v = load_f(vf + e, left, al);
-      } else {
-        const uint32_t cm = load_b(mb + e, left, al);
-        const uint32_t cv = load_b(vb + e, left, al);
-        const float ms = m_scale[at / 256], vs = v_scale[at / 256];
-        m = from_e4m3(cm);
-        v = from_e4m3(cv);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          m[i] = m[i] * ms;
-          const float r = v[i] * vs;
-          v[i] = r * r;
-        }
-      }
+  return y;
+}
+
+// Four elements a lane: one block of an 8-bit state a wave.
+template <int BITS>
+struct Four {
+  f32x4 p, g, m, v;
+  uint32_t cm, cv;
+  float ms, vs;
+};
+
+template <int BITS, bool HALF>
+struct Step {
+  const AdamwArgs& a;
+  Global<float> param, mf, vf, m_scale, v_scale;
+  Global<uint8_t> mb, vb;
+  Global<const float> gf;
+  Global<const __bf16> gh;
+  Global<__bf16> copy;
+  float keep, r1, r2, scale;
+  bool copies;
+
+  __device__ __forceinline__ Step(const AdamwArgs& args, const im_adamw_tensor& t, float r1_, float r2_, float scale_)
+      : a(args), r1(r1_), r2(r2_), scale(scale_) {
+    param = global<float>(t.param);
+    mf = global<float>(t.m), vf = global<float>(t.v);
+    mb = global<uint8_t>(t.m), vb = global<uint8_t>(t.v);
+    m_scale = global<float>(t.m_scale), v_scale = global<float>(t.v_scale);
+    gf = global<const float>(t.grad), gh = global<const __bf16>(t.grad);
+    copy = global<__bf16>(t.copy), copies = t.copy != nullptr;
+    keep = t.decay ? a.keep : 1.f;
+  }
+  // the wave's elements at .. at + 255, of which lane l has left (from l 4 on; 4 and al: at once)
+  __device__ __forceinline__ void load(Four<BITS>& f, int64_t at, int left, bool al) const {
+    const int64_t e = at + (int)(threadIdx.x % 64) * 4;
+    f.p = load_f(param + e, left, al);
+    f.g = HALF ? load_h(gh + e, left, al) : load_f(gf + e, left, al);
+    if constexpr (BITS == 32) {
+      f.m = load_f(mf + e, left, al);
+      f.v = load_f(vf + e, left, al);
+    } else {
+      f.cm = load_b(mb + e, left, al);
+      f.cv = load_b(vb + e, left, al);
+      f.ms = m_scale[at / 256];
+      f.vs = v_scale[at / 256];
+    }
+  }
+  __device__ __forceinline__ void step(Four<BITS>& f, int64_t at, int left, bool al) const {
+    const int64_t e = at + (int)(threadIdx.x % 64) * 4;
+    if constexpr (BITS == 8) {
+      f.m = from_e4m3(f.cm);
+      f.v = from_e4m3(f.cv);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float g = g0[i] * scale;
-        m[i] = m[i] * a.beta1f + g * a.omb1;
-        v[i] = v[i] * a.beta2f + g * g * a.omb2;
-        const float d = __fsqrt_rn(v[i] * r2) + a.eps;
-        p[i] = p[i] * keep - __fdiv_rn(m[i] * r1, d) * a.lr;
+        f.m[i] = f.m[i] * f.ms;
+        const float r = f.v[i] * f.vs;
+        f.v[i] = r * r;
       }
-      store_f(param + e, p, left, al);
-      if (t.copy) {
-        const Global<__bf16> c = global<__bf16>(t.copy) + e;
-        if (left >= 4 && al) {
-          bf16x4 o;
+    }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[i] = (__bf16)p[i];
-          *(Global<bf16x4>)c = o;
-        } else {
+    for (int i = 0; i < 4; ++i) {
+      const float g = f.g[i] * scale;
+      f.m[i] = f.m[i] * a.beta1f + g * a.omb1;
+      f.v[i] = f.v[i] * a.beta2f + g * g * a.omb2;
+      const float d = __fsqrt_rn(f.v[i] * r2) + a.eps;
+      f.p[i] = f.p[i] * keep - __fdiv_rn(f.m[i] * r1, d) * a.lr;
+    }
+    store_f(param + e, f.p, left, al);
+    if (copies) {
+      if (left >= 4 && al) {
+        bf16x4 o;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (i < left) c[i] = (__bf16)p[i];
-        }
-      }
-      if constexpr (BITS == 32) {
-        store_f(mf + e, m, left, al);
-        store_f(vf + e, v, left, al);
+        for (int i = 0; i < 4; ++i) o[i] = (__bf16)f.p[i];
+        *(Global<bf16x4>)(copy + e) = o;
       } else {
-        f32x4 r;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          r[i] = i < left ? __fsqrt_rn(v[i]) : 0.f;
-          m[i] = i < left ? m[i] : 0.f;
-        }
-        float ms, vs;
-        store_b(mb + e, encode(m, false, ms), left, al);
-        store_b(vb + e, encode(r, true, vs), left, al);
-        if (lane == 0) {
-          m_scale[at / 256] = ms;
-          v_scale[at / 256] = vs;
-        }
+        for (int i = 0; i < 4; ++i)
+          if (i < left) copy[e + i] = (__bf16)f.p[i];
+      }
+    }
+    if constexpr (BITS == 32) {
+      store_f(mf + e, f.m, left, al);
+      store_f(vf + e, f.v, left, al);
+    } else {
+      f32x4 r;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        r[i] = i < left ? __fsqrt_rn(f.v[i]) : 0.f;
+        f.m[i] = i < left ? f.m[i] : 0.f;
+      }
+      float ms, vs;
+      store_b(mb + e, encode(f.m, false, ms), left, al);
+      store_b(vb + e, encode(r, true, vs), left, al);
+      if (threadIdx.x % 64 == 0) {
+        m_scale[at / 256] = ms;
+        v_scale[at / 256] = vs;
+      }
+    }
+  }
+};
+
+template <int BITS, bool HALF>
+__global__ __launch_bounds__(256) void adamw_kernel(const AdamwArgs a) {
+  const int64_t t = *a.step + 1;
+  const float r1 = (float)(1.0 / (1.0 - power(a.beta1, t))), r2 = (float)(1.0 / (1.0 - power(a.beta2, t)));
+  const float scale = a.scale ? *a.scale : 1.f;
+  const int wave = threadIdx.x / 64, lane4 = (threadIdx.x % 64) * 4;
+  for (int64_t k = blockIdx.x; k < a.runs; k += gridDim.x) {
+    const AdamwRun run = a.table[k];
+    const im_adamw_tensor tensor = a.tensors[run.tensor];
+    const Step<BITS, HALF> s(a, tensor, r1, r2, scale);
+    const int64_t first = run.first + wave * 256;
+    if (run.aligned && run.first + kRun <= tensor.n) {   // all of the wave's loads in flight at once
+      Four<BITS> f[kRun / 1024];
+#pragma unroll
+      for (int i = 0; i < kRun / 1024; ++i) s.load(f[i], first + i * 1024, 4, true);
+#pragma unroll
+      for (int i = 0; i < kRun / 1024; ++i) s.step(f[i], first + i * 1024, 4, true);
+    } else {
+      const int64_t end = run.first + kRun < tensor.n ? run.first + kRun : tensor.n;
+      for (int64_t at = first; at < end; at += 1024) {
+        const int64_t over = end - at - lane4;
+        const int left = over >= 4 ? 4 : (int)over;
+        Four<BITS> f;
+        s.load(f, at, left, run.aligned);
+        s.step(f, at, left, run.aligned);
       }
     }
   }
   // the last block to end counts the step (every block has read it by then)
+  __syncthreads();
   if (threadIdx.x == 0) {
     const uint32_t done = __hip_atomic_fetch_add(a.done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
     if (done == gridDim.x - 1) {
-      *a.step += 1;
+      *a.step = t;
       *a.done = 0;
     }
   }
@@ -206,7 +259,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwArgs a) {
 }  // namespace
 
 hipError_t launch_adamw(const AdamwArgs& a, int bits, int grad_dtype, hipStream_t s) {
-  const dim3 grid((unsigned)(a.runs > 0 ? a.runs : 1)), block(256);
+  const dim3 grid((unsigned)(a.runs < 1 ? 1 : (a.runs < a.blocks ? a.runs : a.blocks))), block(256);
   if (bits == 32) {
     if (grad_dtype == IM_BF16) hipLaunchKernelGGL((adamw_kernel<32, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((adamw_kernel<32, false>), grid, block, 0, s, a);

@@ -89,7 +89,9 @@ hipError_t launch_sums(const SumArgs& a, int dtype, int shape, hipStream_t s);
 // db_g = sum of the column sums of the group's row tiles (of `step` rows).
 hipError_t launch_bias_sum(const int32_t* offsets, int G, int n, int step, const float* part, int64_t width, float* db,
                            hipStream_t s);
-int rows_per_tile(int shape);
+int rows_per_tile(int shape);   // of a row product
+int cols_per_tile(int shape);
+int rows_per_sum(int shape);    // rows of W a tile of the sums covers
 
 }  // namespace learn
 }  // namespace im

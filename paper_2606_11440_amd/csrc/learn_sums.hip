@@ -27,10 +27,11 @@ __device__ __forceinline__ void store_some(T* p, f32x4 v, int left) {
 }
 
 template <typename T, class S>
-__global__ __launch_bounds__(S::NT) void sums_kernel(const SumArgs a) {
-  using P = ColTile<T, S::BM, S::NT>;
-  using Q = ColTile<T, S::BN, S::NT>;
-  __shared__ __attribute__((aligned(16))) char lds[2 * (P::kBytes + Q::kBytes)];
+__global__ __launch_bounds__(S::NT, S::kWaves) void sums_kernel(const SumArgs a) {
+  using P = ColTile<T, S::BM, S::NT, S::D, S::SB>;
+  using Q = ColTile<T, S::BN, S::NT, S::D, S::SB>;
+  using Product = Sum<T, S, P, Q, true>;
+  __shared__ __attribute__((aligned(16))) char lds[2 * Product::kBuf];
   // the tiles of a chunk follow one another, so that they share its rows in an XCD's L2
   int chunk, tile;
   {
@@ -47,21 +48,24 @@ __global__ __launch_bounds__(S::NT) void sums_kernel(const SumArgs a) {
   if (!found) return;
 
   const int m_first = rt * S::BM, n_first = ct * S::BN, rows = part.hi - part.lo;
-  f32x4 acc[S::MI][S::NJ], sum[S::MI];
-#pragma unroll
-  for (int i = 0; i < S::MI; ++i) {
-    sum[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < S::NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, wm = wave / S::WN, wn = wave % S::WN;
   const bool bias = a.db && ct == 0 && wn == 0;
-  P p;
-  Q q;
-  p.init(static_cast<const T*>(a.P), a.ldp, m_first, a.M, part.hi);
-  q.init(static_cast<const T*>(a.Q), a.ldq, n_first, a.N, part.hi, a.live);
-  sum_stages<T, S, P, Q, true>(p, q, lds, (rows + kStage<T> - 1) / kStage<T>, acc, sum, bias, part.lo, kStage<T>,
-                               part.lo, kStage<T>);
+  // rows to leave out are looked at one by one only where the chunk has any
+  const uint8_t* live = nullptr;
+  if (a.live) {
+    int out = 0;
+    for (int i = part.lo + (int)threadIdx.x; i < part.hi; i += S::NT) out |= !a.live[i];
+    if (__syncthreads_or(out)) live = a.live;
+  }
+  Product x;
+  x.lds = lds;
+  x.steps = (rows + P::kStage - 1) / P::kStage;
+  x.alone = bias;
+  x.p.init(static_cast<const T*>(a.P), a.ldp, m_first, a.M, part.lo, part.hi);
+  x.q.init(static_cast<const T*>(a.Q), a.ldq, n_first, a.N, part.lo, part.hi, live);
+  x.run();
+  auto& acc = x.acc;
+  auto& sum = x.sum;
 
   const bool only = part.count == 1;
   float* to = only ? nullptr : a.part + (int64_t)chunk * a.part_width;
@@ -69,8 +73,12 @@ __global__ __launch_bounds__(S::NT) void sums_kernel(const SumArgs a) {
 #pragma unroll
   for (int i = 0; i < S::MI; ++i) {
     const int m = m_first + (wm * S::MI + i) * 16 + lane % 16;
+    if (bias) {
+      sum[i] += __shfl_xor(sum[i], 16);
+      sum[i] += __shfl_xor(sum[i], 32);
+      if (lane < 16 && m < a.M) (only ? a.db + (int64_t)part.g * a.M : to + a.db_at)[m] = sum[i];
+    }
     if (m >= a.M) continue;
-    if (bias && lane < 16) (only ? a.db + (int64_t)part.g * a.M : to + a.db_at)[m] = sum[i][0];
     if (!a.dW) continue;
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) {
@@ -136,9 +144,9 @@ __global__ __launch_bounds__(1024) void bias_sum_kernel(const int32_t* offsets, 
   db[g * width + col] = v;
 }
 
-using Large = Shape<2, 4, 8, 4>;    // 256 x 256, 512 threads
-using Middle = Shape<2, 2, 4, 4>;   // 128 x 128
-using Small = Shape<2, 2, 2, 2>;    // 64 x 64
+using Large = Shape<2, 4, 8, 4, 2, 64>;    // 256 x 256, 512 threads
+using Middle = Shape<2, 2, 4, 4, 2, 64>;   // 128 x 128
+using Small = Shape<2, 2, 2, 2, 4, 64>;    // 64 x 64
 
 template <typename T, class S>
 hipError_t launch(const SumArgs& a, hipStream_t s) {
@@ -163,6 +171,8 @@ hipError_t launch_type(const SumArgs& a, int shape, hipStream_t s) {
 
 }  // namespace
 
+int rows_per_sum(int shape) { return shape == 0 ? Large::BM : (shape == 1 ? Middle::BM : Small::BM); }
+
 SumPlan plan_sums(int dtype, int64_t n, int64_t G, int64_t M, int64_t N, int cus) {
   SumPlan p;
   const int64_t least = M < N ? M : N;
@@ -172,9 +182,9 @@ SumPlan plan_sums(int dtype, int64_t n, int64_t G, int64_t M, int64_t N, int cus
   p.row_tiles = (M + b - 1) / b;
   p.col_tiles = (N + b - 1) / b;
   const int64_t want = (2 * per_cu * cus + p.row_tiles * p.col_tiles - 1) / (p.row_tiles * p.col_tiles);
-  const int64_t stage = dtype == IM_BF16 ? kStage<__bf16> : kStage<float>;
+  const int64_t stage = kHalf / (dtype == IM_BF16 ? 2 : 4);
   int64_t chunk = (n + want - 1) / want;
-  if (chunk < 4 * stage) chunk = 4 * stage;
+  if (chunk < 8 * stage) chunk = 8 * stage;
   p.chunk = (chunk + stage - 1) / stage * stage;
   p.chunks = n > 0 ? (n + p.chunk - 1) / p.chunk + G - 1 : 0;
   return p;

@@ -8,7 +8,7 @@
 // columns and columns. Nothing is transposed in memory: a column tile goes to
 // LDS as it lies there and is transposed on the way to registers.
 //
-// A stage is 128 bytes of k (64 bf16 or 32 fp32). Fragments are those of
+// A stage is SB = 64 or 128 bytes of k. Fragments are those of
 // v_mfma_f32_16x16x32_bf16: lane l holds row l % 16, 8 values of k from
 // 8 (l / 16). For fp32 a fragment is 4 values of k from 4 (l / 16), used by
 // four v_mfma_f32_16x16x4_f32 in turn (the sum runs over the same k in another
@@ -29,9 +29,8 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kStageBytes = 128;
-template <typename T> constexpr int kVec = 16 / (int)sizeof(T);             // elements of a 16-byte unit
-template <typename T> constexpr int kStage = kStageBytes / (int)sizeof(T);  // k of a stage
+template <typename T> constexpr int kVec = 16 / (int)sizeof(T);   // elements of a 16-byte unit
+constexpr int kHalf = 64;                                          // bytes of k that a fragment covers
 
 template <typename T>
 __device__ __forceinline__ u32x4 load16(const T* p) {
@@ -57,56 +56,80 @@ __device__ __forceinline__ u32x4 load_few(const T* p, int n) {
   return v;
 }
 
-// A tile of ROWS memory rows with k contiguous, staged by NT threads. Rows past
-// the operand's last are read from its last row: they reach results that are
-// not stored only. In LDS a row is 8 units of 16 bytes; unit u of row r lies at
-// u ^ (r / 2 % 8), so that the 16 lanes of a fragment read touch all 64 banks
-// once (128-byte rows: two rows span the banks).
-template <typename T, int ROWS, int NT>
+__device__ __forceinline__ int clamp_units(int n, int most) { return n < 0 ? 0 : (n > most ? most : n); }
+
+// A tile of ROWS memory rows with k contiguous, staged by NT threads, D stages
+// in flight in registers. Rows past the operand's last are read from its last
+// row: they reach results that are not stored only. A unit that the row ends in
+// is read so that it ends with the row, and moved into place on the way to LDS
+// (no load depends on a branch: the waits count loads). In LDS unit u of row r
+// lies at u ^ key(r), so that the 16 lanes of a fragment read that are served
+// together (a quarter wave, or four lanes of each quarter) touch all 64 banks
+// once.
+template <typename T, int ROWS, int NT, int D, int SB>
 struct RowTile {
-  static constexpr int kUnits = ROWS * 8 / NT;
-  static constexpr int kBytes = ROWS * kStageBytes;
-  static_assert(ROWS * 8 % NT == 0 && NT % 8 == 0, "whole units per thread");
-  const T* p[kUnits];
-  u32x4 r[kUnits];
+  static constexpr int kRowUnits = SB / 16, kStage = SB / (int)sizeof(T);
+  static constexpr int kUnits = ROWS * kRowUnits / NT;
+  static constexpr int kBytes = ROWS * SB;
+  static_assert(ROWS * kRowUnits % NT == 0 && NT % kRowUnits == 0, "whole units per thread");
+  const char* base;         // of the tile's first row (uniform)
+  uint32_t p[kUnits];       // byte offsets of the thread's units
+  u32x4 r[D][kUnits];
   int K;
 
-  // rows [first, last] of the operand are the tile's (last - first may be less than ROWS - 1)
-  __device__ __forceinline__ void init(const T* base, int64_t ld, int64_t first, int64_t last, int K_) {
+  static __device__ __forceinline__ int key(int row) {
+    return SB == 128 ? (row >> 1) & 7 : (4 - (row >> 2)) & 3;
+  }
+  static __device__ __forceinline__ int unit() { return (int)threadIdx.x % kRowUnits; }
+  // rows [first, last] of the operand are the tile's: first <= last (which may be nearer than ROWS - 1)
+  __device__ __forceinline__ void init(const T* from, int64_t ld, int64_t first, int64_t last, int K_) {
     K = K_;
+    base = reinterpret_cast<const char*>(from + first * ld);
+    const int most = last - first < ROWS ? (int)(last - first) : ROWS - 1;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
-      const int64_t row = first + ((int)threadIdx.x + i * NT) / 8;
-      p[i] = base + (row < last ? row : last) * ld + ((int)threadIdx.x % 8) * kVec<T>;
+      const int row = ((int)threadIdx.x + i * NT) / kRowUnits;
+      p[i] = ((uint32_t)(row < most ? row : most) * (uint32_t)ld + unit() * kVec<T>) * (uint32_t)sizeof(T);
     }
   }
+  __device__ __forceinline__ int whole() const { return K / kStage; }   // stages without an end inside
+  __device__ __forceinline__ int left(int kt) const { return K - kt * kStage - unit() * kVec<T>; }
+  __device__ __forceinline__ const T* at(int kt, uint32_t off) const {
+    return reinterpret_cast<const T*>(base + (int64_t)kt * SB + off);
+  }
+  template <int SLOT>
+  __device__ __forceinline__ void load_whole(int kt) {
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) r[SLOT][i] = load16(at(kt, p[i]));
+  }
+  template <int SLOT>
   __device__ __forceinline__ void load(int kt) {
-    const int k0 = kt * kStage<T>;
-    if (k0 + kStage<T> <= K) {
+    const int n = left(kt);
+    if (K >= kVec<T>) {
 #pragma unroll
-      for (int i = 0; i < kUnits; ++i) r[i] = load16(p[i] + k0);
-    } else {   // the row ends inside the stage: its last unit is read so that it ends with the row
-      const int n = K - k0 - ((int)threadIdx.x % 8) * kVec<T>;
+      for (int i = 0; i < kUnits; ++i) r[SLOT][i] = load16(at(kt, p[i]) + (n < kVec<T> ? n - kVec<T> : 0));
+    } else {
 #pragma unroll
-      for (int i = 0; i < kUnits; ++i) {
-        if (n >= kVec<T>) r[i] = load16(p[i] + k0);
-        else if (n <= 0) r[i] = u32x4{0, 0, 0, 0};
-        else if (K >= kVec<T>) r[i] = keep_last<T>(load16(p[i] + k0 + n - kVec<T>), n);
-        else r[i] = load_few(p[i] + k0, n);
-      }
+      for (int i = 0; i < kUnits; ++i) r[SLOT][i] = n > 0 ? load_few(at(kt, p[i]), n) : u32x4{0, 0, 0, 0};
     }
   }
-  __device__ __forceinline__ void store(char* lds) const {
+  template <int SLOT>
+  __device__ __forceinline__ void store(int kt, char* lds) {
+    if ((kt + 1) * kStage > K && K >= kVec<T>) {
+      const int n = clamp_units(left(kt), kVec<T>);
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) r[SLOT][i] = keep_last<T>(r[SLOT][i], n);
+    }
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
-      const int idx = (int)threadIdx.x + i * NT, row = idx / 8, u = idx % 8;
-      *reinterpret_cast<u32x4*>(lds + row * kStageBytes + ((u ^ ((row >> 1) & 7)) << 4)) = r[i];
+      const int row = ((int)threadIdx.x + i * NT) / kRowUnits;
+      *reinterpret_cast<u32x4*>(lds + row * SB + ((unit() ^ key(row)) << 4)) = r[SLOT][i];
     }
   }
   // fragment of rows [m0, m0 + 16), half s of the stage
   static __device__ __forceinline__ u32x4 frag(const char* lds, int m0, int s) {
     const int lane = (int)threadIdx.x % 64, row = m0 + lane % 16;
-    return *reinterpret_cast<const u32x4*>(lds + row * kStageBytes + (((s * 4 + lane / 16) ^ ((row >> 1) & 7)) << 4));
+    return *reinterpret_cast<const u32x4*>(lds + row * SB + (((s * 4 + lane / 16) ^ key(row)) << 4));
   }
 };
 
@@ -116,58 +139,72 @@ struct RowTile {
 // fragment read over the banks: bf16 fragments take the rows of k in fours
 // (ds_read_b64_tr_b16: lane i of 16 gives the address of 4 columns of row i / 4
 // and receives the 4 rows of column i), fp32 ones a word per row.
-template <typename T, int COLS, int NT>
+template <typename T, int COLS, int NT, int D, int SB>
 struct ColTile {
-  static constexpr int kRowUnits = COLS * (int)sizeof(T) / 16;
-  static constexpr int kUnits = kStage<T> * kRowUnits / NT;
+  static constexpr int kRowUnits = COLS * (int)sizeof(T) / 16, kStage = SB / (int)sizeof(T);
+  static constexpr int kUnits = kStage * kRowUnits / NT;
+  static constexpr int kEvery = NT / kRowUnits;   // rows of k between a thread's units
   static constexpr int kPitch = COLS * (int)sizeof(T) + (sizeof(T) == 2 ? 32 : 16);
-  static constexpr int kBytes = kStage<T> * kPitch + (sizeof(T) == 2 ? 8 * 128 : 0);
-  static_assert(kStage<T> * kRowUnits % NT == 0 && NT % kRowUnits == 0, "whole units per thread");
-  const T* p;       // the thread's column in row 0 of k
+  static constexpr int kBytes = kStage * kPitch + (sizeof(T) == 2 ? kStage / 8 * 128 : 0);
+  static_assert(kStage * kRowUnits % NT == 0 && NT % kRowUnits == 0, "whole units per thread");
+  const T* p;            // the thread's column in its first row of k
   int64_t ld;
-  int n;            // columns of the thread's unit that exist (kVec: all; 0: none)
-  bool narrow;      // fewer columns than a unit holds
-  int k_end;
+  int first, n;          // its first row; columns of its units that exist (kVec: all; 0: none)
+  bool edge, narrow;     // the operand's columns end inside the tile; there are fewer than a unit holds
+  int k0, k_end;         // rows of k [k0, k_end) are summed
   const uint8_t* live;   // rows of k to take (others are zero, whatever they hold), or NULL: all
-  u32x4 r[kUnits];
+  u32x4 r[D][kUnits];
 
   static __device__ __forceinline__ int at(int k) {
     return k * kPitch + (sizeof(T) == 2 ? (k >> 3) * 128 : 0);
   }
-  // columns [first, C) of the operand, rows of k [.., k_end_) (k_end_ >= 1)
-  __device__ __forceinline__ void init(const T* base, int64_t ld_, int first, int C, int k_end_,
+  // columns [from, C) of the operand
+  __device__ __forceinline__ void init(const T* base, int64_t ld_, int from, int C, int k0_, int k_end_,
                                        const uint8_t* live_ = nullptr) {
     ld = ld_;
+    k0 = k0_;
     k_end = k_end_;
     live = live_;
-    const int c = first + ((int)threadIdx.x % kRowUnits) * kVec<T>;
-    n = C - c;
-    n = n > kVec<T> ? kVec<T> : (n < 0 ? 0 : n);
+    first = (int)threadIdx.x / kRowUnits;
+    const int c = from + ((int)threadIdx.x % kRowUnits) * kVec<T>;
+    n = clamp_units(C - c, kVec<T>);
+    edge = from + COLS > C;
     narrow = C < kVec<T>;
     // a unit that the operand's columns end in (or before) is read so that it ends with them
-    p = base + (n == kVec<T> ? c : (narrow ? 0 : C - kVec<T>));
+    p = base + (k0 + first) * ld + (n == kVec<T> ? c : (narrow ? 0 : C - kVec<T>));
   }
-  // rows of k [k0, k0 + stage)
-  __device__ __forceinline__ void load(int64_t k0) {
-    const bool whole = k0 + kStage<T> <= k_end;
+  __device__ __forceinline__ int whole() const { return live || narrow ? 0 : (k_end - k0) / kStage; }
+  template <int SLOT>
+  __device__ __forceinline__ void load_whole(int kt) {
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) r[SLOT][i] = load16(p + (int64_t)(kt * kStage + i * kEvery) * ld);
+  }
+  template <int SLOT>
+  __device__ __forceinline__ void load(int kt) {
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
-      const int64_t k = k0 + ((int)threadIdx.x + i * NT) / kRowUnits;
-      if ((!whole && k >= k_end) || (live && !live[k])) {
-        r[i] = u32x4{0, 0, 0, 0};
-        continue;
-      }
-      const T* q = p + k * ld;
-      if (n == kVec<T>) r[i] = load16(q);
-      else if (!narrow) r[i] = keep_last<T>(load16(q), n);
-      else r[i] = n > 0 ? load_few(q, n) : u32x4{0, 0, 0, 0};
+      const int k = kt * kStage + i * kEvery, last = k_end - 1 - k0 - first;   // k to read, and the last there is
+      const T* q = p + (int64_t)(k < last ? k : last) * ld;
+      if (narrow) r[SLOT][i] = n > 0 ? load_few(q, n) : u32x4{0, 0, 0, 0};
+      else r[SLOT][i] = load16(q);
+      if (live && k <= last && !live[k0 + first + k]) r[SLOT][i] = u32x4{0, 0, 0, 0};
     }
   }
-  __device__ __forceinline__ void store(char* lds) const {
+  template <int SLOT>
+  __device__ __forceinline__ void store(int kt, char* lds) {
+    if (edge && !narrow) {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) r[SLOT][i] = keep_last<T>(r[SLOT][i], n);
+    }
+    if (k0 + (kt + 1) * kStage > k_end) {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i)
+        if (k0 + first + kt * kStage + i * kEvery >= k_end) r[SLOT][i] = u32x4{0, 0, 0, 0};
+    }
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       const int idx = (int)threadIdx.x + i * NT;
-      *reinterpret_cast<u32x4*>(lds + at(idx / kRowUnits) + (idx % kRowUnits) * 16) = r[i];
+      *reinterpret_cast<u32x4*>(lds + at(idx / kRowUnits) + (idx % kRowUnits) * 16) = r[SLOT][i];
     }
   }
   static __device__ __forceinline__ u32x4 frag(const char* lds, int m0, int s) {
@@ -181,8 +218,7 @@ struct ColTile {
     } else {
       u32x4 v;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        v[j] = *reinterpret_cast<const uint32_t*>(lds + at(s * 16 + g * 4 + j) + (m0 + i) * 4);
+      for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const uint32_t*>(lds + at(s * 16 + g * 4 + j) + (m0 + i) * 4);
       return v;
     }
   }
@@ -202,64 +238,123 @@ __device__ __forceinline__ f32x4 mma(u32x4 q, u32x4 p, f32x4 acc) {
   }
 }
 
-// Block shape: WM x WN waves, each MI x NJ fragments of 16 x 16.
-template <int WM_, int WN_, int MI_, int NJ_>
+// Sum of a fragment's values of k of one row.
+template <typename T>
+__device__ __forceinline__ float add_up(u32x4 a) {
+  float v = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = a[i];
+    if constexpr (sizeof(T) == 2)
+      v += __builtin_bit_cast(float, w << 16) + __builtin_bit_cast(float, w & 0xffff0000u);
+    else
+      v += __builtin_bit_cast(float, w);
+  }
+  return v;
+}
+
+// Block shape: WM x WN waves, each MI x NJ fragments of 16 x 16; D stages of SB bytes in flight.
+template <int WM_, int WN_, int MI_, int NJ_, int D_, int SB_>
 struct Shape {
-  static constexpr int WM = WM_, WN = WN_, MI = MI_, NJ = NJ_;
+  static constexpr int WM = WM_, WN = WN_, MI = MI_, NJ = NJ_, D = D_, SB = SB_;
+  static constexpr int kWaves = MI * NJ >= 32 ? 2 : (MI * NJ >= 16 ? 3 : 4);   // a SIMD, by the registers they take
   static constexpr int NT = WM * WN * 64, BM = WM * MI * 16, BN = WN * NJ * 16;
 };
 
-// The sum over stages [0, steps) of P and Q. Two LDS buffers: a stage is loaded
-// into registers while the one before it is multiplied, then written to the
-// other buffer. `first`: row of k of the column tiles' stage 0.
-// ONES: also sums P alone over k, into sum[i] (lanes of one m hold the same value).
-template <typename T, class S, class P, class Q, bool ONES>
-__device__ __forceinline__ void sum_stages(P& p, Q& q, char* lds, int steps, f32x4 (&acc)[S::MI][S::NJ],
-                                           f32x4 (&sum)[S::MI], bool ones, int64_t p0, int64_t p_step, int64_t q0,
-                                           int64_t q_step) {
-  constexpr int kBuf = P::kBytes + Q::kBytes;
-  const int wave = (int)threadIdx.x / 64, m0 = (wave / S::WN) * S::MI * 16, n0 = (wave % S::WN) * S::NJ * 16;
-  if (steps <= 0) return;
-  const uint32_t one = sizeof(T) == 2 ? 0x3f803f80u : 0x3f800000u;
-  const u32x4 all_one = {one, one, one, one};
-  p.load(p0);
-  q.load(q0);
-  p.store(lds);
-  q.store(lds + P::kBytes);
-  __syncthreads();
-  for (int kt = 0; kt < steps; ++kt) {
-    const char* at = lds + (kt & 1) * kBuf;
-    const bool more = kt + 1 < steps;
-    if (more) {
-      p.load(p0 + (kt + 1) * p_step);
-      q.load(q0 + (kt + 1) * q_step);
+// The sum over stages [0, steps) of P and Q, through two LDS buffers: before a
+// stage is multiplied the next one, whose loads were issued D stages ago, is
+// written to the other buffer, and the loads of the stage D behind it are issued.
+// ALONE: also sums P by itself where `alone` is set; sum[i] of the four lanes of
+// an m add up to it.
+template <typename T, class S, class P, class Q, bool ALONE>
+struct Sum {
+  static constexpr int kBuf = P::kBytes + Q::kBytes;
+  P p;
+  Q q;
+  char* lds;
+  int steps;
+  bool alone;
+  f32x4 acc[S::MI][S::NJ];
+  float sum[ALONE ? S::MI : 1];
+
+  template <int SLOT, bool WHOLE>
+  __device__ __forceinline__ void one(int kt) {
+    constexpr int kNext = (SLOT + 1) % S::D;   // slot of the next stage, and of the one D behind it
+    if (WHOLE || kt + 1 < steps) {
+      char* to = lds + ((kt + 1) & 1) * kBuf;
+      p.template store<kNext>(kt + 1, to);
+      q.template store<kNext>(kt + 1, to + P::kBytes);
     }
+    if constexpr (WHOLE) {
+      p.template load_whole<kNext>(kt + 1 + S::D);
+      q.template load_whole<kNext>(kt + 1 + S::D);
+    } else if (kt + 1 + S::D < steps) {
+      p.template load<kNext>(kt + 1 + S::D);
+      q.template load<kNext>(kt + 1 + S::D);
+    }
+    const int wave = (int)threadIdx.x / 64, m0 = (wave / S::WN) * S::MI * 16, n0 = (wave % S::WN) * S::NJ * 16;
+    const char* at = lds + (kt & 1) * kBuf;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < S::SB / kHalf; ++s) {
       u32x4 a[S::MI], b[S::NJ];
 #pragma unroll
-      for (int i = 0; i < S::MI; ++i) a[i] = P::frag(at, m0 + i * 16, s);
-#pragma unroll
       for (int j = 0; j < S::NJ; ++j) b[j] = Q::frag(at + P::kBytes, n0 + j * 16, s);
+#pragma unroll
+      for (int i = 0; i < S::MI; ++i) a[i] = P::frag(at, m0 + i * 16, s);
 #pragma unroll
       for (int i = 0; i < S::MI; ++i)
 #pragma unroll
         for (int j = 0; j < S::NJ; ++j) acc[i][j] = mma<T>(b[j], a[i], acc[i][j]);
-      if constexpr (ONES) {
-        if (ones) {
+      if constexpr (ALONE) {
+        if (alone) {
 #pragma unroll
-          for (int i = 0; i < S::MI; ++i) sum[i] = mma<T>(all_one, a[i], sum[i]);
+          for (int i = 0; i < S::MI; ++i) sum[i] += add_up<T>(a[i]);
         }
       }
     }
-    if (more) {
-      char* to = lds + ((kt + 1) & 1) * kBuf;
-      p.store(to);
-      q.store(to + P::kBytes);
-    }
     __syncthreads();
   }
-}
+  template <int SLOT>
+  __device__ __forceinline__ void first_loads() {
+    if constexpr (SLOT < S::D) {
+      if (SLOT < steps) {
+        p.template load<SLOT>(SLOT);
+        q.template load<SLOT>(SLOT);
+      }
+      first_loads<SLOT + 1>();
+    }
+  }
+  template <int SLOT, bool WHOLE>
+  __device__ __forceinline__ void round(int kt) {   // D stages from kt on (kt a multiple of D)
+    if constexpr (SLOT < S::D) {
+      if (!WHOLE && kt >= steps) return;
+      one<SLOT, WHOLE>(kt);
+      round<SLOT + 1, WHOLE>(kt + 1);
+    }
+  }
+  __device__ __forceinline__ void run() {
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i) {
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (ALONE) sum[i] = 0.f;
+    }
+    if (steps <= 0) return;
+    first_loads<0>();
+    p.template store<0>(0, lds);
+    q.template store<0>(0, lds + P::kBytes);
+    if (S::D < steps) {
+      p.template load<0>(S::D);
+      q.template load<0>(S::D);
+    }
+    __syncthreads();
+    // stages that are whole, as are those D ahead of them, take no branch
+    const int wp = p.whole(), wq = q.whole(), whole = (wp < wq ? wp : wq);
+    int kt = 0;
+    for (; kt + 2 * S::D + 1 <= whole; kt += S::D) round<0, true>(kt);
+    for (; kt < steps; kt += S::D) round<0, false>(kt);
+  }
+};
 
 // ---- groups ----------------------------------------------------------------
 

@@ -115,7 +115,7 @@ def _matrix(t, name, dtype, device, rows, cols):
         if ld < cols:
             _bad(f"the rows of {name} overlap")
         return ld
-    return max(ld, cols)
+    return cols
 
 
 def _flat(t, name, dtype, device, count):

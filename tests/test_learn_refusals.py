@@ -75,7 +75,8 @@ def test_layer_arguments():
                  (R(d), None, A, A, odd, A, None, 0, None, None), (R(d), odd, A, A, A, A, None, 0, None, None),
                  (R(linear_desc(n_groups=2)), None, A, A, A, A, None, 0, None, None),
                  (R(linear_desc(ld_x=15)), None, A, A, A, A, None, 0, None, None),
-                 (R(linear_desc(ld_y=23)), None, A, A, A, A, None, 0, None, None)]:
+                 (R(linear_desc(ld_y=23)), None, A, A, A, A, None, 0, None, None),
+                 (R(linear_desc(ld_x=(1 << 22) + 1)), None, A, A, A, A, None, 0, None, None)]:
         assert f(*args) == EINVAL
     b = L().im_linear_backward
     d = linear_desc(n_groups=3, n_rows=5000)
