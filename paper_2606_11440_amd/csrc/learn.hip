@@ -131,6 +131,7 @@ RowArgs row_args(const int32_t* offsets, int32_t G, int32_t n, const RowPlan& p,
   a.row_tiles = (int32_t)p.row_tiles;
   a.col_tiles = (int32_t)p.col_tiles;
   a.error = error;
+  a.cus = compute_units();
   return a;
 }
 

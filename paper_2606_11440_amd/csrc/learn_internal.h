@@ -30,7 +30,8 @@ struct RowArgs {
   int64_t ldc;
   int32_t relu;
   int32_t* error;
-  int32_t row_tiles, col_tiles;   // of the launch
+  int32_t row_tiles, col_tiles;   // at most, and exactly
+  int32_t cus;                    // compute units of the device
   // kStoreInput
   const void* X;              // relu_in: the layer's input
   int64_t ldx;

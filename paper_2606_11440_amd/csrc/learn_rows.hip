@@ -10,41 +10,10 @@ namespace im {
 namespace learn {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-__device__ __forceinline__ float exp_(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLeast = -300.f;   // 2^-300 is 0 in fp32
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// kVec neighbouring values of a row, of which `left` exist (kVec or more: all).
-template <typename T>
-struct Run {
-  static constexpr int N = kVec<T>;
-  float v[N];
-  __device__ __forceinline__ void load(const T* p, int left) {
-    if (left >= N) {
-      const u32x4 x = load16(p);
-      T e[N];
-      __builtin_memcpy(e, &x, 16);
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = (float)e[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = i < left ? (float)p[i] : 0.f;
-    }
-  }
-  __device__ __forceinline__ void store(T* p, int left) const {
-    T e[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) e[i] = (T)v[i];
-    if (left >= N) {
-      u32x4 x;
-      __builtin_memcpy(&x, e, 16);
-      *reinterpret_cast<u32x4_any*>(p) = x;
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (i < left) p[i] = e[i];
-    }
-  }
-};
 __device__ __forceinline__ f32x4 load4(const float* p, int left) {
   typedef f32x4 any __attribute__((aligned(4)));
   if (left >= 4) return *reinterpret_cast<const any*>(p);
@@ -64,51 +33,99 @@ __device__ __forceinline__ void store4(float* p, f32x4 v, int left) {
   }
 }
 
-// Passes a block's results through LDS to runs of a row: f(row of the tile,
-// column of the tile, run). A fragment's own layout would store 32 bytes of 16
-// rows at a time; here a wave stores whole lines. 16 WM rows at a time, through
-// two buffers in turn, so that one barrier does for each. A thread keeps its column.
-template <typename T, class S, class F>
-__device__ __forceinline__ void by_rows(const f32x4 (&acc)[S::MI][S::NJ], char* lds, F f) {
-  constexpr int kPitch = S::BN * 4 + 16, kRows = S::WM * 16, kAcross = S::BN / kVec<T>;
-  static_assert(S::NT % kAcross == 0 && kRows * kAcross % S::NT == 0, "a thread keeps its column");
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, wm = wave / S::WN, wn = wave % S::WN;
-  const int c = ((int)threadIdx.x % kAcross) * kVec<T>;
+// Passes a block's results, rounded to U, through LDS to 16-byte units of a row.
+// A fragment's own layout would store 32 bytes of 16 rows at a time; here a wave
+// stores whole lines. Unit u of a row lies at u ^ (row % 16), so that neither the
+// fragments' writes nor the units' reads meet in a bank. Where the LDS does not
+// hold the tile it goes in passes.
+//   value(i, j)   the fragment to put, final
+//   after()       called when the first pass is in LDS (one pass: acc is free)
+//   use(k, m, c, unit)   unit k of the thread's: of tile row m, from column c on
+template <typename U, class S, int kLds>
+struct Out {
+  static constexpr int kPitch = S::BN * (int)sizeof(U), kAcross = kPitch / 16;
+  static constexpr int kPasses = S::BM * kPitch <= kLds ? 1 : 2, kMi = S::MI / kPasses;
+  static constexpr int kUnits = S::WM * kMi * 16 * kAcross / S::NT;   // of a thread, a pass
+  static_assert(S::WM * kMi * 16 * kPitch <= kLds && S::MI % kPasses == 0, "a pass fits");
+  static_assert(S::WM * kMi * 16 * kAcross % S::NT == 0 && S::NT % kAcross == 0, "whole units per thread");
+  static __device__ __forceinline__ int key(int row) { return row & (kAcross < 16 ? kAcross - 1 : 15); }
+
+  static __device__ __forceinline__ int row_of(int pass, int k, int tid) {
+    const int r = tid / kAcross + k * (S::NT / kAcross);
+    return kPasses == 1 ? r : (r / (kMi * 16)) * S::MI * 16 + pass * kMi * 16 + r % (kMi * 16);
+  }
+  static __device__ __forceinline__ int column_of(int tid) { return tid % kAcross * (16 / (int)sizeof(U)); }
+
+  template <class V, class A, class F>
+  static __device__ __forceinline__ void run(char* lds, int tid, V value, A after, F use) {
+    const int lane = tid % 64, wave = tid / 64, wm = wave / S::WN, wn = wave % S::WN, g = lane / 16;
 #pragma unroll
-  for (int i = 0; i < S::MI; ++i) {
-    char* buf = lds + (i & 1) * kRows * kPitch;
+    for (int pass = 0; pass < kPasses; ++pass) {
+      if (pass) __syncthreads();
 #pragma unroll
-    for (int j = 0; j < S::NJ; ++j)
-      *reinterpret_cast<f32x4*>(buf + (wm * 16 + lane % 16) * kPitch + ((wn * S::NJ + j) * 16 + (lane / 16) * 4) * 4) =
-          acc[i][j];
-    __syncthreads();
+      for (int i = 0; i < kMi; ++i) {
+        const int r = (wm * kMi + i) * 16 + lane % 16;
 #pragma unroll
-    for (int k = 0; k < kRows * kAcross / S::NT; ++k) {
-      const int r = (int)threadIdx.x / kAcross + k * (S::NT / kAcross);
-      Run<T> run;
+        for (int j = 0; j < S::NJ; ++j) {
+          const f32x4 v = value(pass * kMi + i, j);
+          const int at = (wn * S::NJ + j) * 16 + g * 4;
+          char* to = lds + r * kPitch + (((at * (int)sizeof(U) / 16) ^ key(r)) << 4);
+          if constexpr (sizeof(U) == 2) {
+            bf16x4 o;
 #pragma unroll
-      for (int e = 0; e < kVec<T>; e += 4) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(buf + r * kPitch + (c + e) * 4);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) run.v[e + q] = v[q];
+            for (int q = 0; q < 4; ++q) o[q] = (__bf16)v[q];
+            *reinterpret_cast<bf16x4*>(to + (g & 1) * 8) = o;
+          } else {
+            *reinterpret_cast<f32x4*>(to) = v;
+          }
+        }
       }
-      f((r / 16) * S::MI * 16 + i * 16 + r % 16, c, run);
+      __syncthreads();
+      if (pass == 0) after();
+#pragma unroll
+      for (int k = 0; k < kUnits; ++k) {
+        const int r = tid / kAcross + k * (S::NT / kAcross);
+        use(pass * kUnits + k, row_of(pass, k, tid), column_of(tid),
+            *reinterpret_cast<const u32x4*>(lds + r * kPitch + ((tid % kAcross ^ key(r)) << 4)));
+      }
     }
   }
+};
+
+// Some of a unit's values to p (n: how many exist).
+template <typename U>
+__device__ __forceinline__ void store_few(U* p, u32x4 x, int n) {
+  U e[kVec<U>];
+  __builtin_memcpy(e, &x, 16);
+#pragma unroll
+  for (int i = 0; i < kVec<U>; ++i)
+    if (i < n) p[i] = e[i];
+}
+// A unit of results where x is above zero, else zeros.
+template <typename T>
+__device__ __forceinline__ u32x4 where_positive(u32x4 v, u32x4 x) {
+  T e[kVec<T>], q[kVec<T>];
+  __builtin_memcpy(e, &v, 16);
+  __builtin_memcpy(q, &x, 16);
+#pragma unroll
+  for (int i = 0; i < kVec<T>; ++i) e[i] = (float)q[i] > 0.f ? e[i] : T(0.f);
+  __builtin_memcpy(&v, e, 16);
+  return v;
 }
 
-// Softmax statistics of some classes of a row: the largest logit, and with it
-// subtracted sum exp and sum exp z. Nothing seen: {-inf, 0, 0}.
+// Softmax statistics of some classes of a row, in powers of two (t = z log2 e):
+// the largest t, and with it subtracted sum 2^t and sum 2^t t. Nothing seen:
+// {-inf, 0, 0}.
 struct Stats {
-  float top, sum, zsum;
+  float top, sum, tsum;
 };
 __device__ __forceinline__ Stats join(const Stats& a, const Stats& b) {
   Stats o;
   o.top = fmaxf(a.top, b.top);
   const float da = a.top == -INFINITY ? 0.f : a.top - o.top, db = b.top == -INFINITY ? 0.f : b.top - o.top;
-  const float ea = exp_(da), eb = exp_(db);   // a side that saw nothing has sums of zero (NaN sums stay)
+  const float ea = exp2_(da), eb = exp2_(db);   // a side that saw nothing has sums of zero (NaN sums stay)
   o.sum = a.sum * ea + b.sum * eb;
-  o.zsum = (a.zsum + da * a.sum) * ea + (b.zsum + db * b.sum) * eb;
+  o.tsum = (a.tsum + da * a.sum) * ea + (b.tsum + db * b.sum) * eb;
   return o;
 }
 
@@ -116,259 +133,387 @@ __device__ __forceinline__ Stats join(const Stats& a, const Stats& b) {
 __device__ __forceinline__ bool class_valid(const RowArgs& a, int64_t row, int j) {
   return !a.valid || ((a.valid[row * a.words + (j >> 5)] >> (j & 31)) & 1u);
 }
-__device__ __forceinline__ int target_of(const RowArgs& a, int64_t row, bool& wrong) {
-  const int y = a.target[row];
-  wrong = y < -1 || y >= a.V || (y >= 0 && !class_valid(a, row, y));
-  return wrong ? -1 : y;
+__device__ __forceinline__ bool target_wrong(const RowArgs& a, int64_t row, int y) {
+  return y < -1 || y >= a.V || (y >= 0 && !class_valid(a, row, y));
 }
-// What a head's epilogue reads of a row.
+// ty: t of the target
+__device__ __forceinline__ void put_row(const RowArgs& a, int64_t row, const Stats& s, int y, float ty) {
+  const bool some = !(s.sum == 0.f);
+  const float lg = some ? __builtin_amdgcn_logf(s.sum) : 0.f;   // log2
+  a.logp[row] = some && y >= 0 ? (ty - s.top - lg) * kLn2 : 0.f;
+  if (a.entropy) a.entropy[row] = some ? (lg - s.tsum / s.sum) * kLn2 : 0.f;
+  if (a.lse) a.lse[row] = some ? (s.top + lg) * kLn2 : -INFINITY;
+}
+
+// What a head's epilogue reads of a row. For the gradient, with t = log2 pi:
+//   dz = 2^t (A + B t), and `up` more at the target;
+//   A = -up - ent H, B = -ent ln 2, t = z log2 e - lse log2 e
+// A row that adds nothing has A = B = up = 0 and lse = +inf, so that t is the
+// least there is and every dz is 0, whatever its logits are.
 struct Row {
   int y;
-  float lse, up, ent, H;
+  float lse2, A, B, up;
+  bool live;
   __device__ __forceinline__ void load(const RowArgs& a, int64_t row, int hi, bool gradient) {
     y = -1;
+    A = B = up = 0.f;
+    lse2 = INFINITY;
+    live = false;
     if (row >= hi) return;
     y = a.target[row];
     if (!gradient) return;
-    lse = a.lse[row];
+    lse2 = a.lse[row];
     up = a.dlogp[row];
-    ent = a.dentropy ? a.dentropy[row] : 0.f;
-    H = a.dentropy ? a.entropy[row] : 0.f;
+    A = a.dentropy ? a.entropy[row] : 0.f;
+    B = a.dentropy ? a.dentropy[row] : 0.f;
   }
   // the target is a valid class of the row, or none; true where it was neither
-  __device__ __forceinline__ bool check(const RowArgs& a, int64_t row, int hi) {
+  __device__ __forceinline__ bool check(const RowArgs& a, int64_t row, int hi, bool gradient) {
     if (row >= hi) return false;
-    const bool wrong = y < -1 || y >= a.V || (y >= 0 && !class_valid(a, row, y));
+    const bool wrong = target_wrong(a, row, y);
     if (wrong) y = -1;
+    if (!gradient) return wrong;
     if (y < 0) up = 0.f;
+    const float H = A, ent = B, lse = lse2;
+    live = (up != 0.f || ent != 0.f) && lse != -INFINITY;
+    up = live ? up : 0.f;
+    A = live ? -up - ent * H + (lse - lse) : 0.f;   // an lse that is not finite makes the row NaN
+    B = live ? -ent * kLn2 : 0.f;
+    lse2 = live ? lse * kLog2e : INFINITY;
     return wrong;
   }
 };
-__device__ __forceinline__ void put_row(const RowArgs& a, int64_t row, const Stats& s, int y, float zy) {
-  const bool some = !(s.sum == 0.f);
-  const float ln = some ? __logf(s.sum) : 0.f;
-  a.logp[row] = some && y >= 0 ? zy - s.top - ln : 0.f;
-  if (a.entropy) a.entropy[row] = some ? ln - s.zsum / s.sum : 0.f;
-  if (a.lse) a.lse[row] = some ? s.top + ln : -INFINITY;
-}
 
 template <typename T, class S, bool COLUMNS, int EPI>
 __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a) {
   using P = RowTile<T, S::BM, S::NT, S::D, S::SB>;
-  using Q = typename std::conditional<COLUMNS, ColTile<T, S::BN, S::NT, S::D, S::SB>, RowTile<T, S::BN, S::NT, S::D, S::SB>>::type;
+  using Q = typename std::conditional<COLUMNS, ColTile<T, S::BN, S::NT, S::D, S::SB>,
+                                      RowTile<T, S::BN, S::NT, S::D, S::SB>>::type;
   using Product = Sum<T, S, P, Q, false>;
+  constexpr bool kHead = EPI == kStats || EPI == kGradLogits;
   __shared__ __attribute__((aligned(16))) char lds[2 * Product::kBuf];
-  __shared__ Row rows[EPI == kStats || EPI == kGradLogits ? S::BM : 1];
+  __shared__ Row rows[kHead ? S::BM : 1];
+  __shared__ Groups groups;
+  __shared__ float column_sums[EPI == kGradLogits ? S::WM * S::BN : 1];
+  static_assert(S::NT >= S::BM, "a thread a row");
+  static_assert(EPI != kGradLogits || S::NT >= S::BN, "a thread a column");
 
-  int rt, ct;
-  tile_of(blockIdx.x, a.row_tiles, a.col_tiles, rt, ct);
-  Part part;
-  bool bad;
-  const bool found = find_part(a.offsets, a.G, a.n, S::BM, rt, part, bad);
-  if (bad && blockIdx.x == 0 && threadIdx.x == 0 && a.error) atomicOr(a.error, IM_ERR_COUNT);
-  if (!found) return;
+  groups.init(a.offsets, a.G, a.n, S::BM);
+  __syncthreads();
+  if (groups.total < 0) {
+    if (blockIdx.x == 0 && threadIdx.x == 0 && a.error) atomicOr(a.error, IM_ERR_COUNT);
+    return;
+  }
+  const int row_tiles = groups.total, total = row_tiles * a.col_tiles;
+  int tile = blockIdx.x;
+  if (tile >= total) return;
 
-  const T* A = static_cast<const T*>(a.A);
-  const T* B = static_cast<const T*>(a.B) + part.g * a.b_group;
-  const int n_first = ct * S::BN;   // < N: the launch has no column tiles past the operand
   Product x;
   x.lds = lds;
   x.steps = (a.K + P::kStage - 1) / P::kStage;
-  x.p.init(A, a.lda, part.lo, part.hi - 1, a.K);
-  if constexpr (COLUMNS) x.q.init(B, a.ldb, n_first, a.N, 0, a.K);
-  else x.q.init(B, a.ldb, n_first, a.N - 1, a.K);
-  // a head's row: loaded before the sums, needed after them
-  Row mine{};
-  if constexpr (EPI == kStats || EPI == kGradLogits) mine.load(a, part.lo + (int)threadIdx.x, part.hi, EPI == kGradLogits);
-  x.run();
-  auto& acc = x.acc;
-  if constexpr (EPI == kStats || EPI == kGradLogits) {
-    const bool wrong = mine.check(a, part.lo + (int)threadIdx.x, part.hi);
-    if (wrong && a.col0 == 0 && ct == 0 && a.error) atomicOr(a.error, IM_ERR_ACTION);
-    static_assert(S::NT >= S::BM, "a thread a row");
-    if ((int)threadIdx.x < S::BM) rows[threadIdx.x] = mine;
-    __syncthreads();
-  }
+  Row mine;
+  int rt, ct, g, lo, hi;
+  auto enter = [&](int t) {   // takes tile t: its first loads are on their way
+    const int tid = fresh_thread();
+    tile_of(t, row_tiles, a.col_tiles, rt, ct);
+    groups.find(a.G, S::BM, rt, g, lo, hi);
+    const T* B = static_cast<const T*>(a.B) + g * a.b_group;
+    x.p.init(static_cast<const T*>(a.A), a.lda, lo, hi - 1, a.K, tid);
+    // ct * BN < N: the launch has no column tiles past the operand
+    if constexpr (COLUMNS) x.q.init(B, a.ldb, ct * S::BN, a.N, 0, a.K, tid);
+    else x.q.init(B, a.ldb, ct * S::BN, a.N - 1, a.K, tid);
+    x.begin();
+    if constexpr (kHead) mine.load(a, (int64_t)lo + tid, hi, EPI == kGradLogits);
+  };
+  enter(tile);
+  x.first_stage();
+  while (true) {
+    x.run();
+    auto& acc = x.acc;
+    const int tid = fresh_thread(), lane = tid % 64, wave = tid / 64, g4 = (lane / 16) * 4;
+    const int wm = wave / S::WN, wn = wave % S::WN, m_at = wm * S::MI * 16 + lane % 16;
+    // the tile at hand; the next one's loads run through its epilogue
+    const int at_lo = lo, at_hi = hi, at_rt = rt, at_ct = ct, at_g = g, n_first = ct * S::BN;
+    if constexpr (kHead) {
+      const bool wrong = mine.check(a, (int64_t)lo + tid, hi, EPI == kGradLogits);
+      if (wrong && a.col0 == 0 && ct == 0 && a.error) atomicOr(a.error, IM_ERR_ACTION);
+      if (tid < S::BM) rows[tid] = mine;
+      __syncthreads();
+    }
+    tile += gridDim.x;
+    const bool more = tile < total;
+    auto next = [&] {
+      if (more) enter(tile);
+    };
+    auto last = [&](bool on) {   // the next tile's first stage takes the LDS that the epilogue has read
+      if (!on) return;
+      __syncthreads();
+      x.first_stage();
+    };
+    const int n_at = n_first + wn * S::NJ * 16 + g4;
+    const float* bias = a.bias ? a.bias + at_g * a.bias_group + a.col0 : nullptr;
+    // A tile without an edge takes no branch on its way out: the next tile's loads,
+    // issued before its stores, are then waited for without them.
+    const bool full = at_hi - at_lo == S::BM && n_first + S::BN <= a.N;
+    using O = Out<T, S, (int)sizeof(lds)>;
+    char* const C = reinterpret_cast<char*>(static_cast<T*>(a.C) + (int64_t)at_lo * a.ldc + n_first);
+    auto place = [&](int m, int c) { return ((uint32_t)m * (uint32_t)a.ldc + (uint32_t)c) * (uint32_t)sizeof(T); };
+    auto put = [&](int, int m, int c, u32x4 v) { *reinterpret_cast<u32x4_any*>(C + place(m, c)) = v; };
+    auto put_some = [&](int, int m, int c, u32x4 v) {
+      const int left = a.N - n_first - c;
+      if (at_lo + m >= at_hi || left <= 0) return;
+      T* const to = reinterpret_cast<T*>(C + place(m, c));
+      if (left >= kVec<T>) *reinterpret_cast<u32x4_any*>(to) = v;
+      else store_few(to, v, left);
+    };
 
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, g4 = (lane / 16) * 4;
-  const int wm = wave / S::WN, wn = wave % S::WN;
-  const int m_at = wm * S::MI * 16 + lane % 16, n_at = n_first + wn * S::NJ * 16 + g4;
-  const float* bias = a.bias ? a.bias + part.g * a.bias_group + a.col0 : nullptr;
-
-  static_assert(2 * S::WM * 16 * (S::BN * 4 + 16) <= (int)sizeof(lds), "the results pass through the stages' LDS");
-  if constexpr (EPI == kStore) {
-    Run<T> plus;
-    const int c = n_first + ((int)threadIdx.x % (S::BN / kVec<T>)) * kVec<T>;
-#pragma unroll
-    for (int e = 0; e < kVec<T>; ++e) plus.v[e] = bias && c + e < a.N ? bias[c + e] : 0.f;
-    by_rows<T, S>(acc, lds, [&](int m, int n, Run<T>& run) {
-      const int64_t row = part.lo + m;
-      if (row >= part.hi || n_first + n >= a.N) return;
-#pragma unroll
-      for (int e = 0; e < kVec<T>; ++e) {
-        run.v[e] += plus.v[e];
-        if (a.relu) run.v[e] = run.v[e] < 0.f ? 0.f : run.v[e];   // NaN stays
-      }
-      run.store(static_cast<T*>(a.C) + row * a.ldc + n_first + n, a.N - n_first - n);
-    });
-  }
-  if constexpr (EPI == kStoreInput) {
-    by_rows<T, S>(acc, lds, [&](int m, int n0, Run<T>& run) {
-      const int64_t row = part.lo + m;
-      const int n = n_first + n0, left = a.N - n;
-      if (row >= part.hi || left <= 0) return;
-      if (a.sum) {
-        float* sum = a.sum + row * a.N + n;
-#pragma unroll
-        for (int e = 0; e < kVec<T>; e += 4) {
-          f32x4 v = {run.v[e], run.v[e + 1], run.v[e + 2], run.v[e + 3]};
-          if (!a.first && left > e) v += load4(sum + e, left - e);
-          if (!a.last && left > e) store4(sum + e, v, left - e);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) run.v[e + q] = v[q];
-        }
-        if (!a.last) return;
-      }
-      if (a.X) {
-        Run<T> x;
-        x.load(static_cast<const T*>(a.X) + row * a.ldx + n, left);
-#pragma unroll
-        for (int e = 0; e < kVec<T>; ++e) run.v[e] = x.v[e] > 0.f ? run.v[e] : 0.f;
-      }
-      run.store(static_cast<T*>(a.C) + row * a.ldc + n, left);
-    });
-  }
-
-  if constexpr (EPI == kStats) {
-    // each row's classes lie in four lanes of WN waves
-    float* taken = reinterpret_cast<float*>(lds);                    // [BM]
-    Stats* across = reinterpret_cast<Stats*>(lds + S::BM * 4);       // [WN][BM]
-    static_assert(S::BM * 4 + S::WN * S::BM * sizeof(Stats) <= sizeof(lds), "fits");
-    const bool whole = a.col_tiles == 1;
-#pragma unroll
-    for (int i = 0; i < S::MI; ++i) {
-      const int m = m_at + i * 16;
-      const int64_t row = part.lo + m;
-      const bool in = row < part.hi;
-      const int y = rows[m].y;
-      Stats s{-INFINITY, 0.f, 0.f};
-      uint32_t ok = 0;
+    if constexpr (EPI == kStore) {
+      f32x4 plus[S::NJ];
 #pragma unroll
       for (int j = 0; j < S::NJ; ++j) {
-        const int n = n_at + j * 16, left = a.N - n;
-        if (left <= 0 || !in) continue;
-        if (bias) acc[i][j] += load4(bias + n, left);
-        uint32_t bits = left >= 4 ? 15u : (1u << left) - 1u;
-        // four classes from a multiple of 4: one word
-        if (a.valid) bits &= a.valid[row * a.words + (n >> 5)] >> (n & 31);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float z = acc[i][j][r];
-          if (n + r == y) (whole ? taken[m] : a.taken[row]) = z;
-          if (!((bits >> r) & 1u) || z == -INFINITY) continue;
-          ok |= 1u << (j * 4 + r);
-          s.top = fmaxf(s.top, z);
-        }
+        plus[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (bias && n_at + j * 16 < a.N) plus[j] = load4(bias + n_at + j * 16, a.N - n_at - j * 16);
       }
-      const float ref = s.top == -INFINITY ? 0.f : s.top;
+      const float least = a.relu ? 0.f : -INFINITY;
+      auto value = [&](int i, int j) {
+        f32x4 v = acc[i][j] + plus[j];
 #pragma unroll
-      for (int j = 0; j < S::NJ; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float d = acc[i][j][r] - ref, e = exp_(d);
-          const bool take = (ok >> (j * 4 + r)) & 1u;
-          s.sum += take ? e : 0.f;
-          s.zsum += take ? e * d : 0.f;
-        }
-#pragma unroll
-      for (int d = 16; d < 64; d *= 2) {
-        const Stats o{__shfl_xor(s.top, d), __shfl_xor(s.sum, d), __shfl_xor(s.zsum, d)};
-        s = join(s, o);
-      }
-      if (g4 == 0) across[wn * S::BM + m] = s;
-    }
-    __syncthreads();
-    for (int m = threadIdx.x; m < S::BM; m += S::NT) {
-      const int64_t row = part.lo + m;
-      if (row >= part.hi) continue;
-      Stats s = across[m];
-#pragma unroll
-      for (int w = 1; w < S::WN; ++w) s = join(s, across[w * S::BM + m]);
-      if (whole) {
-        put_row(a, row, s, rows[m].y, taken[m]);
+        for (int r = 0; r < 4; ++r) v[r] = v[r] < least ? least : v[r];   // NaN stays
+        return v;
+      };
+      if (full) {
+        O::run(lds, tid, value, next, put);
+        last(more);
       } else {
-        float* to = a.stats + ((int64_t)ct * a.n + row) * 3;
-        to[0] = s.top, to[1] = s.sum, to[2] = s.zsum;
+        O::run(lds, tid, value, next, put_some);
+        last(more);
       }
     }
-  }
 
-  if constexpr (EPI == kGradLogits) {
-    float colsum[S::NJ][4];
+    if constexpr (EPI == kStoreInput) {
+      auto value = [&](int i, int j) { return acc[i][j]; };
+      if (a.sum) {   // a piece of a head's classes
+        using F = Out<float, S, (int)sizeof(lds)>;
+        F::run(lds, tid, value, [] {}, [&](int, int m, int c, u32x4 x) {
+          const int64_t row = (int64_t)at_lo + m;
+          const int n = n_first + c, left = a.N - n;
+          if (row >= at_hi || left <= 0) return;
+          f32x4 v = __builtin_bit_cast(f32x4, x);
+          float* sum = a.sum + row * a.N + n;
+          if (!a.first) v += load4(sum, left);
+          if (!a.last) {
+            store4(sum, v, left);
+            return;
+          }
+          for (int q = 0; q < 4 && q < left; ++q) {
+            const float y = v[q];
+            const bool keep = !a.X || (float)static_cast<const T*>(a.X)[row * a.ldx + n + q] > 0.f;
+            static_cast<T*>(a.C)[row * a.ldc + n + q] = (T)(keep ? y : 0.f);
+          }
+        });
+        next();
+        last(more);
+      } else if (!a.X) {
+        if (full) {
+          O::run(lds, tid, value, next, put);
+          last(more);
+        } else {
+          O::run(lds, tid, value, next, put_some);
+          last(more);
+        }
+      } else {
+        // the layer's input, loaded before the results that it lets through are read
+        const char* const X = reinterpret_cast<const char*>(static_cast<const T*>(a.X) + (int64_t)at_lo * a.ldx + n_first);
+        auto x_at = [&](int k) {
+          const int m = O::row_of(k / O::kUnits, k % O::kUnits, tid), c = O::column_of(tid);
+          return ((uint32_t)m * (uint32_t)a.ldx + (uint32_t)c) * (uint32_t)sizeof(T);
+        };
+        constexpr int kAll = O::kUnits * O::kPasses, kAhead = kAll < 8 ? kAll : 8;
+        u32x4 xs[kAhead];
+        if (full) {
+          O::run(lds, tid, value,
+                 [&] {
+                   if (O::kPasses == 1) next();
 #pragma unroll
-    for (int j = 0; j < S::NJ; ++j)
+                   for (int k = 0; k < kAhead; ++k) xs[k] = *reinterpret_cast<const u32x4_any*>(X + x_at(k));
+                 },
+                 [&](int k, int m, int c, u32x4 v) {
+                   put(k, m, c, where_positive<T>(v, xs[k % kAhead]));
+                   if (k + kAhead < kAll) xs[k % kAhead] = *reinterpret_cast<const u32x4_any*>(X + x_at(k + kAhead));
+                 });
+          if (O::kPasses > 1) next();
+          last(more);
+        } else {
+          O::run(lds, tid, value, next, [&](int k, int m, int c, u32x4 v) {
+            const int left = a.N - n_first - c;
+            if (at_lo + m >= at_hi || left <= 0) return;
+            const T* const from = reinterpret_cast<const T*>(X + x_at(k));
+            put_some(k, m, c, where_positive<T>(v, left >= kVec<T> ? load16(from) : load_few(from, left)));
+          });
+          last(more);
+        }
+      }
+    }
+
+    if constexpr (kHead) {
+      // A wave's columns begin at a multiple of 32 classes (as pieces do): their mask words
+      constexpr int kWords = (S::NJ * 16 + 31) / 32;
+      uint32_t words[S::MI][kWords];
+      if (a.valid) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) colsum[j][r] = 0.f;
+        for (int i = 0; i < S::MI; ++i) {
+          const int64_t row = at_lo + m_at + i * 16 < at_hi ? at_lo + m_at + i * 16 : at_hi - 1;
 #pragma unroll
-    for (int i = 0; i < S::MI; ++i) {
-      const int64_t row = part.lo + m_at + i * 16;
-      if (row >= part.hi) continue;
-      const Row& of = rows[m_at + i * 16];
-      const int y = of.y;
-      const float lse = of.lse, up = of.up, ent = of.ent, H = of.H;
-      const bool live = (up != 0.f || ent != 0.f) && lse != -INFINITY;
-      // a row that adds nothing is kept from the sums over rows where its h is not finite (its
-      // logits then are not either); elsewhere its zeros do
-      if (a.live && a.col0 == 0 && ct == 0 && wn == 0 && g4 == 0)
-        a.live[row] = live || fabsf(acc[i][0][0]) < INFINITY;
+          for (int w = 0; w < kWords; ++w) {
+            const int at = (a.col0 + n_first + wn * S::NJ * 16) / 32 + w;
+            words[i][w] = a.valid[row * a.words + (at < a.words ? at : a.words - 1)];
+          }
+        }
+      }
+      auto bits_of = [&](int i, int j) { return words[i][j / 2] >> ((j & 1) * 16 + g4); };
+      f32x4 plus[S::NJ];   // the classes' biases times log2 e
 #pragma unroll
       for (int j = 0; j < S::NJ; ++j) {
-        const int n = n_at + j * 16, left = a.N - n;
-        if (left <= 0) continue;
-        f32x4 z = acc[i][j], dz;   // dz takes the logits' place
-        if (bias) z += load4(bias + n, left);
-        const int c = a.col0 + n;   // pieces begin at multiples of 32 classes
-        uint32_t bits = live ? (left >= 4 ? 15u : (1u << left) - 1u) : 0u;
-        if (a.valid) bits &= a.valid[row * a.words + (c >> 5)] >> (c & 31);
+        plus[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (bias && n_at + j * 16 < a.N) plus[j] = load4(bias + n_at + j * 16, a.N - n_at - j * 16);
+        plus[j] *= kLog2e;
+      }
+
+      if constexpr (EPI == kStats) {
+        // each row's classes lie in four lanes of WN waves
+        float* taken = reinterpret_cast<float*>(lds);                    // [BM]
+        Stats* across = reinterpret_cast<Stats*>(lds + S::BM * 4);       // [WN][BM]
+        static_assert(S::BM * 4 + S::WN * S::BM * sizeof(Stats) <= sizeof(lds), "fits");
+        const bool whole = a.col_tiles == 1, edge = n_first + S::BN > a.N;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float lp = z[r] - lse, pr = exp_(lp);
-          const bool ok = ((bits >> r) & 1u) && z[r] != -INFINITY;
-          float d = up * ((c + r == y ? 1.f : 0.f) - pr);
-          if (a.dentropy && pr != 0.f) d -= ent * pr * (lp + H);
-          dz[r] = ok ? d : 0.f;
-          colsum[j][r] += dz[r];
+        for (int i = 0; i < S::MI; ++i) {
+          const int m = m_at + i * 16, y = rows[m].y;
+          Stats s{-INFINITY, 0.f, 0.f};
+#pragma unroll
+          for (int j = 0; j < S::NJ; ++j) {
+            f32x4 t;
+            const int n = n_at + j * 16;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) t[r] = fmaf(acc[i][j][r], kLog2e, plus[j][r]);
+            if ((unsigned)(y - n) < 4u) {
+              const float ty = y - n == 0 ? t[0] : (y - n == 1 ? t[1] : (y - n == 2 ? t[2] : t[3]));
+              (whole ? taken[m] : a.taken[(int64_t)at_lo + m]) = ty;
+            }
+            if (a.valid) {
+              const uint32_t bits = bits_of(i, j);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) t[r] = (bits >> r) & 1u ? t[r] : -INFINITY;
+            }
+            if (edge) {
+#pragma unroll
+              for (int r = 0; r < 4; ++r) t[r] = n + r < a.N ? t[r] : -INFINITY;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s.top = fmaxf(s.top, t[r]);
+            acc[i][j] = t;
+          }
+          const float ref = s.top == -INFINITY ? 0.f : s.top;
+#pragma unroll
+          for (int j = 0; j < S::NJ; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float d = acc[i][j][r] - ref, e = exp2_(d);
+              s.sum += e;                                // NaN goes this way
+              s.tsum = fmaf(e, fmaxf(d, kLeast), s.tsum);   // no 0 times infinity
+            }
+#pragma unroll
+          for (int d = 16; d < 64; d *= 2) {
+            const Stats o{__shfl_xor(s.top, d), __shfl_xor(s.sum, d), __shfl_xor(s.tsum, d)};
+            s = join(s, o);
+          }
+          if (g4 == 0) across[wn * S::BM + m] = s;
         }
-        acc[i][j] = dz;
+        next();
+        __syncthreads();
+        for (int m = tid; m < S::BM; m += S::NT) {
+          const int64_t row = (int64_t)at_lo + m;
+          if (row >= at_hi) continue;
+          Stats s = across[m];
+#pragma unroll
+          for (int w = 1; w < S::WN; ++w) s = join(s, across[w * S::BM + m]);
+          if (whole) {
+            put_row(a, row, s, rows[m].y, taken[m]);
+          } else {
+            float* to = a.stats + ((int64_t)at_ct * a.n + row) * 3;
+            to[0] = s.top, to[1] = s.sum, to[2] = s.tsum;
+          }
+        }
+        last(more);
+      }
+
+      if constexpr (EPI == kGradLogits) {
+        f32x4 colsum[S::NJ];
+#pragma unroll
+        for (int j = 0; j < S::NJ; ++j) colsum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i) {
+          const int m = m_at + i * 16;
+          const Row of = rows[m];
+          // a row that adds nothing is kept from the sums over rows where its h is not finite
+          // (its logits then are not either); elsewhere its zeros do
+          if (a.live && a.col0 == 0 && at_ct == 0 && wn == 0 && g4 == 0 && at_lo + m < at_hi)
+            a.live[(int64_t)at_lo + m] = of.live || fabsf(acc[i][0][0]) < INFINITY;
+          const int y = of.y - a.col0;
+#pragma unroll
+          for (int j = 0; j < S::NJ; ++j) {
+            const int n = n_at + j * 16;
+            f32x4 dz;   // takes the logits' place
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float t = fmaxf(fmaf(acc[i][j][r], kLog2e, plus[j][r] - of.lse2), kLeast);
+              dz[r] = exp2_(t) * fmaf(of.B, t, of.A);
+            }
+            if ((unsigned)(y - n) < 4u) {
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                dz[r] += y - n == r && fmaf(acc[i][j][r], kLog2e, plus[j][r]) != -INFINITY ? of.up : 0.f;
+            }
+            if (a.valid) {
+              const uint32_t bits = bits_of(i, j);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) dz[r] = (bits >> r) & 1u ? dz[r] : 0.f;
+            }
+            colsum[j] += dz;   // rows past the tile's last have A = B = up = 0: nothing
+            acc[i][j] = dz;
+          }
+        }
+        if (a.db_part) {
+          float* across = column_sums;   // [WM][BN]
+#pragma unroll
+          for (int j = 0; j < S::NJ; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              float v = colsum[j][r];
+#pragma unroll
+              for (int d = 1; d < 16; d *= 2) v += __shfl_xor(v, d);
+              if (lane % 16 == 0) across[wm * S::BN + n_at - n_first + j * 16 + r] = v;
+            }
+        }
+        auto value = [&](int i, int j) { return acc[i][j]; };
+        auto sums = [&] {   // behind the barrier of the pass through LDS
+          if (a.db_part && tid < S::BN && n_first + tid < a.N) {
+            float v = column_sums[tid];
+#pragma unroll
+            for (int w = 1; w < S::WM; ++w) v += column_sums[w * S::BN + tid];
+            a.db_part[(int64_t)at_rt * a.db_width + a.col0 + n_first + tid] = v;
+          }
+          next();
+        };
+        if (full) {
+          O::run(lds, tid, value, sums, put);
+          last(more);
+        } else {
+          O::run(lds, tid, value, sums, put_some);
+          last(more);
+        }
       }
     }
-    by_rows<T, S>(acc, lds, [&](int m, int n, Run<T>& run) {
-      const int64_t row = part.lo + m;
-      if (row < part.hi && n_first + n < a.N)
-        run.store(static_cast<T*>(a.C) + row * a.ldc + n_first + n, a.N - n_first - n);
-    });
-    if (a.db_part) {
-      __syncthreads();
-      float* across = reinterpret_cast<float*>(lds);   // [WM][BN]
-      static_assert(S::WM * S::BN * 4 <= sizeof(lds), "fits");
-#pragma unroll
-      for (int j = 0; j < S::NJ; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float v = colsum[j][r];
-#pragma unroll
-          for (int d = 1; d < 16; d *= 2) v += __shfl_xor(v, d);
-          if (lane % 16 == 0) across[wm * S::BN + n_at - n_first + j * 16 + r] = v;
-        }
-      __syncthreads();
-      for (int c = threadIdx.x; c < S::BN; c += S::NT) {
-        if (n_first + c >= a.N) continue;
-        float v = across[c];
-#pragma unroll
-        for (int w = 1; w < S::WM; ++w) v += across[w * S::BN + c];
-        a.db_part[(int64_t)rt * a.db_width + a.col0 + n_first + c] = v;
-      }
-    }
+    if (!more) break;
   }
 }
 
@@ -392,14 +537,14 @@ __global__ __launch_bounds__(256) void join_kernel(const RowArgs a) {
       s = join(s, Stats{p[0], p[1], p[2]});
     }
 #pragma unroll
-  for (int d = 16; d < 64; d *= 2) s = join(s, Stats{__shfl_xor(s.top, d), __shfl_xor(s.sum, d), __shfl_xor(s.zsum, d)});
+  for (int d = 16; d < 64; d *= 2) s = join(s, Stats{__shfl_xor(s.top, d), __shfl_xor(s.sum, d), __shfl_xor(s.tsum, d)});
   if (threadIdx.x % 64 < 16) across[threadIdx.x / 64][r] = s;
   __syncthreads();
   if (threadIdx.x >= 16 || row >= end) return;
   for (int w = 1; w < 4; ++w) s = join(s, across[w][r]);
-  bool wrong;
-  const int y = target_of(a, row, wrong);
-  put_row(a, row, s, y, y >= 0 ? a.taken[row] : 0.f);
+  const int y = a.target[row];
+  const bool none = y < 0 || target_wrong(a, row, y);
+  put_row(a, row, s, none ? -1 : y, none ? 0.f : a.taken[row]);
 }
 
 using Large = Shape<2, 4, 8, 4, 1, 128>;    // 256 x 256, 512 threads
@@ -409,7 +554,9 @@ using Small = Shape<2, 2, 2, 2, 2, 128>;    // 64 x 64
 
 template <typename T, class S, bool COLUMNS, int EPI>
 hipError_t launch(const RowArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((rows_kernel<T, S, COLUMNS, EPI>), dim3((unsigned)(a.row_tiles * a.col_tiles)), dim3(S::NT), 0, s, a);
+  // blocks that share the tiles: as many as run at once
+  const int tiles = a.row_tiles * a.col_tiles, most = a.cus * S::kBlocks;
+  hipLaunchKernelGGL((rows_kernel<T, S, COLUMNS, EPI>), dim3((unsigned)(tiles < most ? tiles : most)), dim3(S::NT), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && EPI == kStats && a.col_tiles > 1) {
     hipLaunchKernelGGL(join_kernel, dim3((unsigned)((a.n + 15) / 16)), dim3(256), 0, s, a);

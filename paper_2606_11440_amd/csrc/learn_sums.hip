@@ -27,7 +27,7 @@ __device__ __forceinline__ void store_some(T* p, f32x4 v, int left) {
 }
 
 template <typename T, class S>
-__global__ __launch_bounds__(S::NT, S::kWaves) void sums_kernel(const SumArgs a) {
+__global__ __launch_bounds__(S::NT, S::MI * S::NJ >= 32 ? 2 : 3) void sums_kernel(const SumArgs a) {
   using P = ColTile<T, S::BM, S::NT, S::D, S::SB>;
   using Q = ColTile<T, S::BN, S::NT, S::D, S::SB>;
   using Product = Sum<T, S, P, Q, true>;
@@ -61,8 +61,10 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void sums_kernel(const SumArgs a)
   x.lds = lds;
   x.steps = (rows + P::kStage - 1) / P::kStage;
   x.alone = bias;
-  x.p.init(static_cast<const T*>(a.P), a.ldp, m_first, a.M, part.lo, part.hi);
-  x.q.init(static_cast<const T*>(a.Q), a.ldq, n_first, a.N, part.lo, part.hi, live);
+  x.p.init(static_cast<const T*>(a.P), a.ldp, m_first, a.M, part.lo, part.hi, (int)threadIdx.x);
+  x.q.init(static_cast<const T*>(a.Q), a.ldq, n_first, a.N, part.lo, part.hi, (int)threadIdx.x, live);
+  x.begin();   // a run of rows is not empty
+  x.first_stage();
   x.run();
   auto& acc = x.acc;
   auto& sum = x.sum;

@@ -18,6 +18,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "inframind_learn.h"
+
 namespace im {
 namespace learn {
 
@@ -56,6 +58,15 @@ __device__ __forceinline__ u32x4 load_few(const T* p, int n) {
   return v;
 }
 
+// The thread's number, as a value the compiler takes for new each time: what
+// follows from it is worked out where it is used, not kept in registers through
+// a block's loop over its tiles.
+__device__ __forceinline__ int fresh_thread() {
+  int t = (int)threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
+
 __device__ __forceinline__ int clamp_units(int n, int most) { return n < 0 ? 0 : (n > most ? most : n); }
 
 // A tile of ROWS memory rows with k contiguous, staged by NT threads, D stages
@@ -75,20 +86,21 @@ struct RowTile {
   const char* base;         // of the tile's first row (uniform)
   uint32_t p[kUnits];       // byte offsets of the thread's units
   u32x4 r[D][kUnits];
-  int K;
+  int K, tid;
 
   static __device__ __forceinline__ int key(int row) {
     return SB == 128 ? (row >> 1) & 7 : (4 - (row >> 2)) & 3;
   }
-  static __device__ __forceinline__ int unit() { return (int)threadIdx.x % kRowUnits; }
+  __device__ __forceinline__ int unit() const { return tid % kRowUnits; }
   // rows [first, last] of the operand are the tile's: first <= last (which may be nearer than ROWS - 1)
-  __device__ __forceinline__ void init(const T* from, int64_t ld, int64_t first, int64_t last, int K_) {
+  __device__ __forceinline__ void init(const T* from, int64_t ld, int64_t first, int64_t last, int K_, int tid_) {
     K = K_;
+    tid = tid_;
     base = reinterpret_cast<const char*>(from + first * ld);
     const int most = last - first < ROWS ? (int)(last - first) : ROWS - 1;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
-      const int row = ((int)threadIdx.x + i * NT) / kRowUnits;
+      const int row = (tid + i * NT) / kRowUnits;
       p[i] = ((uint32_t)(row < most ? row : most) * (uint32_t)ld + unit() * kVec<T>) * (uint32_t)sizeof(T);
     }
   }
@@ -122,13 +134,13 @@ struct RowTile {
     }
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
-      const int row = ((int)threadIdx.x + i * NT) / kRowUnits;
+      const int row = (tid + i * NT) / kRowUnits;
       *reinterpret_cast<u32x4*>(lds + row * SB + ((unit() ^ key(row)) << 4)) = r[SLOT][i];
     }
   }
   // fragment of rows [m0, m0 + 16), half s of the stage
-  static __device__ __forceinline__ u32x4 frag(const char* lds, int m0, int s) {
-    const int lane = (int)threadIdx.x % 64, row = m0 + lane % 16;
+  static __device__ __forceinline__ u32x4 frag(const char* lds, int m0, int s, int lane) {
+    const int row = m0 + lane % 16;
     return *reinterpret_cast<const u32x4*>(lds + row * SB + (((s * 4 + lane / 16) ^ key(row)) << 4));
   }
 };
@@ -154,19 +166,21 @@ struct ColTile {
   int k0, k_end;         // rows of k [k0, k_end) are summed
   const uint8_t* live;   // rows of k to take (others are zero, whatever they hold), or NULL: all
   u32x4 r[D][kUnits];
+  int tid;
 
   static __device__ __forceinline__ int at(int k) {
     return k * kPitch + (sizeof(T) == 2 ? (k >> 3) * 128 : 0);
   }
   // columns [from, C) of the operand
-  __device__ __forceinline__ void init(const T* base, int64_t ld_, int from, int C, int k0_, int k_end_,
+  __device__ __forceinline__ void init(const T* base, int64_t ld_, int from, int C, int k0_, int k_end_, int tid_,
                                        const uint8_t* live_ = nullptr) {
     ld = ld_;
+    tid = tid_;
     k0 = k0_;
     k_end = k_end_;
     live = live_;
-    first = (int)threadIdx.x / kRowUnits;
-    const int c = from + ((int)threadIdx.x % kRowUnits) * kVec<T>;
+    first = tid / kRowUnits;
+    const int c = from + (tid % kRowUnits) * kVec<T>;
     n = clamp_units(C - c, kVec<T>);
     edge = from + COLS > C;
     narrow = C < kVec<T>;
@@ -203,12 +217,12 @@ struct ColTile {
     }
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
-      const int idx = (int)threadIdx.x + i * NT;
+      const int idx = tid + i * NT;
       *reinterpret_cast<u32x4*>(lds + at(idx / kRowUnits) + (idx % kRowUnits) * 16) = r[SLOT][i];
     }
   }
-  static __device__ __forceinline__ u32x4 frag(const char* lds, int m0, int s) {
-    const int lane = (int)threadIdx.x % 64, i = lane % 16, g = lane / 16;
+  static __device__ __forceinline__ u32x4 frag(const char* lds, int m0, int s, int lane) {
+    const int i = lane % 16, g = lane / 16;
     if constexpr (sizeof(T) == 2) {
       const char* q = lds + at(s * 32 + g * 8 + i / 4) + (m0 + (i % 4) * 4) * 2;
       typedef __attribute__((address_space(3))) s16x4 lds4;
@@ -257,7 +271,8 @@ __device__ __forceinline__ float add_up(u32x4 a) {
 template <int WM_, int WN_, int MI_, int NJ_, int D_, int SB_>
 struct Shape {
   static constexpr int WM = WM_, WN = WN_, MI = MI_, NJ = NJ_, D = D_, SB = SB_;
-  static constexpr int kWaves = MI * NJ >= 32 ? 2 : (MI * NJ >= 16 ? 3 : 4);   // a SIMD, by the registers they take
+  static constexpr int kWaves = MI * NJ >= 16 ? 2 : 3;   // a SIMD, by the registers (and LDS) they take
+  static constexpr int kBlocks = MI * NJ >= 32 ? 1 : (MI * NJ >= 16 ? 2 : (MI * NJ >= 8 ? 3 : 4));   // a CU
   static constexpr int NT = WM * WN * 64, BM = WM * MI * 16, BN = WN * NJ * 16;
 };
 
@@ -292,15 +307,15 @@ struct Sum {
       p.template load<kNext>(kt + 1 + S::D);
       q.template load<kNext>(kt + 1 + S::D);
     }
-    const int wave = (int)threadIdx.x / 64, m0 = (wave / S::WN) * S::MI * 16, n0 = (wave % S::WN) * S::NJ * 16;
+    const int wave = p.tid / 64, lane = p.tid % 64, m0 = (wave / S::WN) * S::MI * 16, n0 = (wave % S::WN) * S::NJ * 16;
     const char* at = lds + (kt & 1) * kBuf;
 #pragma unroll
     for (int s = 0; s < S::SB / kHalf; ++s) {
       u32x4 a[S::MI], b[S::NJ];
 #pragma unroll
-      for (int j = 0; j < S::NJ; ++j) b[j] = Q::frag(at + P::kBytes, n0 + j * 16, s);
+      for (int j = 0; j < S::NJ; ++j) b[j] = Q::frag(at + P::kBytes, n0 + j * 16, s, lane);
 #pragma unroll
-      for (int i = 0; i < S::MI; ++i) a[i] = P::frag(at, m0 + i * 16, s);
+      for (int i = 0; i < S::MI; ++i) a[i] = P::frag(at, m0 + i * 16, s, lane);
 #pragma unroll
       for (int i = 0; i < S::MI; ++i)
 #pragma unroll
@@ -332,23 +347,26 @@ struct Sum {
       round<SLOT + 1, WHOLE>(kt + 1);
     }
   }
-  __device__ __forceinline__ void run() {
-#pragma unroll
-    for (int i = 0; i < S::MI; ++i) {
-#pragma unroll
-      for (int j = 0; j < S::NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if constexpr (ALONE) sum[i] = 0.f;
-    }
-    if (steps <= 0) return;
-    first_loads<0>();
+  // A sum in three parts: begin() issues the first loads (p, q and steps set),
+  // first_stage() takes the first stage to LDS, run() multiplies.
+  __device__ __forceinline__ void begin() { first_loads<0>(); }
+  __device__ __forceinline__ void first_stage() {
     p.template store<0>(0, lds);
     q.template store<0>(0, lds + P::kBytes);
     if (S::D < steps) {
       p.template load<0>(S::D);
       q.template load<0>(S::D);
     }
+  }
+  __device__ __forceinline__ void run() {   // steps >= 1
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i) {
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (ALONE) sum[i] = 0.f;
+    }
     __syncthreads();
-    // stages that are whole, as are those D ahead of them, take no branch
+    // stages that are whole, as are those D behind them, take no branch
     const int wp = p.whole(), wq = q.whole(), whole = (wp < wq ? wp : wq);
     int kt = 0;
     for (; kt + 2 * S::D + 1 <= whole; kt += S::D) round<0, true>(kt);
@@ -435,7 +453,70 @@ __device__ __forceinline__ bool find_group(const int32_t* off, int G, int n, int
   return true;
 }
 
-// Tile (row, column) of block `b` of rows x cols tiles: the blocks of an XCD
+// The groups' rows cut into runs of `step`, as find_part counts them, kept in
+// LDS by a block that takes many of them.
+struct Groups {
+  int start[IM_MAX_GROUPS + 1];   // runs before group g
+  int row[IM_MAX_GROUPS + 1];     // first row of group g
+  int total;                      // runs; -1: the CSR is broken
+
+  __device__ __forceinline__ void init(const int32_t* off, int G, int n, int step) {
+    const int lane = (int)threadIdx.x % 64;
+    if (threadIdx.x >= 64) return;
+    if (!off) {
+      if (lane == 0) {
+        start[0] = row[0] = 0;
+        row[1] = n;
+        start[1] = total = (int)(((int64_t)n + step - 1) / step);
+      }
+      return;
+    }
+    int before = 0;
+    bool bad = false;
+    for (int base = 0; base < G; base += 64) {
+      const int g = base + lane;
+      const int a = g < G ? off[g] : 0, b = g < G ? off[g + 1] : 0;
+      const bool wrong = a < 0 || b < a || b > n || (g == 0 && a != 0);
+      bad |= __ballot(wrong) != 0;
+      if (bad) break;
+      const int t = (int)(((int64_t)(b - a) + step - 1) / step);
+      int s = t;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const int o = __shfl_up(s, d);
+        if (lane >= d) s += o;
+      }
+      if (g < G) {
+        start[g] = before + s - t;
+        row[g] = a;
+        if (g == G - 1) row[G] = b;
+      }
+      before += __builtin_amdgcn_readlane(s, 63);
+    }
+    if (lane == 0) {
+      start[G] = before;
+      total = bad ? -1 : before;
+    }
+  }
+  // The group of run `want` (< total) and its rows; the same in all lanes.
+  __device__ __forceinline__ void find(int G, int step, int want, int& g, int& lo, int& hi) const {
+    const int lane = (int)threadIdx.x % 64;
+    g = 0;
+    if (G > 1) {   // the last group that starts at or before it
+      const int each = (G + 63) / 64, first = lane * each;
+      const int c = __builtin_popcountll(__ballot(first < G && start[first < G ? first : 0] <= want));
+      const int base = (c - 1) * each, at = base + lane;
+      const bool in = lane < each && at < G;
+      g = base + __builtin_popcountll(__ballot(in && start[in ? at : 0] <= want)) - 1;
+    }
+    g = __builtin_amdgcn_readfirstlane(g);
+    const int end = __builtin_amdgcn_readfirstlane(row[g + 1]);
+    lo = __builtin_amdgcn_readfirstlane(row[g] + (want - start[g]) * step);
+    hi = end - lo > step ? lo + step : end;
+  }
+};
+
+// Tile (row, column) of number `b` of rows x cols tiles: the blocks of an XCD
 // (b % 8) take neighbouring tiles, eight rows of tiles at a time, so that those
 // running together share operands in its L2.
 __device__ __forceinline__ void tile_of(int b, int rows, int cols, int& row, int& col) {
