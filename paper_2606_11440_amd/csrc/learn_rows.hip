@@ -192,7 +192,6 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
   using Product = Sum<T, S, P, Q, false>;
   constexpr bool kHead = EPI == kStats || EPI == kGradLogits;
   __shared__ __attribute__((aligned(16))) char lds[2 * Product::kBuf];
-  __shared__ Row rows[kHead ? S::BM : 1];
   __shared__ Groups groups;
   __shared__ float column_sums[EPI == kGradLogits ? S::WM * S::BN : 1];
   static_assert(S::NT >= S::BM, "a thread a row");
@@ -216,7 +215,7 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
   auto enter = [&](int t) {   // takes tile t: its first loads are on their way
     const int tid = fresh_thread();
     tile_of(t, row_tiles, a.col_tiles, rt, ct);
-    groups.find(a.G, S::BM, rt, g, lo, hi);
+    groups.find(a.offsets, a.G, a.n, S::BM, rt, g, lo, hi);
     const T* B = static_cast<const T*>(a.B) + g * a.b_group;
     x.p.init(static_cast<const T*>(a.A), a.lda, lo, hi - 1, a.K, tid);
     // ct * BN < N: the launch has no column tiles past the operand
@@ -234,6 +233,9 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
     const int wm = wave / S::WN, wn = wave % S::WN, m_at = wm * S::MI * 16 + lane % 16;
     // the tile at hand; the next one's loads run through its epilogue
     const int at_lo = lo, at_hi = hi, at_rt = rt, at_ct = ct, at_g = g, n_first = ct * S::BN;
+    // a head's rows, behind what the statistics take of the stages' LDS
+    Row* const rows = reinterpret_cast<Row*>(lds + S::BM * 4 + S::WN * S::BM * (int)sizeof(Stats));
+    static_assert(S::BM * (4 + S::WN * (int)sizeof(Stats) + (int)sizeof(Row)) <= (int)sizeof(lds), "fits");
     if constexpr (kHead) {
       const bool wrong = mine.check(a, (int64_t)lo + tid, hi, EPI == kGradLogits);
       if (wrong && a.col0 == 0 && ct == 0 && a.error) atomicOr(a.error, IM_ERR_ACTION);
@@ -383,7 +385,6 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
         // each row's classes lie in four lanes of WN waves
         float* taken = reinterpret_cast<float*>(lds);                    // [BM]
         Stats* across = reinterpret_cast<Stats*>(lds + S::BM * 4);       // [WN][BM]
-        static_assert(S::BM * 4 + S::WN * S::BM * sizeof(Stats) <= sizeof(lds), "fits");
         const bool whole = a.col_tiles == 1, edge = n_first + S::BN > a.N;
 #pragma unroll
         for (int i = 0; i < S::MI; ++i) {
@@ -494,6 +495,7 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
               if (lane % 16 == 0) across[wm * S::BN + n_at - n_first + j * 16 + r] = v;
             }
         }
+        __syncthreads();   // the rows are read: the results take the LDS
         auto value = [&](int i, int j) { return acc[i][j]; };
         auto sums = [&] {   // behind the barrier of the pass through LDS
           if (a.db_part && tid < S::BN && n_first + tid < a.N) {

@@ -457,7 +457,6 @@ __device__ __forceinline__ bool find_group(const int32_t* off, int G, int n, int
 // LDS by a block that takes many of them.
 struct Groups {
   int start[IM_MAX_GROUPS + 1];   // runs before group g
-  int row[IM_MAX_GROUPS + 1];     // first row of group g
   int total;                      // runs; -1: the CSR is broken
 
   __device__ __forceinline__ void init(const int32_t* off, int G, int n, int step) {
@@ -465,8 +464,7 @@ struct Groups {
     if (threadIdx.x >= 64) return;
     if (!off) {
       if (lane == 0) {
-        start[0] = row[0] = 0;
-        row[1] = n;
+        start[0] = 0;
         start[1] = total = (int)(((int64_t)n + step - 1) / step);
       }
       return;
@@ -488,8 +486,6 @@ struct Groups {
       }
       if (g < G) {
         start[g] = before + s - t;
-        row[g] = a;
-        if (g == G - 1) row[G] = b;
       }
       before += __builtin_amdgcn_readlane(s, 63);
     }
@@ -499,7 +495,8 @@ struct Groups {
     }
   }
   // The group of run `want` (< total) and its rows; the same in all lanes.
-  __device__ __forceinline__ void find(int G, int step, int want, int& g, int& lo, int& hi) const {
+  __device__ __forceinline__ void find(const int32_t* off, int G, int n, int step, int want, int& g, int& lo,
+                                       int& hi) const {
     const int lane = (int)threadIdx.x % 64;
     g = 0;
     if (G > 1) {   // the last group that starts at or before it
@@ -510,8 +507,8 @@ struct Groups {
       g = base + __builtin_popcountll(__ballot(in && start[in ? at : 0] <= want)) - 1;
     }
     g = __builtin_amdgcn_readfirstlane(g);
-    const int end = __builtin_amdgcn_readfirstlane(row[g + 1]);
-    lo = __builtin_amdgcn_readfirstlane(row[g] + (want - start[g]) * step);
+    const int begin = off ? off[g] : 0, end = off ? off[g + 1] : n;
+    lo = begin + (want - __builtin_amdgcn_readfirstlane(start[g])) * step;
     hi = end - lo > step ? lo + step : end;
   }
 };
