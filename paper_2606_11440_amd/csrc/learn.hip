@@ -82,8 +82,14 @@ im_status check_work(const void* ws, int64_t have, int64_t need) {
   LEARN_CHECK(need == 0 || aligned(ws, 256), "workspace is not 256-byte aligned");
   return IM_OK;
 }
-im_status check_launch(int64_t tiles) {
-  if (tiles > 0x7fffffff) return fail(IM_EUNSUPPORTED, "more than 2^31 - 1 tiles");
+im_status check_launch(const RowPlan& p) {
+  if (p.row_tiles * p.col_tiles * p.splits > 0x7fffffff) return fail(IM_EUNSUPPORTED, "more than 2^31 - 1 tiles");
+  return IM_OK;
+}
+im_status check_grid(const SumPlan& p, int64_t groups) {
+  // tiles and groups are the second and third dimension of the joining launch
+  if (p.parts * p.row_tiles * p.col_tiles > 0x7fffffff) return fail(IM_EUNSUPPORTED, "more than 2^31 - 1 blocks");
+  if (p.row_tiles * p.col_tiles > 65535 || groups > 65535) return fail(IM_EUNSUPPORTED, "more than 65535 tiles of a gradient");
   return IM_OK;
 }
 #define LEARN_OK(call)                       \
@@ -105,20 +111,17 @@ im_status check_linear(const im_linear_desc* d) {
   return IM_OK;
 }
 
-struct LinearWork {
-  SumPlan sums;
+struct SumWork {
+  SumPlan plan;
   float* part;
-  int64_t part_width, db_at, bytes;
+  int64_t bytes;
 };
-// Plan and workspace of the weight and bias gradients.
-LinearWork linear_work(int dtype, int64_t n, int64_t G, int64_t M, int64_t N, void* ws) {
-  LinearWork w;
-  w.sums = plan_sums(dtype, n, G, M, N, compute_units());
-  w.db_at = (M * N + 3) & ~(int64_t)3;
-  w.part_width = w.db_at + ((M + 3) & ~(int64_t)3);
+// Plan and workspace of the sums over rows.
+SumWork sum_work(int dtype, int64_t n, int64_t G, int64_t M, int64_t N, void* ws) {
+  SumWork w;
+  w.plan = plan_sums(dtype, n, G, M, N, compute_units());
   Sections s(ws);
-  // one group of one chunk stores its gradient at once
-  w.part = s.take<float>(w.sums.chunks > 1 ? w.sums.chunks * w.part_width : 0);
+  w.part = s.take<float>(w.plan.parts > 1 || G > 1 ? 2 * w.plan.parts * w.plan.row_tiles * w.plan.col_tiles * w.plan.piece : 0);
   w.bytes = s.used;
   return w;
 }
@@ -132,7 +135,40 @@ RowArgs row_args(const int32_t* offsets, int32_t G, int32_t n, const RowPlan& p,
   a.col_tiles = (int32_t)p.col_tiles;
   a.error = error;
   a.cus = compute_units();
+  a.splits = (int32_t)p.splits;
+  a.split_k = (int32_t)p.split_k;
   return a;
+}
+
+// A row product with the workspace of its runs of k.
+struct RowWork {
+  RowPlan plan;
+  float* part;
+  int64_t bytes;
+};
+RowWork row_work(int dtype, int64_t n, int64_t G, int64_t N, int64_t K, bool may_split, void* ws) {
+  RowWork w;
+  w.plan = plan_rows(dtype, n, G, N, K, compute_units(), may_split);
+  Sections s(ws);
+  w.part = s.take<float>(w.plan.splits > 1 ? w.plan.splits * n * N : 0);
+  w.bytes = s.used;
+  return w;
+}
+RowWork linear_forward(const im_linear_desc& d, void* ws) {
+  return row_work(d.dtype, d.n_rows, d.n_groups, d.out_dim, d.in_dim, true, ws);
+}
+struct LinearBackward {
+  RowWork input;
+  SumWork sums;
+  int64_t bytes;
+};
+LinearBackward linear_backward(const im_linear_desc& d, void* ws) {
+  LinearBackward w;
+  w.input = row_work(d.dtype, d.n_rows, d.n_groups, d.in_dim, d.out_dim, true, ws);
+  w.sums = sum_work(d.dtype, d.n_rows, d.n_groups, d.out_dim, d.in_dim,
+                    ws ? static_cast<char*>(ws) + w.input.bytes : nullptr);
+  w.bytes = w.input.bytes + w.sums.bytes;
+  return w;
 }
 
 }  // namespace
@@ -145,7 +181,7 @@ im_status im_linear_workspace(const im_linear_desc* d, int32_t backward, int64_t
   LEARN_OK(check_linear(d));
   LEARN_CHECK(bytes, "bytes is NULL");
   LEARN_CHECK(backward == 0 || backward == 1, "backward is 0 or 1");
-  *bytes = backward ? linear_work(d->dtype, d->n_rows, d->n_groups, d->out_dim, d->in_dim, nullptr).bytes : 0;
+  *bytes = backward ? linear_backward(*d, nullptr).bytes : linear_forward(*d, nullptr).bytes;
   return IM_OK;
 }
 
@@ -158,11 +194,12 @@ im_status im_linear_forward(const im_linear_desc* d, const int32_t* offsets, con
   LEARN_CHECK(W && (d->n_rows == 0 || (x && y)), "x, W or y is NULL");
   LEARN_CHECK(aligned(x, e) && aligned(W, e) && aligned(y, e) && aligned(b, 4) && aligned(error, 4),
               "a pointer is not aligned to its elements");
-  LEARN_OK(check_work(ws, ws_bytes, 0));
+  const RowWork w = linear_forward(*d, ws);
+  LEARN_OK(check_work(ws, ws_bytes, w.bytes));
   if (d->n_rows == 0) return IM_OK;
-  const RowPlan p = plan_rows(d->dtype, d->n_rows, d->n_groups, d->out_dim, compute_units());
-  LEARN_OK(check_launch(p.row_tiles * p.col_tiles));
-  RowArgs a = row_args(offsets, d->n_groups, d->n_rows, p, error);
+  LEARN_OK(check_launch(w.plan));
+  RowArgs a = row_args(offsets, d->n_groups, d->n_rows, w.plan, error);
+  a.part = w.part;
   a.K = d->in_dim;
   a.N = d->out_dim;
   a.A = x;
@@ -175,7 +212,7 @@ im_status im_linear_forward(const im_linear_desc* d, const int32_t* offsets, con
   a.C = y;
   a.ldc = d->ld_y;
   a.relu = d->relu;
-  LEARN_HIP(launch_rows_product(a, d->dtype, p.shape, kStore, (hipStream_t)stream));
+  LEARN_HIP(launch_rows_product(a, d->dtype, w.plan.shape, kStore, (hipStream_t)stream));
   return IM_OK;
 }
 
@@ -194,13 +231,13 @@ im_status im_linear_backward(const im_linear_desc* d, const int32_t* offsets, co
   LEARN_CHECK(aligned(dy, e) && aligned(x, e) && aligned(W, e) && aligned(dx, e) && aligned(dW, e) && aligned(db, 4) &&
                   aligned(error, 4),
               "a pointer is not aligned to its elements");
-  const LinearWork w = linear_work(d->dtype, d->n_rows, d->n_groups, d->out_dim, d->in_dim, ws);
+  const LinearBackward w = linear_backward(*d, ws);
   LEARN_OK(check_work(ws, ws_bytes, w.bytes));
-  const RowPlan p = plan_rows(d->dtype, d->n_rows, d->n_groups, d->in_dim, compute_units());
-  LEARN_OK(check_launch(p.row_tiles * p.col_tiles));
-  LEARN_OK(check_launch(w.sums.chunks * w.sums.row_tiles * w.sums.col_tiles));
+  LEARN_OK(check_launch(w.input.plan));
+  LEARN_OK(check_grid(w.sums.plan, d->n_groups));
   if (dx && some) {
-    RowArgs a = row_args(offsets, d->n_groups, d->n_rows, p, error);
+    RowArgs a = row_args(offsets, d->n_groups, d->n_rows, w.input.plan, error);
+    a.part = w.input.part;
     a.K = d->out_dim;
     a.N = d->in_dim;
     a.A = dy;
@@ -213,7 +250,7 @@ im_status im_linear_backward(const im_linear_desc* d, const int32_t* offsets, co
     a.X = d->relu_in ? x : nullptr;
     a.ldx = d->ld_x;
     a.first = a.last = 1;
-    LEARN_HIP(launch_rows_product(a, d->dtype, p.shape, kStoreInput, (hipStream_t)stream));
+    LEARN_HIP(launch_rows_product(a, d->dtype, w.input.plan.shape, kStoreInput, (hipStream_t)stream));
   }
   if (dW || db) {
     SumArgs a = {};
@@ -229,15 +266,13 @@ im_status im_linear_backward(const im_linear_desc* d, const int32_t* offsets, co
     a.dW = dW;
     a.w_group = (int64_t)d->in_dim * d->out_dim;
     a.db = db;
-    a.part = w.part;
-    a.part_width = w.part_width;
-    a.db_at = w.db_at;
-    a.chunk = (int32_t)w.sums.chunk;
-    a.chunks = (int32_t)w.sums.chunks;
-    a.row_tiles = (int32_t)w.sums.row_tiles;
-    a.col_tiles = dW ? (int32_t)w.sums.col_tiles : 1;
+    a.part = w.sums.part;
+    a.granule = (int32_t)w.sums.plan.granule;
+    a.parts = (int32_t)w.sums.plan.parts;
+    a.row_tiles = (int32_t)w.sums.plan.row_tiles;
+    a.col_tiles = dW ? (int32_t)w.sums.plan.col_tiles : 1;
     a.error = error;
-    LEARN_HIP(launch_sums(a, d->dtype, w.sums.shape, (hipStream_t)stream));
+    LEARN_HIP(launch_sums(a, d->dtype, w.sums.plan.shape, (hipStream_t)stream));
   }
   return IM_OK;
 }
@@ -266,7 +301,7 @@ struct HeadForward {
 };
 HeadForward head_forward(const im_head_desc& d, void* ws) {
   HeadForward w;
-  w.plan = plan_rows(d.dtype, d.n_rows, d.n_groups, d.n_classes, compute_units());
+  w.plan = plan_rows(d.dtype, d.n_rows, d.n_groups, d.n_classes, d.dim, compute_units(), false);
   Sections s(ws);
   const bool split = w.plan.col_tiles > 1;
   w.stats = s.take<float>(split ? w.plan.col_tiles * d.n_rows * 3 : 0);
@@ -278,32 +313,33 @@ HeadForward head_forward(const im_head_desc& d, void* ws) {
 // The gradient's pieces: dz of `width` classes at a time.
 struct HeadBackward {
   int64_t width, pieces;
-  RowPlan logits, input;
-  LinearWork sums;
+  RowPlan logits;
+  RowWork input;
+  SumWork sums;
   void* dz;
   float *sum, *db_part;
   uint8_t* live;
-  void* sums_ws;
   int64_t bytes;
 };
 HeadBackward head_backward(const im_head_desc& d, void* ws) {
   HeadBackward w;
   const int64_t n = d.n_rows, G = d.n_groups, V = d.n_classes;
   const int cus = compute_units();
-  // dz of a piece stays within 2^27 elements, and a piece is 1024 classes at least
-  int64_t width = n > 0 ? ((int64_t)1 << 27) / n : V;
-  width = width < 1024 ? 1024 : width / 1024 * 1024;
-  w.pieces = (V + width - 1) / width;
-  w.width = w.pieces > 1 ? width : (V + 7) / 8 * 8;
-  w.logits = plan_rows(d.dtype, n, G, w.pieces > 1 ? width : V, cus);
-  w.input = plan_rows(d.dtype, n, G, d.dim, cus);
+  // dz of a piece stays within 2^27 elements; pieces are alike and 1024 classes at least
+  const int64_t most = n > 0 ? ((int64_t)1 << 27) / n : V;
+  w.pieces = (V + (most < 1024 ? 1024 : most) - 1) / (most < 1024 ? 1024 : most);
+  w.width = w.pieces > 1 ? ((V + w.pieces - 1) / w.pieces + 255) / 256 * 256 : (V + 7) / 8 * 8;
+  w.pieces = (V + w.width - 1) / w.width;
+  const int64_t classes = w.pieces > 1 ? w.width : V;
+  w.logits = plan_rows(d.dtype, n, G, classes, d.dim, cus, false);
   Sections s(ws);
   w.dz = s.take<char>(n * w.width * size_of(d.dtype));
   w.sum = s.take<float>(w.pieces > 1 ? n * d.dim : 0);
   w.db_part = s.take<float>(w.logits.row_tiles * V);
   w.live = s.take<uint8_t>(n);
-  w.sums_ws = s.base ? s.base + s.used : nullptr;
-  w.sums = linear_work(d.dtype, n, G, w.pieces > 1 ? width : V, d.dim, w.sums_ws);
+  w.input = row_work(d.dtype, n, G, d.dim, classes, true, s.base ? s.base + s.used : nullptr);
+  s.used += w.input.bytes;
+  w.sums = sum_work(d.dtype, n, G, classes, d.dim, s.base ? s.base + s.used : nullptr);
   w.bytes = s.used + w.sums.bytes;
   return w;
 }
@@ -334,7 +370,7 @@ im_status im_head_forward(const im_head_desc* d, const int32_t* offsets, const v
   if (d->n_rows == 0) return IM_OK;
   const HeadForward w = head_forward(*d, ws);
   LEARN_OK(check_work(ws, ws_bytes, w.bytes));
-  LEARN_OK(check_launch(w.plan.row_tiles * w.plan.col_tiles));
+  LEARN_OK(check_launch(w.plan));
   RowArgs a = row_args(offsets, d->n_groups, d->n_rows, w.plan, error);
   a.K = d->dim;
   a.N = a.V = d->n_classes;
@@ -374,9 +410,9 @@ im_status im_head_backward(const im_head_desc* d, const int32_t* offsets, const 
               "a pointer is not aligned to its elements");
   const HeadBackward w = head_backward(*d, ws);
   LEARN_OK(check_work(ws, ws_bytes, w.bytes));
-  LEARN_OK(check_launch(w.logits.row_tiles * w.logits.col_tiles));
-  LEARN_OK(check_launch(w.input.row_tiles * w.input.col_tiles));
-  LEARN_OK(check_launch(w.sums.sums.chunks * w.sums.sums.row_tiles * w.sums.sums.col_tiles));
+  LEARN_OK(check_launch(w.logits));
+  LEARN_OK(check_launch(w.input.plan));
+  LEARN_OK(check_grid(w.sums.plan, d->n_groups));
   if (!dh && !dW && !db) return IM_OK;
   const hipStream_t s = (hipStream_t)stream;
   const int64_t V = d->n_classes;
@@ -412,7 +448,9 @@ im_status im_head_backward(const im_head_desc* d, const int32_t* offsets, const 
       LEARN_HIP(launch_rows_product(a, d->dtype, w.logits.shape, kGradLogits, s));
     }
     if (dh && some) {
-      RowArgs a = row_args(offsets, d->n_groups, d->n_rows, w.input, error);
+      RowArgs a = row_args(offsets, d->n_groups, d->n_rows, w.input.plan, error);
+      a.part = w.input.part;
+      if (a.split_k * (int64_t)(a.splits - 1) >= width) a.splits = (int32_t)((width + a.split_k - 1) / a.split_k);   // the last piece
       a.K = (int32_t)width;
       a.N = d->dim;
       a.A = w.dz;
@@ -427,7 +465,7 @@ im_status im_head_backward(const im_head_desc* d, const int32_t* offsets, const 
       a.sum = w.pieces > 1 ? w.sum : nullptr;
       a.first = piece == 0;
       a.last = piece == w.pieces - 1;
-      LEARN_HIP(launch_rows_product(a, d->dtype, w.input.shape, kStoreInput, s));
+      LEARN_HIP(launch_rows_product(a, d->dtype, w.input.plan.shape, kStoreInput, s));
     }
     if (dW) {
       SumArgs a = {};
@@ -444,15 +482,13 @@ im_status im_head_backward(const im_head_desc* d, const int32_t* offsets, const 
       a.dW = static_cast<char*>(dW) + c0 * d->dim * e;
       a.w_group = V * d->dim;
       a.part = w.sums.part;
-      a.part_width = w.sums.part_width;
-      a.db_at = (width * d->dim + 3) & ~(int64_t)3;
-      a.chunk = (int32_t)w.sums.sums.chunk;
-      a.chunks = (int32_t)w.sums.sums.chunks;
-      const int64_t tile = rows_per_sum(w.sums.sums.shape);
+      a.granule = (int32_t)w.sums.plan.granule;
+      a.parts = (int32_t)w.sums.plan.parts;
+      const int64_t tile = rows_per_sum(w.sums.plan.shape);
       a.row_tiles = (int32_t)((width + tile - 1) / tile);
-      a.col_tiles = (int32_t)w.sums.sums.col_tiles;
+      a.col_tiles = (int32_t)w.sums.plan.col_tiles;
       a.error = error;
-      LEARN_HIP(launch_sums(a, d->dtype, w.sums.sums.shape, s));
+      LEARN_HIP(launch_sums(a, d->dtype, w.sums.plan.shape, s));
     }
   }
   if (db)

@@ -13,7 +13,8 @@ enum Epilogue {
   kStore = 0,     // y = act(sum + b)
   kStoreInput,    // dx = sum, zero where x <= 0 with relu_in
   kStats,         // per row and column tile: largest logit, sum exp, sum exp (z - largest)
-  kGradLogits     // dz of a piece of the classes
+  kGradLogits,    // dz of a piece of the classes
+  kPartial        // the sums of a run of k, in fp32 (joined by a kernel of their own)
 };
 
 // A product of the groups' rows with their weights: out[i][j] = sum_k A[i][k] B_g(j, k).
@@ -32,6 +33,8 @@ struct RowArgs {
   int32_t* error;
   int32_t row_tiles, col_tiles;   // at most, and exactly
   int32_t cus;                    // compute units of the device
+  int32_t splits, split_k;        // runs of k, and their length (a multiple of the stage); 1: the whole
+  float* part;                    // [splits][n][N] with splits > 1
   // kStoreInput
   const void* X;              // relu_in: the layer's input
   int64_t ldx;
@@ -65,9 +68,8 @@ struct SumArgs {
   void* dW;                   // [G x w_group], rows of N
   int64_t w_group;
   float* db;                  // [G x M] or NULL
-  float* part;                // [chunks][part_width] sums of groups of several chunks: M x N, then M at db_at
-  int64_t part_width, db_at;
-  int32_t chunk, chunks;      // rows of a chunk; chunks the launch covers
+  float* part;                // [2 parts][tiles][tile and its rows]: pieces of groups that parts cut
+  int32_t granule, parts;     // rows of a granule; parts of the line of granules
   int32_t row_tiles, col_tiles;
   int32_t* error;
 };
@@ -76,14 +78,15 @@ struct SumArgs {
 // (row tiles: at most; the groups' sizes are known on the device only).
 struct RowPlan {
   int shape;
-  int64_t row_tiles, col_tiles;
+  int64_t row_tiles, col_tiles, splits, split_k;
 };
-RowPlan plan_rows(int dtype, int64_t n, int64_t G, int64_t N, int cus);
+// may_split: the epilogue can follow a join of several runs of k
+RowPlan plan_rows(int dtype, int64_t n, int64_t G, int64_t N, int64_t K, int cus, bool may_split);
 hipError_t launch_rows_product(const RowArgs& a, int dtype, int shape, int epilogue, hipStream_t s);
 
 struct SumPlan {
   int shape;
-  int64_t row_tiles, col_tiles, chunk, chunks;
+  int64_t row_tiles, col_tiles, granule, parts, piece;   // piece: floats of a block's piece
 };
 SumPlan plan_sums(int dtype, int64_t n, int64_t G, int64_t M, int64_t N, int cus);
 hipError_t launch_sums(const SumArgs& a, int dtype, int shape, hipStream_t s);

@@ -203,7 +203,8 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
     if (blockIdx.x == 0 && threadIdx.x == 0 && a.error) atomicOr(a.error, IM_ERR_COUNT);
     return;
   }
-  const int row_tiles = groups.total, total = row_tiles * a.col_tiles;
+  // with several runs of k a tile is as many units of work, one after the other
+  const int row_tiles = groups.total, splits = EPI == kPartial ? a.splits : 1, total = row_tiles * a.col_tiles * splits;
   int tile = blockIdx.x;
   if (tile >= total) return;
 
@@ -211,16 +212,24 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
   x.lds = lds;
   x.steps = (a.K + P::kStage - 1) / P::kStage;
   Row mine;
-  int rt, ct, g, lo, hi;
+  int rt, ct, g, lo, hi, split = 0;
   auto enter = [&](int t) {   // takes tile t: its first loads are on their way
     const int tid = fresh_thread();
+    int k0 = 0, K = a.K;
+    if constexpr (EPI == kPartial) {
+      split = t % splits;
+      t /= splits;
+      k0 = split * a.split_k;
+      K = a.K - k0 < a.split_k ? a.K - k0 : a.split_k;
+      x.steps = (K + P::kStage - 1) / P::kStage;
+    }
     tile_of(t, row_tiles, a.col_tiles, rt, ct);
     groups.find(a.offsets, a.G, a.n, S::BM, rt, g, lo, hi);
     const T* B = static_cast<const T*>(a.B) + g * a.b_group;
-    x.p.init(static_cast<const T*>(a.A), a.lda, lo, hi - 1, a.K, tid);
+    x.p.init(static_cast<const T*>(a.A) + k0, a.lda, lo, hi - 1, K, tid);
     // ct * BN < N: the launch has no column tiles past the operand
-    if constexpr (COLUMNS) x.q.init(B, a.ldb, ct * S::BN, a.N, 0, a.K, tid);
-    else x.q.init(B, a.ldb, ct * S::BN, a.N - 1, a.K, tid);
+    if constexpr (COLUMNS) x.q.init(B, a.ldb, ct * S::BN, a.N, k0, k0 + K, tid);
+    else x.q.init(B + k0, a.ldb, ct * S::BN, a.N - 1, K, tid);
     x.begin();
     if constexpr (kHead) mine.load(a, (int64_t)lo + tid, hi, EPI == kGradLogits);
   };
@@ -232,7 +241,7 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
     const int tid = fresh_thread(), lane = tid % 64, wave = tid / 64, g4 = (lane / 16) * 4;
     const int wm = wave / S::WN, wn = wave % S::WN, m_at = wm * S::MI * 16 + lane % 16;
     // the tile at hand; the next one's loads run through its epilogue
-    const int at_lo = lo, at_hi = hi, at_rt = rt, at_ct = ct, at_g = g, n_first = ct * S::BN;
+    const int at_lo = lo, at_hi = hi, at_rt = rt, at_ct = ct, at_g = g, at_split = split, n_first = ct * S::BN;
     // a head's rows, behind what the statistics take of the stages' LDS
     Row* const rows = reinterpret_cast<Row*>(lds + S::BM * 4 + S::WN * S::BM * (int)sizeof(Stats));
     static_assert(S::BM * (4 + S::WN * (int)sizeof(Stats) + (int)sizeof(Row)) <= (int)sizeof(lds), "fits");
@@ -268,6 +277,17 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
       if (left >= kVec<T>) *reinterpret_cast<u32x4_any*>(to) = v;
       else store_few(to, v, left);
     };
+
+    if constexpr (EPI == kPartial) {
+      using F = Out<float, S, (int)sizeof(lds)>;
+      float* const part = a.part + (int64_t)at_split * a.n * a.N;
+      F::run(lds, tid, [&](int i, int j) { return acc[i][j]; }, next, [&](int, int m, int c, u32x4 v) {
+        const int64_t row = (int64_t)at_lo + m;
+        const int n = n_first + c;
+        if (row < at_hi && n < a.N) store4(part + row * a.N + n, __builtin_bit_cast(f32x4, v), a.N - n);
+      });
+      last(more);
+    }
 
     if constexpr (EPI == kStore) {
       f32x4 plus[S::NJ];
@@ -549,6 +569,58 @@ __global__ __launch_bounds__(256) void join_kernel(const RowArgs a) {
   put_row(a, row, s, none ? -1 : y, none ? 0.f : a.taken[row]);
 }
 
+// Joins the runs of k and finishes as kStore (STORE) or kStoreInput do: four
+// columns of a row a thread.
+template <typename T, bool STORE>
+__global__ __launch_bounds__(256) void join_k_kernel(const RowArgs a) {
+  const int across = (a.N + 3) / 4;
+  int end = a.n;
+  if (a.offsets) {
+    Part run;
+    bool bad;
+    find_part(a.offsets, a.G, a.n, 1, 0, run, bad);
+    if (bad) return;
+    end = a.offsets[a.G];
+  }
+  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x, row = idx / across;
+  if (row >= end) return;
+  const int n = (int)(idx % across) * 4, left = a.N - n;
+  const int64_t step = (int64_t)a.n * a.N;
+  const float* part = a.part + row * a.N + n;
+  f32x4 v = load4(part, left);
+#pragma unroll 4
+  for (int s = 1; s < a.splits; ++s) v += load4(part + s * step, left);
+  if constexpr (STORE) {
+    if (a.bias) {
+      int g = 0, over = a.offsets ? a.G : 1;   // the last group that begins at or before the row
+      while (over - g > 1) {
+        const int mid = (g + over) / 2;
+        if (a.offsets[mid] <= row) g = mid;
+        else over = mid;
+      }
+      v += load4(a.bias + g * a.bias_group + n, left);
+    }
+    if (a.relu) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = v[r] < 0.f ? 0.f : v[r];   // NaN stays
+    }
+  } else if (a.sum) {
+    float* sum = a.sum + row * a.N + n;
+    if (!a.first) v += load4(sum, left);
+    if (!a.last) {
+      store4(sum, v, left);
+      return;
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    if (r >= left) break;
+    const float y = v[r];
+    const bool keep = STORE || !a.X || (float)static_cast<const T*>(a.X)[row * a.ldx + n + r] > 0.f;
+    static_cast<T*>(a.C)[row * a.ldc + n + r] = (T)(keep ? y : 0.f);
+  }
+}
+
 using Large = Shape<2, 4, 8, 4, 1, 128>;    // 256 x 256, 512 threads
 using Middle = Shape<2, 2, 4, 4, 1, 128>;   // 128 x 128
 using Narrow = Shape<4, 1, 2, 4, 1, 128>;   // 128 x 64
@@ -557,7 +629,7 @@ using Small = Shape<2, 2, 2, 2, 2, 128>;    // 64 x 64
 template <typename T, class S, bool COLUMNS, int EPI>
 hipError_t launch(const RowArgs& a, hipStream_t s) {
   // blocks that share the tiles: as many as run at once
-  const int tiles = a.row_tiles * a.col_tiles, most = a.cus * S::kBlocks;
+  const int tiles = a.row_tiles * a.col_tiles * (EPI == kPartial ? a.splits : 1), most = a.cus * S::kBlocks;
   hipLaunchKernelGGL((rows_kernel<T, S, COLUMNS, EPI>), dim3((unsigned)(tiles < most ? tiles : most)), dim3(S::NT), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && EPI == kStats && a.col_tiles > 1) {
@@ -575,11 +647,20 @@ hipError_t launch_shape(const RowArgs& a, int shape, hipStream_t s) {
     default: return launch<T, Small, COLUMNS, EPI>(a, s);
   }
 }
+template <typename T, bool COLUMNS>
+hipError_t launch_split(const RowArgs& a, int shape, hipStream_t s) {
+  hipError_t e = shape == 1 ? launch<T, Middle, COLUMNS, kPartial>(a, s) : launch<T, Small, COLUMNS, kPartial>(a, s);
+  if (e != hipSuccess) return e;
+  const int64_t quads = (int64_t)a.n * ((a.N + 3) / 4);
+  hipLaunchKernelGGL((join_k_kernel<T, !COLUMNS>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
 template <typename T>
 hipError_t launch_type(const RowArgs& a, int shape, int epilogue, hipStream_t s) {
   switch (epilogue) {
-    case kStore: return launch_shape<T, false, kStore>(a, shape, s);
-    case kStoreInput: return launch_shape<T, true, kStoreInput>(a, shape, s);
+    case kStore: return a.splits > 1 ? launch_split<T, false>(a, shape, s) : launch_shape<T, false, kStore>(a, shape, s);
+    case kStoreInput:
+      return a.splits > 1 ? launch_split<T, true>(a, shape, s) : launch_shape<T, true, kStoreInput>(a, shape, s);
     case kStats: return launch_shape<T, false, kStats>(a, shape, s);
     default: return launch_shape<T, false, kGradLogits>(a, shape, s);
   }
@@ -587,20 +668,47 @@ hipError_t launch_type(const RowArgs& a, int shape, int epilogue, hipStream_t s)
 
 }  // namespace
 
-RowPlan plan_rows(int dtype, int64_t n, int64_t G, int64_t N, int cus) {
+// The shape with the least time: the rounds that its tiles take, each of as many
+// stages as k has and of an epilogue. A stage takes kStageUs where the card is
+// full of such blocks (measured: 8192 rows, 4096 x 4096), its share of that with
+// fewer blocks on a CU, and kAlone at least (a block by itself waits for its loads). Several runs of k, joined by a second
+// kernel, where few tiles would leave the card empty.
+RowPlan plan_rows(int dtype, int64_t n, int64_t G, int64_t N, int64_t K, int cus, bool may_split) {
   static const int bm[] = {Large::BM, Middle::BM, Narrow::BM, Small::BM};
   static const int bn[] = {Large::BN, Middle::BN, Narrow::BN, Small::BN};
-  auto tiles = [&](int s) { return (n / bm[s] + G) * ((N + bn[s] - 1) / bn[s]); };
-  int s = 3;
-  if (N <= Narrow::BN && n >= 64 * cus) s = 2;
-  else if (N > Narrow::BN && tiles(0) >= cus && n >= 256 * G) s = 0;
-  else if (N > Narrow::BN && tiles(1) >= cus && n >= 128 * G) s = 1;
-  (void)dtype;
-  RowPlan p;
-  p.shape = s;
-  p.row_tiles = (n + bm[s] - 1) / bm[s] + (G > 1 ? G - 1 : 0);
-  p.col_tiles = (N + bn[s] - 1) / bn[s];
-  return p;
+  static const int per_cu[] = {Large::kBlocks, Middle::kBlocks, Narrow::kBlocks, Small::kBlocks};
+  static const double kStageUs[2][4] = {{10.0, 5.0, 4.2, 3.3}, {2.0, 1.35, 1.2, 1.2}};
+  static const double kEpilogueUs[4] = {6.0, 4.0, 3.0, 2.5};
+  constexpr double kAlone = 0.7, kJoin = 8.0;
+  const bool half = dtype == IM_BF16;
+  const int64_t stage = 128 / (half ? 2 : 4);
+  RowPlan best = {};
+  double least = 0;
+  for (int s = 0; s < 4; ++s) {
+    RowPlan p;
+    p.shape = s;
+    p.row_tiles = (n + bm[s] - 1) / bm[s] + (G > 1 ? G - 1 : 0);
+    p.col_tiles = (N + bn[s] - 1) / bn[s];
+    const int64_t steps = (K + stage - 1) / stage, slots = (int64_t)cus * per_cu[s];
+    // ragged groups: about half of the tiles that there may be at most
+    const double tiles = (G > 1 ? (double)n / bm[s] + 0.5 * (double)(G < n ? G : n) + 0.5 : (double)p.row_tiles) * p.col_tiles;
+    for (int64_t splits = 1; splits <= 64; splits *= 2) {
+      if (splits > 1 && (!may_split || s == 0 || s == 2 || steps < 4 * splits || tiles * splits > 2 * slots)) break;
+      const int64_t each = (steps + splits - 1) / splits;
+      p.splits = (steps + each - 1) / each;
+      p.split_k = each * stage;
+      const double fill = tiles * splits / slots, rounds = fill < 1 ? 1 : (fill < 8 ? (double)(int64_t)(fill + 0.999) : fill);
+      // blocks that share a CU
+      const double beside = fill < 1 ? (double)(int64_t)(fill * per_cu[s] + 0.999) / per_cu[s] : 1;
+      const double full = kStageUs[half][s] * beside, us = rounds * (each * (full > kAlone ? full : kAlone) + kEpilogueUs[s]) +
+                        (p.splits > 1 ? kJoin + (double)p.splits * n * N * 8 / 3e6 : 0.0);
+      if ((s == 0 && splits == 1) || us < least) {
+        best = p;
+        least = us;
+      }
+    }
+  }
+  return best;
 }
 
 int rows_per_tile(int shape) {

@@ -1,8 +1,11 @@
-// Sums over rows: the gradients of weights and biases. The rows of a group are
-// cut into chunks, so that a few small matrices over many rows still fill the
-// card; a group of one chunk stores its gradient at once, the others' chunks
-// are joined in their order by a second kernel (no atomics: the same bits each
-// time).
+// Sums over rows: the gradients of weights and biases. The groups' rows, cut into
+// granules, are one line; `parts` equal runs of it are taken by as many blocks
+// for every tile of the gradient, so that one small matrix over many rows and
+// many ragged groups alike fill the card, and the blocks of a run read the same
+// rows at the same time. A group within a run is stored at once; of one that a
+// run's end cuts each block keeps its piece (at most two a block: where its run
+// begins and where it ends), and a second kernel adds the pieces in their order
+// (no atomics: the same bits each time).
 #include "learn_internal.h"
 #include "learn_tile.h"
 
@@ -26,99 +29,169 @@ __device__ __forceinline__ void store_some(T* p, f32x4 v, int left) {
   }
 }
 
+// How the parts cut the line of granules.
+struct Line {
+  int64_t units;
+  int64_t parts;   // those that are not empty
+  __device__ __forceinline__ int64_t begin(int64_t p) const { return p * units / parts; }
+  // the part that granule u falls to
+  __device__ __forceinline__ int64_t part_of(int64_t u) const {
+    int64_t p = u * parts / units;
+    while (p + 1 < parts && begin(p + 1) <= u) ++p;
+    while (begin(p) > u) --p;
+    return p;
+  }
+};
+
 template <typename T, class S>
 __global__ __launch_bounds__(S::NT, S::MI * S::NJ >= 32 ? 2 : 3) void sums_kernel(const SumArgs a) {
   using P = ColTile<T, S::BM, S::NT, S::D, S::SB>;
   using Q = ColTile<T, S::BN, S::NT, S::D, S::SB>;
   using Product = Sum<T, S, P, Q, true>;
   __shared__ __attribute__((aligned(16))) char lds[2 * Product::kBuf];
-  // the tiles of a chunk follow one another, so that they share its rows in an XCD's L2
-  int chunk, tile;
+  __shared__ Groups groups;
+  groups.init(a.offsets, a.G, a.n, a.granule);
+  __syncthreads();
+  if (groups.total < 0) {
+    if (blockIdx.x == 0 && threadIdx.x == 0 && a.error) atomicOr(a.error, IM_ERR_COUNT);
+    return;
+  }
+  const int tiles = a.row_tiles * a.col_tiles;
+  Line line;
+  line.units = groups.total;
+  line.parts = a.parts < groups.total ? a.parts : groups.total;
+  // the tiles of a part follow one another on one XCD: they share its rows in the L2
+  int tile;
+  int64_t run;
   {
-    const int tiles = a.row_tiles * a.col_tiles, total = a.chunks * tiles, each = total / 8, more = total % 8;
-    const int x = blockIdx.x % 8, at = x * each + (x < more ? x : more) + (int)blockIdx.x / 8;
-    chunk = at / tiles;
+    const int total = (int)line.parts * tiles, each = total / 8, more = total % 8, x = blockIdx.x % 8;
+    if ((int)blockIdx.x >= total) return;
+    const int at = x * each + (x < more ? x : more) + (int)blockIdx.x / 8;
+    run = at / tiles;
     tile = at % tiles;
   }
-  const int rt = tile / a.col_tiles, ct = tile % a.col_tiles;
-  Part part;
-  bool bad;
-  const bool found = find_part(a.offsets, a.G, a.n, a.chunk, chunk, part, bad);
-  if (bad && blockIdx.x == 0 && threadIdx.x == 0 && a.error) atomicOr(a.error, IM_ERR_COUNT);
-  if (!found) return;
+  const int begin = (int)line.begin(run), end = (int)line.begin(run + 1);
+  for (int u = begin; u < end;) {
+    int g, lo, hi;
+    groups.find(a.offsets, a.G, a.n, a.granule, u, g, lo, hi);
+    const int first = __builtin_amdgcn_readfirstlane(groups.start[g]);
+    const int count = __builtin_amdgcn_readfirstlane(groups.start[g + 1]) - first;
+    const int k = u - first, length = end - u < count - k ? end - u : count - k;
+    const int rows1 = a.offsets ? a.offsets[g + 1] : a.n;
+    hi = rows1 - lo > (int64_t)length * a.granule ? lo + length * a.granule : rows1;
 
-  const int m_first = rt * S::BM, n_first = ct * S::BN, rows = part.hi - part.lo;
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, wm = wave / S::WN, wn = wave % S::WN;
-  const bool bias = a.db && ct == 0 && wn == 0;
-  // rows to leave out are looked at one by one only where the chunk has any
-  const uint8_t* live = nullptr;
-  if (a.live) {
-    int out = 0;
-    for (int i = part.lo + (int)threadIdx.x; i < part.hi; i += S::NT) out |= !a.live[i];
-    if (__syncthreads_or(out)) live = a.live;
-  }
-  Product x;
-  x.lds = lds;
-  x.steps = (rows + P::kStage - 1) / P::kStage;
-  x.alone = bias;
-  x.p.init(static_cast<const T*>(a.P), a.ldp, m_first, a.M, part.lo, part.hi, (int)threadIdx.x);
-  x.q.init(static_cast<const T*>(a.Q), a.ldq, n_first, a.N, part.lo, part.hi, (int)threadIdx.x, live);
-  x.begin();   // a run of rows is not empty
-  x.first_stage();
-  x.run();
-  auto& acc = x.acc;
-  auto& sum = x.sum;
-
-  const bool only = part.count == 1;
-  float* to = only ? nullptr : a.part + (int64_t)chunk * a.part_width;
-  T* dW = static_cast<T*>(a.dW) + part.g * a.w_group;
-#pragma unroll
-  for (int i = 0; i < S::MI; ++i) {
-    const int m = m_first + (wm * S::MI + i) * 16 + lane % 16;
+    const int rt = tile / a.col_tiles, ct = tile % a.col_tiles;
+    const int m_first = rt * S::BM, n_first = ct * S::BN, tid = fresh_thread();
+    const int lane = tid % 64, wave = tid / 64, wm = wave / S::WN, wn = wave % S::WN;
+    const bool bias = a.db && ct == 0 && wn == 0;
+    // rows to leave out are looked at one by one only where there are any
+    const uint8_t* live = nullptr;
+    if (a.live) {
+      int out = 0;
+      for (int i = lo + tid; i < hi; i += S::NT) out |= !a.live[i];
+      if (__syncthreads_or(out)) live = a.live;
+    }
+    Product x;
+    x.lds = lds;
+    x.steps = (hi - lo + P::kStage - 1) / P::kStage;
+    x.alone = bias;
+    x.p.init(static_cast<const T*>(a.P), a.ldp, m_first, a.M, lo, hi, tid);
+    x.q.init(static_cast<const T*>(a.Q), a.ldq, n_first, a.N, lo, hi, tid, live);
+    x.begin();   // a part of the line is not empty
+    x.first_stage();
+    x.run();
+    auto& acc = x.acc;
     if (bias) {
-      sum[i] += __shfl_xor(sum[i], 16);
-      sum[i] += __shfl_xor(sum[i], 32);
-      if (lane < 16 && m < a.M) (only ? a.db + (int64_t)part.g * a.M : to + a.db_at)[m] = sum[i];
-    }
-    if (m >= a.M) continue;
-    if (!a.dW) continue;
 #pragma unroll
-    for (int j = 0; j < S::NJ; ++j) {
-      const int n = n_first + (wn * S::NJ + j) * 16 + (lane / 16) * 4, left = a.N - n;
-      if (left <= 0) continue;
-      if (only) store_some(dW + (int64_t)m * a.N + n, acc[i][j], left);
-      else store_some(to + (int64_t)m * a.N + n, acc[i][j], left);
+      for (int i = 0; i < S::MI; ++i) {
+        x.sum[i] += __shfl_xor(x.sum[i], 16);
+        x.sum[i] += __shfl_xor(x.sum[i], 32);
+      }
     }
+    if (length == count) {
+      T* dW = static_cast<T*>(a.dW) + g * a.w_group;
+#pragma unroll
+      for (int i = 0; i < S::MI; ++i) {
+        const int m = m_first + (wm * S::MI + i) * 16 + lane % 16;
+        if (m >= a.M) continue;
+        if (bias && lane < 16) a.db[(int64_t)g * a.M + m] = x.sum[i];
+        if (!a.dW) continue;
+#pragma unroll
+        for (int j = 0; j < S::NJ; ++j) {
+          const int n = n_first + (wn * S::NJ + j) * 16 + (lane / 16) * 4, left = a.N - n;
+          if (left > 0) store_some(dW + (int64_t)m * a.N + n, acc[i][j], left);
+        }
+      }
+    } else {   // as the registers lie
+      float* to = a.part + ((2 * run + (u == begin ? 0 : 1)) * tiles + tile) * (S::BM * S::BN + S::BM);
+#pragma unroll
+      for (int i = 0; i < S::MI; ++i) {
+#pragma unroll
+        for (int j = 0; j < S::NJ; ++j) *reinterpret_cast<f32x4*>(to + ((i * S::NJ + j) * S::NT + tid) * 4) = acc[i][j];
+        if (bias && lane < 16) to[S::BM * S::BN + (wm * S::MI + i) * 16 + lane] = x.sum[i];
+      }
+    }
+    u += length;
   }
 }
 
-// Joins the chunks of the groups that have none (zeros) or several. A thread
-// takes four neighbouring elements.
-template <typename T>
-__global__ __launch_bounds__(256) void join_chunks_kernel(const SumArgs a) {
-  Part part;
-  const int g = blockIdx.y;
-  if (!find_group(a.offsets, a.G, a.n, a.chunk, g, part) || part.count == 1) return;
-  const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, mn = (int64_t)a.M * a.N;
-  if (e >= a.db_at + a.M) return;
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  const f32x4* from = reinterpret_cast<const f32x4*>(a.part + part.before * a.part_width + e);
-  const int64_t step = a.part_width / 4;
-  int c = 0;
-  for (; c + 4 <= part.count; c += 4) {
-    const f32x4 x0 = from[c * step], x1 = from[(c + 1) * step], x2 = from[(c + 2) * step], x3 = from[(c + 3) * step];
-    v += x0;
-    v += x1;
-    v += x2;
-    v += x3;
+// Adds the pieces of the groups that several parts cut, and clears the gradient
+// of empty groups. `share` threads (a power of two) go through a tile's pieces
+// for four neighbouring elements, and add up in a fixed order.
+template <typename T, class S>
+__global__ __launch_bounds__(256) void join_pieces_kernel(const SumArgs a, int share) {
+  __shared__ f32x4 sums[256];
+  constexpr int kQuads = (S::BM * S::BN + S::BM) / 4, kTile = S::BM * S::BN / 4;
+  const int tiles = a.row_tiles * a.col_tiles, g = blockIdx.z, tile = blockIdx.y;
+  // all groups' granules, and this group's place among them
+  Part all, part;
+  Line line;
+  if (a.offsets) {
+    if (!find_group(a.offsets, a.G, a.n, a.granule, a.G - 1, all) || !find_group(a.offsets, a.G, a.n, a.granule, g, part))
+      return;
+    line.units = all.before + all.count;
+  } else {
+    find_group(nullptr, 1, a.n, a.granule, 0, part);
+    line.units = part.count;
   }
-  for (; c < part.count; ++c) v += from[c * step];
-  if (e < a.db_at) {
-    const int64_t left = mn - e;
-    if (a.dW && left > 0) store_some(static_cast<T*>(a.dW) + g * a.w_group + e, v, left < 4 ? (int)left : 4);
-  } else if (a.db) {
-    const int64_t m = e - a.db_at, left = a.M - m;
-    store_some(a.db + (int64_t)g * a.M + m, v, left < 4 ? (int)left : 4);
+  line.parts = a.parts < line.units ? a.parts : line.units;
+  const int64_t first = part.before;
+  int p0 = 0, p1 = -1, from = 0;   // its parts; 1: the first of them begins in a group before it
+  if (part.count > 0) {
+    p0 = (int)line.part_of(first);
+    p1 = (int)line.part_of(first + part.count - 1);
+    if (p0 == p1) return;   // stored already
+    from = line.begin(p0) >= first ? 0 : 1;
+  }
+  const int wide = 256 / share, at = (int)threadIdx.x % wide, turn = threadIdx.x / wide;
+  const int rt = tile / a.col_tiles, ct = tile % a.col_tiles;
+  for (int q0 = blockIdx.x * wide; q0 < kQuads; q0 += gridDim.x * wide) {
+    const int q = q0 + at;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    const bool in = q < kTile ? a.dW != nullptr : (q < kQuads && a.db && ct == 0);
+    if (in) {
+#pragma unroll 4
+      for (int p = p0 + turn; p <= p1; p += share)
+        v += *reinterpret_cast<const f32x4*>(
+            a.part + ((2 * p + (p == p0 ? from : 0)) * (int64_t)tiles + tile) * (S::BM * S::BN + S::BM) + (int64_t)q * 4);
+    }
+    if (share > 1) {
+      __syncthreads();
+      sums[threadIdx.x] = v;
+      __syncthreads();
+      for (int t = 1; t < share; ++t) v += sums[(turn == 0 ? t * wide : 0) + at];
+    }
+    if (turn != 0 || !in) continue;
+    if (q < kTile) {   // (i, j, thread) as the registers lay
+      const int tid = q % S::NT, i = q / S::NT / S::NJ, j = q / S::NT % S::NJ;
+      const int lane = tid % 64, wave = tid / 64, wm = wave / S::WN, wn = wave % S::WN;
+      const int m = rt * S::BM + (wm * S::MI + i) * 16 + lane % 16;
+      const int n = ct * S::BN + (wn * S::NJ + j) * 16 + (lane / 16) * 4, left = a.N - n;
+      if (m < a.M && left > 0) store_some(static_cast<T*>(a.dW) + g * a.w_group + (int64_t)m * a.N + n, v, left);
+    } else {
+      const int m = rt * S::BM + (q - kTile) * 4, left = a.M - m;
+      if (left > 0) store_some(a.db + (int64_t)g * a.M + m, v, left);
+    }
   }
 }
 
@@ -152,14 +225,20 @@ using Small = Shape<2, 2, 2, 2, 4, 64>;    // 64 x 64
 
 template <typename T, class S>
 hipError_t launch(const SumArgs& a, hipStream_t s) {
-  if (a.chunks > 0) {
-    hipLaunchKernelGGL((sums_kernel<T, S>), dim3((unsigned)(a.chunks * a.row_tiles * a.col_tiles)), dim3(S::NT), 0, s, a);
+  const int tiles = a.row_tiles * a.col_tiles;
+  if (a.parts > 0) {
+    hipLaunchKernelGGL((sums_kernel<T, S>), dim3((unsigned)(a.parts * tiles)), dim3(S::NT), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (!a.offsets && a.chunks == 1) return hipSuccess;   // one group of one chunk: stored already
-  const int64_t quads = (a.db_at + a.M + 3) / 4;
-  hipLaunchKernelGGL(join_chunks_kernel<T>, dim3((unsigned)((quads + 255) / 256), (unsigned)a.G), dim3(256), 0, s, a);
+  if (!a.offsets && a.parts == 1) return hipSuccess;   // one group in one part: stored already
+  int share = 1;
+  while (share < 16 && share * 2 * a.G <= a.parts) share *= 2;
+  // blocks for a tile: some thousands in all
+  const int quads = (S::BM * S::BN + S::BM) / 4, wide = 256 / share, most = (quads + wide - 1) / wide;
+  const int64_t each = 4096 / ((int64_t)tiles * a.G) + 1;
+  hipLaunchKernelGGL((join_pieces_kernel<T, S>), dim3((unsigned)(each < most ? each : most), (unsigned)tiles, (unsigned)a.G),
+                     dim3(256), 0, s, a, share);
   return hipGetLastError();
 }
 template <typename T>
@@ -175,21 +254,45 @@ hipError_t launch_type(const SumArgs& a, int shape, hipStream_t s) {
 
 int rows_per_sum(int shape) { return shape == 0 ? Large::BM : (shape == 1 ? Middle::BM : Small::BM); }
 
+// Shape and parts are those with the least of: the time of the rounds that the
+// blocks take, at the rate that the shape reaches where it fills the card (8192
+// rows, 4096 x 4096: 1.0, 0.8 and 0.45 PFLOP/s in bf16, near 0.11 each in fp32),
+// and that of writing and reading the pieces. A part takes kLeast granules at
+// least: fewer cost more to join than to sum.
 SumPlan plan_sums(int dtype, int64_t n, int64_t G, int64_t M, int64_t N, int cus) {
-  SumPlan p;
-  const int64_t least = M < N ? M : N;
-  p.shape = least > 128 ? 0 : (least > 64 ? 1 : 2);
-  const int b = p.shape == 0 ? Large::BM : (p.shape == 1 ? Middle::BM : Small::BM);
-  const int per_cu = p.shape == 0 ? 1 : (p.shape == 1 ? 2 : 4);
-  p.row_tiles = (M + b - 1) / b;
-  p.col_tiles = (N + b - 1) / b;
-  const int64_t want = (2 * per_cu * cus + p.row_tiles * p.col_tiles - 1) / (p.row_tiles * p.col_tiles);
-  const int64_t stage = kHalf / (dtype == IM_BF16 ? 2 : 4);
-  int64_t chunk = (n + want - 1) / want;
-  if (chunk < 8 * stage) chunk = 8 * stage;
-  p.chunk = (chunk + stage - 1) / stage * stage;
-  p.chunks = n > 0 ? (n + p.chunk - 1) / p.chunk + G - 1 : 0;
-  return p;
+  static const int tile[] = {Large::BM, Middle::BM, Small::BM}, per_cu[] = {1, 2, 4};
+  static const double rate[2][3] = {{1.1e14, 1.05e14, 0.9e14}, {1.0e15, 0.8e15, 0.45e15}};
+  constexpr int64_t kLeast = 4;
+  const bool half = dtype == IM_BF16;
+  SumPlan best = {};
+  double least = 0;
+  for (int s = 0; s < 3; ++s) {
+    SumPlan p;
+    p.shape = s;
+    p.row_tiles = (M + tile[s] - 1) / tile[s];
+    p.col_tiles = (N + tile[s] - 1) / tile[s];
+    p.granule = half ? 64 : 32;
+    p.piece = (int64_t)tile[s] * tile[s] + tile[s];
+    const int64_t tiles = p.row_tiles * p.col_tiles, slots = (int64_t)cus * per_cu[s];
+    const int64_t granules = n > 0 ? (n + p.granule - 1) / p.granule + (G > 1 ? G - 1 : 0) : 0;
+    const int64_t most = granules < 1 ? 0 : (granules + kLeast - 1) / kLeast;
+    // whole rounds of the card: 1, 2, 3 and 4 of them, as near as the tiles allow
+    for (int round = 0; round <= 4; ++round) {
+      int64_t parts = round == 0 ? 1 : round * slots / tiles;
+      if (parts < 1) parts = 1;
+      // many small groups: a part for a handful of granules serves them side by side
+      if (parts > most) parts = most;
+      p.parts = parts;
+      const double rounds = parts > 0 ? (double)((parts * tiles + slots - 1) / slots) : 0;
+      const double sum = parts > 0 ? rounds * 2.0 * ((double)granules * p.granule / parts) * tile[s] * tile[s] * slots / rate[half][s] : 0;
+      const double join = parts > 1 ? 2.0 * 2 * parts * tiles * p.piece * 4 / 4e12 + 4e-6 : 0;
+      if ((s == 0 && round == 0) || sum + join < least) {
+        best = p;
+        least = sum + join;
+      }
+    }
+  }
+  return best;
 }
 
 hipError_t launch_sums(const SumArgs& a, int dtype, int shape, hipStream_t s) {

@@ -204,8 +204,9 @@ def im_linear_forward(x, W, b, y, offsets=None, relu=False, workspace=None, erro
     L = _learn or load_learn()
     d = ImLinearDesc(G, n, k, m, kind, 1 if relu else 0, 0, 0, ld_x, ld_y, 0)
     with _On(dev.index):
+        ws, at, size = _workspace(L.im_linear_workspace, d, (0, dev.index, G, n, k, m, kind), 0, workspace, dev, stream)
         _done(L.im_linear_forward(ctypes.byref(d), _offsets(offsets, G, dev), x.data_ptr(), W.data_ptr(),
-                                  _flat(b, "b", f32, dev, G * m), y.data_ptr(), None, 0,
+                                  _flat(b, "b", f32, dev, G * m), y.data_ptr(), at, size,
                                   _flat(error, "error", i32, dev, 1), _stream(stream)))
 
 
@@ -229,7 +230,7 @@ def im_linear_backward(dy, x, W, dx=None, dW=None, db=None, offsets=None, relu_i
     L = _learn or load_learn()
     d = ImLinearDesc(G, n, k, m, kind, 0, 1 if relu_in else 0, 0, ld_x, ld_y, ld_dx)
     with _On(dev.index):
-        ws, at, size = _workspace(L.im_linear_workspace, d, (0, dev.index, G, n, k, m, kind), 1, workspace, dev, stream)
+        ws, at, size = _workspace(L.im_linear_workspace, d, (1, dev.index, G, n, k, m, kind), 1, workspace, dev, stream)
         _done(L.im_linear_backward(ctypes.byref(d), _offsets(offsets, G, dev), dy.data_ptr(), x.data_ptr(),
                                    W.data_ptr(), None if dx is None else dx.data_ptr(),
                                    _flat(dW, "dW", dt, dev, G * m * k), _flat(db, "db", f32, dev, G * m), at, size,
@@ -261,7 +262,7 @@ def im_head_forward(h, W, b, target, logp, entropy=None, lse=None, valid=None, o
     L = _learn or load_learn()
     d = ImHeadDesc(G, n, k, V, kind, 0, 0, 0, ld, 0)
     with _On(dev.index):
-        ws, at, size = _workspace(L.im_head_workspace, d, (1, dev.index, G, n, k, V, kind), 0, workspace, dev, stream)
+        ws, at, size = _workspace(L.im_head_workspace, d, (2, dev.index, G, n, k, V, kind), 0, workspace, dev, stream)
         _done(L.im_head_forward(ctypes.byref(d), _offsets(offsets, G, dev), h.data_ptr(), W.data_ptr(), pb, pv, pt,
                                 _flat(logp, "logp", f32, dev, n), _flat(entropy, "entropy", f32, dev, n),
                                 _flat(lse, "lse", f32, dev, n), at, size, _flat(error, "error", i32, dev, 1),
@@ -282,7 +283,7 @@ def im_head_backward(h, W, b, target, lse, dlogp, dh=None, dW=None, db=None, val
     L = _learn or load_learn()
     d = ImHeadDesc(G, n, k, V, kind, 1 if relu_in else 0, 0, 0, ld, ld_dh)
     with _On(dev.index):
-        ws, at, size = _workspace(L.im_head_workspace, d, (2, dev.index, G, n, k, V, kind), 1, workspace, dev, stream)
+        ws, at, size = _workspace(L.im_head_workspace, d, (3, dev.index, G, n, k, V, kind), 1, workspace, dev, stream)
         _done(L.im_head_backward(ctypes.byref(d), _offsets(offsets, G, dev), h.data_ptr(), W.data_ptr(), pb, pv, pt,
                                  _flat(lse, "lse", f32, dev, n), _flat(entropy, "entropy", f32, dev, n),
                                  _flat(dlogp, "dlogp", f32, dev, n), _flat(dentropy, "dentropy", f32, dev, n),
