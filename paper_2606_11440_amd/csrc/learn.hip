@@ -114,6 +114,7 @@ im_status check_linear(const im_linear_desc* d) {
 struct SumWork {
   SumPlan plan;
   float* part;
+  int4* cuts;
   int64_t bytes;
 };
 // Plan and workspace of the sums over rows.
@@ -121,7 +122,10 @@ SumWork sum_work(int dtype, int64_t n, int64_t G, int64_t M, int64_t N, void* ws
   SumWork w;
   w.plan = plan_sums(dtype, n, G, M, N, compute_units());
   Sections s(ws);
-  w.part = s.take<float>(w.plan.parts > 1 || G > 1 ? 2 * w.plan.parts * w.plan.row_tiles * w.plan.col_tiles * w.plan.piece : 0);
+  const bool joined = w.plan.parts > 1 || (w.plan.parts == 1 && G > 1);
+  w.part = s.take<float>(joined ? 2 * w.plan.parts * w.plan.row_tiles * w.plan.col_tiles * w.plan.piece : 0);
+  w.cuts = s.take<int4>(joined ? G : 0);
+  if (!joined) w.cuts = nullptr;
   w.bytes = s.used;
   return w;
 }
@@ -267,6 +271,7 @@ im_status im_linear_backward(const im_linear_desc* d, const int32_t* offsets, co
     a.w_group = (int64_t)d->in_dim * d->out_dim;
     a.db = db;
     a.part = w.sums.part;
+    a.cuts = w.sums.cuts;
     a.granule = (int32_t)w.sums.plan.granule;
     a.parts = (int32_t)w.sums.plan.parts;
     a.row_tiles = (int32_t)w.sums.plan.row_tiles;
@@ -482,6 +487,7 @@ im_status im_head_backward(const im_head_desc* d, const int32_t* offsets, const 
       a.dW = static_cast<char*>(dW) + c0 * d->dim * e;
       a.w_group = V * d->dim;
       a.part = w.sums.part;
+      a.cuts = w.sums.cuts;
       a.granule = (int32_t)w.sums.plan.granule;
       a.parts = (int32_t)w.sums.plan.parts;
       const int64_t tile = rows_per_sum(w.sums.plan.shape);

@@ -69,6 +69,7 @@ struct SumArgs {
   int64_t w_group;
   float* db;                  // [G x M] or NULL
   float* part;                // [2 parts][tiles][tile and its rows]: pieces of groups that parts cut
+  int4* cuts;                 // [G] {first part, last part, the first one's piece, 0}, or NULL (no rows)
   int32_t granule, parts;     // rows of a granule; parts of the line of granules
   int32_t row_tiles, col_tiles;
   int32_t* error;

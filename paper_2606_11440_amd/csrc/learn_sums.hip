@@ -54,12 +54,34 @@ __global__ __launch_bounds__(S::NT, S::MI * S::NJ >= 32 ? 2 : 3) void sums_kerne
   __syncthreads();
   if (groups.total < 0) {
     if (blockIdx.x == 0 && threadIdx.x == 0 && a.error) atomicOr(a.error, IM_ERR_COUNT);
+    if (blockIdx.x == 0 && a.cuts)   // nothing to join
+      for (int g = threadIdx.x; g < a.G; g += S::NT) a.cuts[g] = int4{0, 0, 0, 0};
     return;
   }
   const int tiles = a.row_tiles * a.col_tiles;
   Line line;
   line.units = groups.total;
   line.parts = a.parts < groups.total ? a.parts : groups.total;
+  if (blockIdx.x == 0 && a.cuts)   // where the parts cut the groups, for the kernel that joins
+    for (int g = threadIdx.x; g < a.G; g += S::NT) {
+      const int first = groups.start[g], last = groups.start[g + 1] - 1;
+      int4 cut = {0, -1, 0, 0};
+      if (last >= first) {
+        cut.x = (int)line.part_of(first);
+        cut.y = (int)line.part_of(last);
+        cut.z = line.begin(cut.x) >= first ? 0 : 1;
+      }
+      a.cuts[g] = cut;
+    }
+  if (a.G == 1 && a.parts == 1 && groups.total == 0) {   // an empty group: zeros
+    const int rt = blockIdx.x / a.col_tiles, ct = blockIdx.x % a.col_tiles;
+    for (int e = threadIdx.x; e < S::BM * S::BN; e += S::NT) {
+      const int m = rt * S::BM + e / S::BN, n = ct * S::BN + e % S::BN;
+      if (a.dW && m < a.M && n < a.N) static_cast<T*>(a.dW)[(int64_t)m * a.N + n] = T(0.f);
+    }
+    for (int m = rt * S::BM + threadIdx.x; a.db && ct == 0 && m < a.M && m < (rt + 1) * S::BM; m += S::NT) a.db[m] = 0.f;
+    return;
+  }
   // the tiles of a part follow one another on one XCD: they share its rows in the L2
   int tile;
   int64_t run;
@@ -109,18 +131,24 @@ __global__ __launch_bounds__(S::NT, S::MI * S::NJ >= 32 ? 2 : 3) void sums_kerne
       }
     }
     if (length == count) {
-      T* dW = static_cast<T*>(a.dW) + g * a.w_group;
+      if (bias) {
 #pragma unroll
-      for (int i = 0; i < S::MI; ++i) {
-        const int m = m_first + (wm * S::MI + i) * 16 + lane % 16;
-        if (m >= a.M) continue;
-        if (bias && lane < 16) a.db[(int64_t)g * a.M + m] = x.sum[i];
-        if (!a.dW) continue;
-#pragma unroll
-        for (int j = 0; j < S::NJ; ++j) {
-          const int n = n_first + (wn * S::NJ + j) * 16 + (lane / 16) * 4, left = a.N - n;
-          if (left > 0) store_some(dW + (int64_t)m * a.N + n, acc[i][j], left);
+        for (int i = 0; i < S::MI; ++i) {
+          const int m = m_first + (wm * S::MI + i) * 16 + lane;
+          if (lane < 16 && m < a.M) a.db[(int64_t)g * a.M + m] = x.sum[i];
         }
+      }
+      if (a.dW) {
+        T* const to = static_cast<T*>(a.dW) + g * a.w_group + (int64_t)m_first * a.N + n_first;
+        Out<T, S, (int)sizeof(lds)>::run(lds, tid, [&](int i, int j) { return acc[i][j]; }, [] {},
+                                         [&](int, int m, int c, u32x4 v) {
+          const int left = a.N - n_first - c;
+          if (m_first + m >= a.M || left <= 0) return;
+          T* const p = to + (int64_t)m * a.N + c;
+          if (left >= kVec<T>) *reinterpret_cast<u32x4_any*>(p) = v;
+          else store_few(p, v, left);
+        });
+        __syncthreads();   // the next group's stages take the LDS
       }
     } else {   // as the registers lie
       float* to = a.part + ((2 * run + (u == begin ? 0 : 1)) * tiles + tile) * (S::BM * S::BN + S::BM);
@@ -143,26 +171,9 @@ __global__ __launch_bounds__(256) void join_pieces_kernel(const SumArgs a, int s
   __shared__ f32x4 sums[256];
   constexpr int kQuads = (S::BM * S::BN + S::BM) / 4, kTile = S::BM * S::BN / 4;
   const int tiles = a.row_tiles * a.col_tiles, g = blockIdx.z, tile = blockIdx.y;
-  // all groups' granules, and this group's place among them
-  Part all, part;
-  Line line;
-  if (a.offsets) {
-    if (!find_group(a.offsets, a.G, a.n, a.granule, a.G - 1, all) || !find_group(a.offsets, a.G, a.n, a.granule, g, part))
-      return;
-    line.units = all.before + all.count;
-  } else {
-    find_group(nullptr, 1, a.n, a.granule, 0, part);
-    line.units = part.count;
-  }
-  line.parts = a.parts < line.units ? a.parts : line.units;
-  const int64_t first = part.before;
-  int p0 = 0, p1 = -1, from = 0;   // its parts; 1: the first of them begins in a group before it
-  if (part.count > 0) {
-    p0 = (int)line.part_of(first);
-    p1 = (int)line.part_of(first + part.count - 1);
-    if (p0 == p1) return;   // stored already
-    from = line.begin(p0) >= first ? 0 : 1;
-  }
+  const int4 cut = a.cuts ? a.cuts[g] : int4{0, -1, 0, 0};   // no rows at all: zeros
+  const int p0 = cut.x, p1 = cut.y, from = cut.z;   // its parts; 1: the first of them begins in a group before it
+  if (p0 == p1) return;   // stored already
   const int wide = 256 / share, at = (int)threadIdx.x % wide, turn = threadIdx.x / wide;
   const int rt = tile / a.col_tiles, ct = tile % a.col_tiles;
   for (int q0 = blockIdx.x * wide; q0 < kQuads; q0 += gridDim.x * wide) {
@@ -231,7 +242,7 @@ hipError_t launch(const SumArgs& a, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (!a.offsets && a.parts == 1) return hipSuccess;   // one group in one part: stored already
+  if (a.G == 1 && a.parts == 1) return hipSuccess;   // one group in one part: stored already
   int share = 1;
   while (share < 16 && share * 2 * a.G <= a.parts) share *= 2;
   // blocks for a tile: some thousands in all

@@ -374,6 +374,76 @@ struct Sum {
   }
 };
 
+// ---- results ----------------------------------------------------------------
+
+// Passes a block's results, rounded to U, through LDS to 16-byte units of a row.
+// A fragment's own layout would store 32 bytes of 16 rows at a time; here a wave
+// stores whole lines. Unit u of a row lies at u ^ (row % 16), so that neither the
+// fragments' writes nor the units' reads meet in a bank. Where the LDS does not
+// hold the tile it goes in passes.
+//   value(i, j)   the fragment to put, final
+//   after()       called when the first pass is in LDS (one pass: acc is free)
+//   use(k, m, c, unit)   unit k of the thread's: of tile row m, from column c on
+template <typename U, class S, int kLds>
+struct Out {
+  static constexpr int kPitch = S::BN * (int)sizeof(U), kAcross = kPitch / 16;
+  static constexpr int kPasses = S::BM * kPitch <= kLds ? 1 : (S::BM * kPitch <= 2 * kLds ? 2 : 4), kMi = S::MI / kPasses;
+  static constexpr int kUnits = S::WM * kMi * 16 * kAcross / S::NT;   // of a thread, a pass
+  static_assert(S::WM * kMi * 16 * kPitch <= kLds && S::MI % kPasses == 0, "a pass fits");
+  static_assert(S::WM * kMi * 16 * kAcross % S::NT == 0 && S::NT % kAcross == 0, "whole units per thread");
+  static __device__ __forceinline__ int key(int row) { return row & (kAcross < 16 ? kAcross - 1 : 15); }
+
+  static __device__ __forceinline__ int row_of(int pass, int k, int tid) {
+    const int r = tid / kAcross + k * (S::NT / kAcross);
+    return kPasses == 1 ? r : (r / (kMi * 16)) * S::MI * 16 + pass * kMi * 16 + r % (kMi * 16);
+  }
+  static __device__ __forceinline__ int column_of(int tid) { return tid % kAcross * (16 / (int)sizeof(U)); }
+
+  template <class V, class A, class F>
+  static __device__ __forceinline__ void run(char* lds, int tid, V value, A after, F use) {
+    const int lane = tid % 64, wave = tid / 64, wm = wave / S::WN, wn = wave % S::WN, g = lane / 16;
+#pragma unroll
+    for (int pass = 0; pass < kPasses; ++pass) {
+      if (pass) __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kMi; ++i) {
+        const int r = (wm * kMi + i) * 16 + lane % 16;
+#pragma unroll
+        for (int j = 0; j < S::NJ; ++j) {
+          const f32x4 v = value(pass * kMi + i, j);
+          const int at = (wn * S::NJ + j) * 16 + g * 4;
+          char* to = lds + r * kPitch + (((at * (int)sizeof(U) / 16) ^ key(r)) << 4);
+          if constexpr (sizeof(U) == 2) {
+            bf16x4 o;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) o[q] = (__bf16)v[q];
+            *reinterpret_cast<bf16x4*>(to + (g & 1) * 8) = o;
+          } else {
+            *reinterpret_cast<f32x4*>(to) = v;
+          }
+        }
+      }
+      __syncthreads();
+      if (pass == 0) after();
+#pragma unroll
+      for (int k = 0; k < kUnits; ++k) {
+        const int r = tid / kAcross + k * (S::NT / kAcross);
+        use(pass * kUnits + k, row_of(pass, k, tid), column_of(tid),
+            *reinterpret_cast<const u32x4*>(lds + r * kPitch + ((tid % kAcross ^ key(r)) << 4)));
+      }
+    }
+  }
+};
+
+// Some of a unit's values to p (n: how many exist).
+template <typename U>
+__device__ __forceinline__ void store_few(U* p, u32x4 x, int n) {
+  U e[kVec<U>];
+  __builtin_memcpy(e, &x, 16);
+#pragma unroll
+  for (int i = 0; i < kVec<U>; ++i)
+    if (i < n) p[i] = e[i];
+}
 // ---- groups ----------------------------------------------------------------
 
 struct Part {          // a run of `step` rows of a group
