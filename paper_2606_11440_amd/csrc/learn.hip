@@ -586,7 +586,9 @@ im_status im_adamw_create(const im_adamw_tensor* tensors, int32_t n_tensors, int
     o->bits = state_bits;
     o->grad_dtype = grad_dtype;
     o->runs = (int64_t)runs.size();
-    o->blocks = 8 * (int64_t)compute_units();
+    // 2^26 elements, a block a run against blocks that share the runs, 8 a CU: 353 and 367 us
+    // with 32-bit states, 224 and 220 us with 8-bit ones
+    o->blocks = state_bits == 32 ? o->runs : 8 * (int64_t)compute_units();
     const hipStream_t s = (hipStream_t)stream;
     const std::vector<uint32_t> zero(1, 0);
     if (e == hipSuccess && o->runs > 0x7fffffff) e = hipErrorInvalidValue;
