@@ -349,6 +349,27 @@ HeadBackward head_backward(const im_head_desc& d, void* ws) {
   return w;
 }
 
+struct NarrowWork {
+  NarrowPlan plan;
+  float* pieces;
+  int4* cuts;
+  int64_t bytes;
+};
+NarrowWork narrow_work(const im_head_desc& d, void* ws) {
+  NarrowWork w;
+  w.plan = plan_narrow(d.n_rows, d.n_groups, d.dim, d.n_classes, compute_units());
+  Sections s(ws);
+  w.pieces = s.take<float>(2 * w.plan.parts * w.plan.piece);
+  w.cuts = s.take<int4>(w.plan.parts > 0 ? d.n_groups : 0);
+  if (w.plan.parts == 0) w.cuts = nullptr;
+  w.bytes = s.used;
+  return w;
+}
+bool narrow(const im_head_desc& d) { return narrow_supported(d.dtype, d.dim, d.n_classes); }
+int64_t head_backward_bytes(const im_head_desc& d) {
+  return narrow(d) ? narrow_work(d, nullptr).bytes : head_backward(d, nullptr).bytes;
+}
+
 }  // namespace
 
 extern "C" {
@@ -357,7 +378,7 @@ im_status im_head_workspace(const im_head_desc* d, int32_t backward, int64_t* by
   LEARN_OK(check_head(d));
   LEARN_CHECK(bytes, "bytes is NULL");
   LEARN_CHECK(backward == 0 || backward == 1, "backward is 0 or 1");
-  *bytes = d->n_rows == 0 && !backward ? 0 : (backward ? head_backward(*d, nullptr).bytes : head_forward(*d, nullptr).bytes);
+  *bytes = d->n_rows == 0 && !backward ? 0 : (backward ? head_backward_bytes(*d) : head_forward(*d, nullptr).bytes);
   return IM_OK;
 }
 
@@ -413,6 +434,42 @@ im_status im_head_backward(const im_head_desc* d, const int32_t* offsets, const 
                   aligned(target, 4) && aligned(lse, 4) && aligned(entropy, 4) && aligned(dlogp, 4) &&
                   aligned(dentropy, 4) && aligned(db, 4) && aligned(error, 4),
               "a pointer is not aligned to its elements");
+  if (narrow(*d)) {
+    const NarrowWork w = narrow_work(*d, ws);
+    LEARN_OK(check_work(ws, ws_bytes, w.bytes));
+    if (!dh && !dW && !db) return IM_OK;
+    NarrowArgs a = {};
+    a.offsets = offsets;
+    a.G = d->n_groups;
+    a.n = d->n_rows;
+    a.d = d->dim;
+    a.V = d->n_classes;
+    a.words = (d->n_classes + 31) / 32;
+    a.relu_in = d->relu_in;
+    a.h = h;
+    a.ld_h = d->ld_h;
+    a.W = W;
+    a.bias = b;
+    a.valid = valid;
+    a.target = target;
+    a.lse = lse;
+    a.entropy = entropy;
+    a.dlogp = dlogp;
+    a.dentropy = dentropy;
+    a.dh = dh;
+    a.ld_dh = d->ld_dh;
+    a.dW = dW;
+    a.db = db;
+    a.pieces = w.pieces;
+    a.cuts = w.cuts;
+    a.piece = w.plan.piece;
+    a.pitch = w.plan.pitch;
+    a.granule = (int32_t)w.plan.granule;
+    a.parts = (int32_t)w.plan.parts;
+    a.error = error;
+    LEARN_HIP(launch_narrow(a, (hipStream_t)stream));
+    return IM_OK;
+  }
   const HeadBackward w = head_backward(*d, ws);
   LEARN_OK(check_work(ws, ws_bytes, w.bytes));
   LEARN_OK(check_launch(w.logits));

@@ -75,6 +75,34 @@ struct SumArgs {
   int32_t* error;
 };
 
+// The gradient of a narrow head in one pass.
+struct NarrowArgs {
+  const int32_t* offsets;
+  int32_t G, n, d, V, words, relu_in;
+  const void* h;
+  int64_t ld_h;
+  const void* W;
+  const float* bias;
+  const uint32_t* valid;
+  const int32_t* target;
+  const float *lse, *entropy, *dlogp, *dentropy;
+  void* dh;
+  int64_t ld_dh;
+  void* dW;
+  float* db;
+  float* pieces;              // [2 parts][piece]: V rows of `pitch`, then V
+  int4* cuts;                 // [G], or NULL (no rows)
+  int64_t piece, pitch;
+  int32_t granule, parts;
+  int32_t* error;
+};
+struct NarrowPlan {
+  int64_t granule, parts, pitch, piece;
+};
+bool narrow_supported(int dtype, int64_t d, int64_t V);
+NarrowPlan plan_narrow(int64_t n, int64_t G, int64_t d, int64_t V, int cus);
+hipError_t launch_narrow(const NarrowArgs& a, hipStream_t s);
+
 // Tile shape of a row product of n rows in G groups with N columns, and its tiles
 // (row tiles: at most; the groups' sizes are known on the device only).
 struct RowPlan {

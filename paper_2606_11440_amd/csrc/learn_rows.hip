@@ -4,15 +4,13 @@
 #include <type_traits>
 
 #include "learn_internal.h"
+#include "learn_softmax.h"
 #include "learn_tile.h"
 
 namespace im {
 namespace learn {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kLeast = -300.f;   // 2^-300 is 0 in fp32
-__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
 __device__ __forceinline__ f32x4 load4(const float* p, int left) {
   typedef f32x4 any __attribute__((aligned(4)));

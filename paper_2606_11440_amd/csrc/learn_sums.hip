@@ -29,20 +29,6 @@ __device__ __forceinline__ void store_some(T* p, f32x4 v, int left) {
   }
 }
 
-// How the parts cut the line of granules.
-struct Line {
-  int64_t units;
-  int64_t parts;   // those that are not empty
-  __device__ __forceinline__ int64_t begin(int64_t p) const { return p * units / parts; }
-  // the part that granule u falls to
-  __device__ __forceinline__ int64_t part_of(int64_t u) const {
-    int64_t p = u * parts / units;
-    while (p + 1 < parts && begin(p + 1) <= u) ++p;
-    while (begin(p) > u) --p;
-    return p;
-  }
-};
-
 template <typename T, class S>
 __global__ __launch_bounds__(S::NT, S::MI * S::NJ >= 32 ? 2 : 3) void sums_kernel(const SumArgs a) {
   using P = ColTile<T, S::BM, S::NT, S::D, S::SB>;
@@ -63,16 +49,7 @@ __global__ __launch_bounds__(S::NT, S::MI * S::NJ >= 32 ? 2 : 3) void sums_kerne
   line.units = groups.total;
   line.parts = a.parts < groups.total ? a.parts : groups.total;
   if (blockIdx.x == 0 && a.cuts)   // where the parts cut the groups, for the kernel that joins
-    for (int g = threadIdx.x; g < a.G; g += S::NT) {
-      const int first = groups.start[g], last = groups.start[g + 1] - 1;
-      int4 cut = {0, -1, 0, 0};
-      if (last >= first) {
-        cut.x = (int)line.part_of(first);
-        cut.y = (int)line.part_of(last);
-        cut.z = line.begin(cut.x) >= first ? 0 : 1;
-      }
-      a.cuts[g] = cut;
-    }
+    for (int g = threadIdx.x; g < a.G; g += S::NT) a.cuts[g] = line.cut(groups.start[g], groups.start[g + 1]);
   if (a.G == 1 && a.parts == 1 && groups.total == 0) {   // an empty group: zeros
     const int rt = blockIdx.x / a.col_tiles, ct = blockIdx.x % a.col_tiles;
     for (int e = threadIdx.x; e < S::BM * S::BN; e += S::NT) {

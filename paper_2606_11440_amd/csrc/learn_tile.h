@@ -583,6 +583,30 @@ struct Groups {
   }
 };
 
+// How the parts cut the line of granules.
+struct Line {
+  int64_t units;
+  int64_t parts;   // those that are not empty
+  __device__ __forceinline__ int64_t begin(int64_t p) const { return p * units / parts; }
+  // the part that granule u falls to
+  __device__ __forceinline__ int64_t part_of(int64_t u) const {
+    int64_t p = u * parts / units;
+    while (p + 1 < parts && begin(p + 1) <= u) ++p;
+    while (begin(p) > u) --p;
+    return p;
+  }
+  // of granules [first, end): {first part, last part, 1 if the first one begins before them, 0}
+  __device__ __forceinline__ int4 cut(int first, int end) const {
+    int4 c = {0, -1, 0, 0};
+    if (end > first) {
+      c.x = (int)part_of(first);
+      c.y = (int)part_of(end - 1);
+      c.z = begin(c.x) >= first ? 0 : 1;
+    }
+    return c;
+  }
+};
+
 // Tile (row, column) of number `b` of rows x cols tiles: the blocks of an XCD
 // (b % 8) take neighbouring tiles, eight rows of tiles at a time, so that those
 // running together share operands in its L2.
