@@ -138,23 +138,26 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
 
     // a tile's h on its way: thread's unit of rows tid / (8 NW) + 8 i
     u32x4 ahead[kUnits];
-    auto load_h = [&](int t) {
+    auto load_h = [&](int t, auto full) {
       const int tid = fresh_thread(), unit = tid % (NW * 8), u_left = a.d - unit * 8;
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
         const int row = lo + t * kRows + tid / (NW * 8) + i * (NT / (NW * 8));
         const T* const p = H + (int64_t)(row < hi ? row : hi - 1) * a.ld_h + unit * 8;
-        if (a.d >= 8) ahead[i] = u_left > 0 ? load16(p + (u_left < 8 ? u_left - 8 : 0)) : zeros();
+        if constexpr (full) ahead[i] = load16(p);
+        else if (a.d >= 8) ahead[i] = u_left > 0 ? load16(p + (u_left < 8 ? u_left - 8 : 0)) : zeros();
         else ahead[i] = u_left > 0 ? load_few(p, u_left) : zeros();
       }
     };
-    auto store_h = [&](int t) {   // rows that add nothing are zero, whatever they hold
+    auto store_h = [&](int t, auto full) {   // rows that add nothing are zero, whatever they hold
       const int tid = fresh_thread(), unit = tid % (NW * 8), u_left = a.d - unit * 8;
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
         const int row = tid / (NW * 8) + i * (NT / (NW * 8));
         u32x4 v = ahead[i];
-        if (u_left < 8 && u_left > 0 && a.d >= 8) v = keep_last<T>(v, u_left);
+        if constexpr (!full) {
+          if (u_left < 8 && u_left > 0 && a.d >= 8) v = keep_last<T>(v, u_left);
+        }
         if (!info[t & 1][row].live) v = zeros();
         *reinterpret_cast<u32x4*>(h_lds[t & 1] + h_at<NW>(row, unit)) = v;
       }
@@ -196,14 +199,17 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
     };
 
     load_info(0);
-    load_h(0);
+    load_h(0, std::false_type{});
     store_info(0);
     if (tiles > 1) load_info(1);
     __syncthreads();
-    store_h(0);
-    if (tiles > 1) load_h(1);
+    store_h(0, std::false_type{});
+    if (tiles > 1) load_h(1, std::false_type{});
     __syncthreads();
-    for (int t = 0; t < tiles; ++t) {
+    // full: all of the tile's rows and of the waves' columns exist, and two more tiles follow.
+    // Such a tile takes no branch around its stores, so that the wait for the rows that are
+    // on their way leaves the stores behind them alone.
+    auto tile = [&](int t, auto full) {
       const char* const ht = h_lds[t & 1];
       {   // the logits over the wave's columns
         const int lane = fresh_thread() % 64, l16 = lane % 16, g4 = lane / 16;
@@ -223,11 +229,13 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
             *reinterpret_cast<f32x4*>(parts[wave] + z_at(i * 16 + l16, b * 4 + g4)) = z[i][b];
         }
       }
-      if (t + 1 < tiles) store_info(t + 1);
-      if (t + 2 < tiles) load_info(t + 2);
+      if (full || t + 1 < tiles) store_info(t + 1);
       __syncthreads();
-      if (t + 1 < tiles) store_h(t + 1);
-      if (t + 2 < tiles) load_h(t + 2);
+      if (full || t + 1 < tiles) store_h(t + 1, full);
+      if (full || t + 2 < tiles) {
+        load_info(t + 2);
+        load_h(t + 2, full);
+      }
 #pragma unroll
       for (int e = 0; e < kQuads; ++e) {   // dz of four classes of a row
         const int tid = fresh_thread(), quad = tid % 16;
@@ -267,7 +275,7 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
         }
       }
       // dh of the wave's columns, through the wave's own LDS to whole lines
-      if (a.dh) {
+      if (full || a.dh) {
         const int lane = fresh_thread() % 64, l16 = lane % 16, g4 = lane / 16;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -303,13 +311,21 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
           const int row = i * 8 + lane / 8;
           const int64_t at = (int64_t)lo + t * kRows + row;
           const u32x4 v = *reinterpret_cast<const u32x4*>(parts[wave] + dz_at(row, lane % 8));
-          if (at >= hi || left <= 0) continue;
           T* const to = static_cast<T*>(a.dh) + at * a.ld_dh + c;
+          if constexpr (full) {
+            *reinterpret_cast<u32x4_any*>(to) = v;
+            continue;
+          }
+          if (at >= hi || left <= 0) continue;
           if (left >= 8) *reinterpret_cast<u32x4_any*>(to) = v;
           else store_few(to, v, left);
         }
       }
-    }
+    };
+    int t = 0;
+    if (a.d == NW * kSlice && a.dh)
+      for (; t + 2 < tiles; ++t) tile(t, std::true_type{});
+    for (; t < tiles; ++t) tile(t, std::false_type{});
 
     // the group's gradient, or this run's piece of it
     const bool all = length == count;
