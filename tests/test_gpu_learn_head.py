@@ -101,7 +101,8 @@ SHAPES = [  # n, dim, classes, group sizes
     (1, 1, 1, None), (1, 64, 15, None), (2, 5, 2, [1, 1]), (50, 256, 15, None), (64, 64, 64, [64]), (65, 100, 65, [30, 35]),
     (129, 33, 33, [0, 100, 29]), (300, 128, 24, [1] * 100 + [199]), (500, 200, 300, [450]), (1000, 384, 1000, None),
     (257, 72, 4100, [200, 0, 57]), (3, 40, 10007, None), (20000, 64, 15, [7000, 0, 12990]), (40000, 96, 64, [15000, 25000]),
-    (2000, 512, 257, [900, 1100]),
+    (2000, 512, 257, [900, 1100]), (700, 600, 40, [300, 390]), (333, 300, 15, [10, 0, 320]), (9000, 512, 64, [4000, 5000]),
+    (5000, 256, 24, None), (300, 7, 64, [299, 1]), (100, 1030, 9, None),
 ]
 
 

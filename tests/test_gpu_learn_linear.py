@@ -121,6 +121,37 @@ def test_some_gradients(want):
     check_backward(make(500, 100, 70, None, F32, seed=6), relu_in=True, want=want)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,k,m,sizes", [(1, 4096, 200, None), (20, 3000, 130, [5, 0, 15]), (150, 2050, 70, [100]),
+                                         (33, 9000, 20, None)])
+def test_few_rows_and_a_long_sum(n, k, m, sizes, dtype):
+    """The sum is cut into runs that a second kernel joins."""
+    note(f"[long sum] n={n} k={k} m={m} {dtype}")
+    c = make(n, k, m, sizes, dtype, seed=k)
+    check_forward(c, relu=True)
+    check_forward(c, relu=False, b=False)
+    check_backward(make(n, m, k, sizes, dtype, seed=k, relu_x=True), relu_in=True)
+
+
+def test_rows_far_apart():
+    """Element offsets past 32 bits: 70,000 rows of 64 columns, 65,536 apart."""
+    note("[far rows]")
+    torch = need_gpu()
+    n, k, m = 70000, 64, 40
+    wide = torch.zeros(n, 65536, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    wide[:, :k] = torch.randn(n, k, device="cuda", generator=g).to(torch.bfloat16)
+    c = make(n, k, m, None, BF16, seed=1)
+    c["x"] = wide[:, :k]
+    check_forward(c, relu=True)
+    check_backward(c, relu_in=False)
+    dx = torch.empty_like(wide)[:, :k]
+    import paper_2606_11440_amd as P
+    P.im_linear_backward(c["dy"], c["x"], c["W"], dx)
+    ref, tol = U.linear_grad(c["dy"], c["x"], c["W"], None, False)[0]
+    U.close(dx, ref, tol, "dx")
+
+
 def test_no_rows():
     c = make(0, 20, 30, None, BF16)
     run_forward(c, True)
