@@ -322,6 +322,8 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
           }
         }
       }
+      const int n_wave = n_first + wn * S::NJ * 16;
+      auto near = [&](int y) { return (unsigned)(y - n_wave) < (unsigned)(S::NJ * 16); };
       auto bits_of = [&](int i, int j) { return words[i][j / 2] >> ((j & 1) * 16 + g4); };
       f32x4 plus[S::NJ];   // the classes' biases times log2 e
 #pragma unroll
@@ -341,37 +343,52 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
           const int m = m_at + i * 16, y = rows[m].y;
           Stats s{-INFINITY, 0.f, 0.f};
 #pragma unroll
-          for (int j = 0; j < S::NJ; ++j) {
-            f32x4 t;
-            const int n = n_at + j * 16;
+          for (int j = 0; j < S::NJ; ++j)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) t[r] = fmaf(acc[i][j][r], kLog2e, plus[j][r]);
-            if ((unsigned)(y - n) < 4u) {
-              const float ty = y - n == 0 ? t[0] : (y - n == 1 ? t[1] : (y - n == 2 ? t[2] : t[3]));
-              (whole ? taken[m] : a.taken[(int64_t)at_lo + m]) = ty;
+            for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(acc[i][j][r], kLog2e, plus[j][r]);
+          if (__any(near(y))) {   // the target is in the wave's columns for some rows
+#pragma unroll
+            for (int j = 0; j < S::NJ; ++j) {
+              const int at = y - n_at - j * 16;
+              const f32x4 t = acc[i][j];
+              if ((unsigned)at < 4u)
+                (whole ? taken[m] : a.taken[(int64_t)at_lo + m]) = at == 0 ? t[0] : (at == 1 ? t[1] : (at == 2 ? t[2] : t[3]));
             }
-            if (a.valid) {
+          }
+          if (a.valid) {
+#pragma unroll
+            for (int j = 0; j < S::NJ; ++j) {
               const uint32_t bits = bits_of(i, j);
 #pragma unroll
-              for (int r = 0; r < 4; ++r) t[r] = (bits >> r) & 1u ? t[r] : -INFINITY;
+              for (int r = 0; r < 4; ++r) acc[i][j][r] = (bits >> r) & 1u ? acc[i][j][r] : -INFINITY;
             }
-            if (edge) {
-#pragma unroll
-              for (int r = 0; r < 4; ++r) t[r] = n + r < a.N ? t[r] : -INFINITY;
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) s.top = fmaxf(s.top, t[r]);
-            acc[i][j] = t;
           }
-          const float ref = s.top == -INFINITY ? 0.f : s.top;
+          if (edge) {
+#pragma unroll
+            for (int j = 0; j < S::NJ; ++j)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) acc[i][j][r] = n_at + j * 16 + r < a.N ? acc[i][j][r] : -INFINITY;
+          }
 #pragma unroll
           for (int j = 0; j < S::NJ; ++j)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const float d = acc[i][j][r] - ref, e = exp2_(d);
-              s.sum += e;                                // NaN goes this way
-              s.tsum = fmaf(e, fmaxf(d, kLeast), s.tsum);   // no 0 times infinity
-            }
+            for (int r = 0; r < 4; ++r) s.top = fmaxf(s.top, acc[i][j][r]);
+          const float ref = s.top == -INFINITY ? 0.f : s.top;
+          if (a.entropy) {
+#pragma unroll
+            for (int j = 0; j < S::NJ; ++j)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float d = acc[i][j][r] - ref, e = exp2_(d);
+                s.sum += e;                                   // NaN goes this way
+                s.tsum = fmaf(e, fmaxf(d, kLeast), s.tsum);   // no 0 times infinity
+              }
+          } else {
+#pragma unroll
+            for (int j = 0; j < S::NJ; ++j)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) s.sum += exp2_(acc[i][j][r] - ref);
+          }
 #pragma unroll
           for (int d = 16; d < 64; d *= 2) {
             const Stats o{__shfl_xor(s.top, d), __shfl_xor(s.sum, d), __shfl_xor(s.tsum, d)};
@@ -410,6 +427,7 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
           if (a.live && a.col0 == 0 && at_ct == 0 && wn == 0 && g4 == 0 && at_lo + m < at_hi)
             a.live[(int64_t)at_lo + m] = of.live || fabsf(acc[i][0][0]) < INFINITY;
           const int y = of.y - a.col0;
+          const bool target = __any(near(y));   // in the wave's columns for some rows
 #pragma unroll
           for (int j = 0; j < S::NJ; ++j) {
             const int n = n_at + j * 16;
@@ -419,7 +437,7 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
               const float t = fmaxf(fmaf(acc[i][j][r], kLog2e, plus[j][r] - of.lse2), kLeast);
               dz[r] = exp2_(t) * fmaf(of.B, t, of.A);
             }
-            if ((unsigned)(y - n) < 4u) {
+            if (target && (unsigned)(y - n) < 4u) {
 #pragma unroll
               for (int r = 0; r < 4; ++r)
                 dz[r] += y - n == r && fmaf(acc[i][j][r], kLog2e, plus[j][r]) != -INFINITY ? of.up : 0.f;
