@@ -6,8 +6,10 @@
 // over its columns (the parts are added through LDS), then from the dz of all
 // classes it forms its columns of dh = dz W and adds to its columns of dW =
 // sum dz^T h, which stay in registers while the rows of a group pass. W stays
-// there too, in the orders that the two products take it. A block takes 32 rows
-// at a time: two barriers a tile, the next tile's rows on their way meanwhile.
+// there too, in the orders that the two products take it. dz enters the products
+// as two bf16 numbers, its rounding and what that leaves, so that only the
+// results are rounded (the products are a small part of the time). A block takes
+// 32 rows at a time: two barriers a tile, the next tile's rows on their way.
 //
 // As in the sums over rows, the groups' rows are a line of granules that the
 // blocks cut into equal runs; what a run's end cuts is joined in order.
@@ -25,7 +27,7 @@ constexpr int kRows = 32, kClasses = 64, kSlice = 64;
 
 struct NarrowRow {
   int y;
-  float lse2, A, B, up;
+  float lse, A, B, up;
   uint32_t mask[2];
   int live;
 };
@@ -63,7 +65,7 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
   static_assert(kUnits == 4 && kQuads >= 1, "");
   __shared__ __attribute__((aligned(16))) char h_lds[2][kHBytes];
   __shared__ __attribute__((aligned(16))) char parts[NW][kPart];   // of the logits; then a wave's dh
-  __shared__ __attribute__((aligned(16))) char dz_lds[kRows * 128];
+  __shared__ __attribute__((aligned(16))) char dz_lds[2][kRows * 128];   // dz rounded to bf16, and what that leaves
   __shared__ NarrowRow info[2][kRows];
   __shared__ Groups groups;
 
@@ -128,7 +130,7 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
     f32x4 plus = {0.f, 0.f, 0.f, 0.f}, colsum = {0.f, 0.f, 0.f, 0.f};
     if (a.bias)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) plus[r] = quad * 4 + r < a.V ? a.bias[(int64_t)g * a.V + quad * 4 + r] * kLog2e : 0.f;
+      for (int r = 0; r < 4; ++r) plus[r] = quad * 4 + r < a.V ? a.bias[(int64_t)g * a.V + quad * 4 + r] : 0.f;
 
     f32x4 dw[4][4];   // [classes][columns]
 #pragma unroll
@@ -170,7 +172,7 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
       mine = NarrowRow{-1, INFINITY, 0.f, 0.f, 0.f, {0xffffffffu, 0xffffffffu}, 0};
       if (tid >= kRows || row >= hi) return;
       mine.y = a.target[row];
-      mine.lse2 = a.lse[row];
+      mine.lse = a.lse[row];
       mine.up = a.dlogp[row];
       mine.A = a.dentropy ? a.entropy[row] : 0.f;
       mine.B = a.dentropy ? a.dentropy[row] : 0.f;
@@ -188,12 +190,12 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
         const bool wrong = y < -1 || y >= a.V || (y >= 0 && !(((y < 32 ? mine.mask[0] : mine.mask[1]) >> (y & 31)) & 1u));
         if (wrong && a.error) atomicOr(a.error, IM_ERR_ACTION);
         if (wrong) mine.y = -1;
-        const float H = mine.A, ent = mine.B, lse = mine.lse2, up = mine.y < 0 ? 0.f : mine.up;
+        const float H = mine.A, ent = mine.B, lse = mine.lse, up = mine.y < 0 ? 0.f : mine.up;
         mine.live = (up != 0.f || ent != 0.f) && lse != -INFINITY;
         mine.up = mine.live ? up : 0.f;
         mine.A = mine.live ? -up - ent * H + (lse - lse) : 0.f;   // an lse that is not finite makes the row NaN
         mine.B = mine.live ? -ent * kLn2 : 0.f;
-        mine.lse2 = mine.live ? lse * kLog2e : INFINITY;
+        mine.lse = mine.live ? lse : INFINITY;
       }
       info[t & 1][tid] = mine;
     };
@@ -245,33 +247,40 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
         for (int w = 0; w < NW; ++w) z += *reinterpret_cast<const f32x4*>(parts[w] + z_at(row, quad));
         const NarrowRow& of = info[t & 1][row];
         const uint32_t bits = of.mask[quad / 8] >> (quad % 8 * 4);
-        const float lse2 = of.lse2, A = of.A, B = of.B, up = of.up;
+        const float lse = of.lse, A = of.A, B = of.B, up = of.up;
         const int y = of.y;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float zr = fmaf(z[r], kLog2e, plus[r]), tr = fmaxf(zr - lse2, kLeast);
+          const float zr = z[r] + plus[r], tr = fmaxf((zr - lse) * kLog2e, kLeast);
           float v = exp2_(tr) * fmaf(B, tr, A);
           v += quad * 4 + r == y && zr != -INFINITY ? up : 0.f;
           dz[r] = (bits >> r) & 1u && quad * 4 + r < a.V ? v : 0.f;
         }
         colsum += dz;
-        bf16x4 o;
+        bf16x4 o, rest;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[r] = (T)dz[r];
-        *reinterpret_cast<bf16x4*>(dz_lds + dz_at(row, quad / 2) + (quad & 1) * 8) = o;
+        for (int r = 0; r < 4; ++r) {
+          o[r] = (T)dz[r];
+          rest[r] = (T)(dz[r] - (float)o[r]);
+        }
+        *reinterpret_cast<bf16x4*>(dz_lds[0] + dz_at(row, quad / 2) + (quad & 1) * 8) = o;
+        *reinterpret_cast<bf16x4*>(dz_lds[1] + dz_at(row, quad / 2) + (quad & 1) * 8) = rest;
       }
       __syncthreads();
       // dW of the wave's columns
       if (a.dW) {
         const int lane = fresh_thread() % 64;
-        u32x4 p[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = across_rows(dz_lds, lane, i * 16, dz_at);
+        for (int half = 0; half < 2; ++half) {
+          u32x4 p[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const u32x4 q = across_rows(ht, lane, c_first + j * 16, h_at<NW>);
+          for (int i = 0; i < 4; ++i) p[i] = across_rows(dz_lds[half], lane, i * 16, dz_at);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) dw[i][j] = mma<T>(q, p[i], dw[i][j]);
+          for (int j = 0; j < 4; ++j) {
+            const u32x4 q = across_rows(ht, lane, c_first + j * 16, h_at<NW>);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dw[i][j] = mma<T>(q, p[i], dw[i][j]);
+          }
         }
       }
       // dh of the wave's columns, through the wave's own LDS to whole lines
@@ -283,10 +292,10 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
 #pragma unroll
           for (int j = 0; j < 4; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            const u32x4 p = *reinterpret_cast<const u32x4*>(dz_lds + dz_at(i * 16 + l16, s * 4 + g4));
+          for (int s = 0; s < 4; ++s) {   // what the rounding left first
+            const u32x4 p = *reinterpret_cast<const u32x4*>(dz_lds[1 - s / 2] + dz_at(i * 16 + l16, s % 2 * 4 + g4));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] = mma<T>(wv[j][s], p, o[j]);
+            for (int j = 0; j < 4; ++j) o[j] = mma<T>(wv[j][s % 2], p, o[j]);
           }
           const int row = i * 16 + l16;
 #pragma unroll
@@ -357,7 +366,7 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
         colsum[r] += __shfl_xor(colsum[r], 32);
       }
       __syncthreads();   // dz has been read
-      f32x4* const across = reinterpret_cast<f32x4*>(dz_lds);   // [NW][16]
+      f32x4* const across = reinterpret_cast<f32x4*>(dz_lds[0]);   // [NW][16]
       if (lane < 16) across[wave * 16 + lane] = colsum;
       __syncthreads();
       if (tid < 16) {

@@ -77,22 +77,22 @@ __device__ __forceinline__ void put_row(const RowArgs& a, int64_t row, const Sta
 
 // What a head's epilogue reads of a row. For the gradient, with t = log2 pi:
 //   dz = 2^t (A + B t), and `up` more at the target;
-//   A = -up - ent H, B = -ent ln 2, t = z log2 e - lse log2 e
+//   A = -up - ent H, B = -ent ln 2, t = (z - lse) log2 e
 // A row that adds nothing has A = B = up = 0 and lse = +inf, so that t is the
 // least there is and every dz is 0, whatever its logits are.
 struct Row {
   int y;
-  float lse2, A, B, up;
+  float lse, A, B, up;
   bool live;
   __device__ __forceinline__ void load(const RowArgs& a, int64_t row, int hi, bool gradient) {
     y = -1;
     A = B = up = 0.f;
-    lse2 = INFINITY;
+    lse = INFINITY;
     live = false;
     if (row >= hi) return;
     y = a.target[row];
     if (!gradient) return;
-    lse2 = a.lse[row];
+    lse = a.lse[row];
     up = a.dlogp[row];
     A = a.dentropy ? a.entropy[row] : 0.f;
     B = a.dentropy ? a.dentropy[row] : 0.f;
@@ -104,12 +104,12 @@ struct Row {
     if (wrong) y = -1;
     if (!gradient) return wrong;
     if (y < 0) up = 0.f;
-    const float H = A, ent = B, lse = lse2;
+    const float H = A, ent = B;
     live = (up != 0.f || ent != 0.f) && lse != -INFINITY;
     up = live ? up : 0.f;
     A = live ? -up - ent * H + (lse - lse) : 0.f;   // an lse that is not finite makes the row NaN
     B = live ? -ent * kLn2 : 0.f;
-    lse2 = live ? lse * kLog2e : INFINITY;
+    lse = live ? lse : INFINITY;
     return wrong;
   }
 };
@@ -325,12 +325,12 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
       const int n_wave = n_first + wn * S::NJ * 16;
       auto near = [&](int y) { return (unsigned)(y - n_wave) < (unsigned)(S::NJ * 16); };
       auto bits_of = [&](int i, int j) { return words[i][j / 2] >> ((j & 1) * 16 + g4); };
-      f32x4 plus[S::NJ];   // the classes' biases times log2 e
+      f32x4 plus[S::NJ];   // the classes' biases (for the statistics times log2 e)
 #pragma unroll
       for (int j = 0; j < S::NJ; ++j) {
         plus[j] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (bias && n_at + j * 16 < a.N) plus[j] = load4(bias + n_at + j * 16, a.N - n_at - j * 16);
-        plus[j] *= kLog2e;
+        if constexpr (EPI == kStats) plus[j] *= kLog2e;
       }
 
       if constexpr (EPI == kStats) {
@@ -434,13 +434,13 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
             f32x4 dz;   // takes the logits' place
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const float t = fmaxf(fmaf(acc[i][j][r], kLog2e, plus[j][r] - of.lse2), kLeast);
+              const float t = fmaxf((acc[i][j][r] + (plus[j][r] - of.lse)) * kLog2e, kLeast);
               dz[r] = exp2_(t) * fmaf(of.B, t, of.A);
             }
             if (target && (unsigned)(y - n) < 4u) {
 #pragma unroll
               for (int r = 0; r < 4; ++r)
-                dz[r] += y - n == r && fmaf(acc[i][j][r], kLog2e, plus[j][r]) != -INFINITY ? of.up : 0.f;
+                dz[r] += y - n == r && acc[i][j][r] + plus[j][r] != -INFINITY ? of.up : 0.f;
             }
             if (a.valid) {
               const uint32_t bits = bits_of(i, j);
