@@ -46,6 +46,7 @@ extern "C" {
 #endif
 
 #define IM_MAX_GROUPS 1024        /* n_groups                                          */
+#define IM_MAX_ROWS   (1 << 30)   /* n_rows                                            */
 #define IM_MAX_DIM    65536       /* in_dim, out_dim, dim                              */
 #define IM_MAX_LD     (1 << 22)   /* row strides (elements)                            */
 #define IM_MAX_CLASSES (1 << 22)  /* n_classes                                         */
@@ -54,7 +55,7 @@ extern "C" {
 
 /* ---- grouped layers -------------------------------------------------------
  * y_i = act(W_g x_i + b_g) for the rows i of group g.
- *   n_rows    rows of x and y, >= 0
+ *   n_rows    rows of x and y, in [0, IM_MAX_ROWS]
  *   in_dim, out_dim   in [1, IM_MAX_DIM]
  *   dtype     im_dtype of x, W, y and of dy, dx, dW
  *   relu      forward: 1 = act is max(., 0), 0 = none
@@ -92,7 +93,7 @@ im_status im_linear_backward(const im_linear_desc* desc, const int32_t* offsets,
  * z_i = W_g h_i + b_g, pi_i = softmax of z_i over the row's valid classes; the
  * logits are never kept. With target = the taken action, logp and entropy are
  * those that im_route_sample reports (Sec. 4.4, Eq. 5); -logp is the cross entropy.
- *   n_rows    >= 0; dim in [1, IM_MAX_DIM]; n_classes in [1, IM_MAX_CLASSES]
+ *   n_rows    in [0, IM_MAX_ROWS]; dim in [1, IM_MAX_DIM]; n_classes in [1, IM_MAX_CLASSES]
  *   dtype     im_dtype of h, W, dh, dW
  *   relu_in   backward: as in im_linear_desc, for h and dh
  *   ld_h, ld_dh   row strides

@@ -83,13 +83,14 @@ im_status check_work(const void* ws, int64_t have, int64_t need) {
   return IM_OK;
 }
 im_status check_launch(const RowPlan& p) {
-  if (p.row_tiles * p.col_tiles * p.splits > 0x7fffffff) return fail(IM_EUNSUPPORTED, "more than 2^31 - 1 tiles");
+  if (p.row_tiles * p.col_tiles * p.splits >= 1 << 30) return fail(IM_EUNSUPPORTED, "2^30 tiles or more");
   return IM_OK;
 }
 im_status check_grid(const SumPlan& p, int64_t groups) {
-  // tiles and groups are the second and third dimension of the joining launch
-  if (p.parts * p.row_tiles * p.col_tiles > 0x7fffffff) return fail(IM_EUNSUPPORTED, "more than 2^31 - 1 blocks");
-  if (p.row_tiles * p.col_tiles > 65535 || groups > 65535) return fail(IM_EUNSUPPORTED, "more than 65535 tiles of a gradient");
+  if (p.parts * p.row_tiles * p.col_tiles >= 1 << 30) return fail(IM_EUNSUPPORTED, "2^30 blocks or more");
+  // tiles are the second dimension of the launch that joins
+  if ((p.parts > 1 || groups > 1) && p.row_tiles * p.col_tiles > 65535)
+    return fail(IM_EUNSUPPORTED, "more than 65535 tiles of a gradient in pieces");
   return IM_OK;
 }
 #define LEARN_OK(call)                       \
@@ -103,7 +104,7 @@ im_status check_grid(const SumPlan& p, int64_t groups) {
 im_status check_linear(const im_linear_desc* d) {
   LEARN_CHECK(d, "desc is NULL");
   LEARN_CHECK(d->n_groups >= 1 && d->n_groups <= IM_MAX_GROUPS, "n_groups out of range");
-  LEARN_CHECK(d->n_rows >= 0, "n_rows out of range");
+  LEARN_CHECK(d->n_rows >= 0 && d->n_rows <= IM_MAX_ROWS, "n_rows out of range");
   LEARN_CHECK(d->in_dim >= 1 && d->in_dim <= IM_MAX_DIM, "in_dim out of range");
   LEARN_CHECK(d->out_dim >= 1 && d->out_dim <= IM_MAX_DIM, "out_dim out of range");
   LEARN_CHECK(d->dtype == IM_F32 || d->dtype == IM_BF16, "dtype out of range");
@@ -291,7 +292,7 @@ namespace {
 im_status check_head(const im_head_desc* d) {
   LEARN_CHECK(d, "desc is NULL");
   LEARN_CHECK(d->n_groups >= 1 && d->n_groups <= IM_MAX_GROUPS, "n_groups out of range");
-  LEARN_CHECK(d->n_rows >= 0, "n_rows out of range");
+  LEARN_CHECK(d->n_rows >= 0 && d->n_rows <= IM_MAX_ROWS, "n_rows out of range");
   LEARN_CHECK(d->dim >= 1 && d->dim <= IM_MAX_DIM, "dim out of range");
   LEARN_CHECK(d->n_classes >= 1 && d->n_classes <= IM_MAX_CLASSES, "n_classes out of range");
   LEARN_CHECK(d->dtype == IM_F32 || d->dtype == IM_BF16, "dtype out of range");

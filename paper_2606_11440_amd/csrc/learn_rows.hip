@@ -625,7 +625,7 @@ RowPlan plan_rows(int dtype, int64_t n, int64_t G, int64_t N, int64_t K, int cus
   static const int bm[] = {Large::BM, Middle::BM, Narrow::BM, Small::BM};
   static const int bn[] = {Large::BN, Middle::BN, Narrow::BN, Small::BN};
   static const int per_cu[] = {Large::kBlocks, Middle::kBlocks, Narrow::kBlocks, Small::kBlocks};
-  static const double kStageUs[2][4] = {{10.0, 5.0, 4.2, 3.3}, {2.0, 1.35, 1.2, 1.2}};
+  static const double kStageUs[2][4] = {{10.0, 5.0, 4.2, 2.5}, {2.0, 1.35, 1.2, 0.9}};
   static const double kEpilogueUs[4] = {6.0, 4.0, 3.0, 2.5};
   constexpr double kAlone = 0.7, kJoin = 8.0;
   const bool half = dtype == IM_BF16;

@@ -272,7 +272,7 @@ template <int WM_, int WN_, int MI_, int NJ_, int D_, int SB_>
 struct Shape {
   static constexpr int WM = WM_, WN = WN_, MI = MI_, NJ = NJ_, D = D_, SB = SB_;
   static constexpr int kWaves = MI * NJ >= 16 ? 2 : 3;   // a SIMD, by the registers (and LDS) they take
-  static constexpr int kBlocks = MI * NJ >= 32 ? 1 : (MI * NJ >= 16 ? 2 : (MI * NJ >= 8 ? 3 : 4));   // a CU
+  static constexpr int kBlocks = MI * NJ >= 32 ? 1 : (MI * NJ >= 16 ? 2 : 3);   // a CU
   static constexpr int NT = WM * WN * 64, BM = WM * MI * 16, BN = WN * NJ * 16;
 };
 

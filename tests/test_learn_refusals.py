@@ -40,9 +40,9 @@ def head_desc(**kw):
     return d
 
 
-BAD_LINEAR = [dict(n_groups=0), dict(n_groups=1025), dict(n_rows=-1), dict(in_dim=0), dict(in_dim=65537),
+BAD_LINEAR = [dict(n_groups=0), dict(n_groups=1025), dict(n_rows=-1), dict(n_rows=(1 << 30) + 1), dict(in_dim=0), dict(in_dim=65537),
               dict(out_dim=0), dict(out_dim=65537), dict(dtype=2), dict(relu=2), dict(relu_in=-1)]
-BAD_HEAD = [dict(n_groups=0), dict(n_groups=1025), dict(n_rows=-1), dict(dim=0), dict(dim=65537), dict(n_classes=0),
+BAD_HEAD = [dict(n_groups=0), dict(n_groups=1025), dict(n_rows=-1), dict(n_rows=(1 << 30) + 1), dict(dim=0), dict(dim=65537), dict(n_classes=0),
             dict(n_classes=(1 << 22) + 1), dict(dtype=-1), dict(relu_in=2)]
 
 
@@ -93,7 +93,7 @@ def test_layer_arguments():
                  (R(linear_desc(n_groups=3, n_rows=5000, ld_dx=3)), A, A, A, A, A, A, A, A, 1 << 40, None, None)]:
         assert b(*args) == EINVAL
     # tiles beyond what a launch counts
-    big = linear_desc(n_rows=2 ** 31 - 1, in_dim=65536, out_dim=65536, ld_x=65536, ld_y=65536)
+    big = linear_desc(n_rows=2 ** 30, in_dim=65536, out_dim=65536, ld_x=65536, ld_y=65536)
     assert f(R(big), None, A, A, A, A, None, 0, None, None) == P._lib.IM_EUNSUPPORTED
 
 
