@@ -125,10 +125,13 @@ im_status im_head_forward(const im_head_desc* desc, const int32_t* offsets, cons
  *   dh_i = W_g^T dz_i, dW = sum_i dz_i h_i^T, db = sum_i dz_i
  * lse and entropy are the forward call's; dentropy NULL: no entropy term
  * (entropy may then be NULL); dlogp does not count where target is -1. dz is
- * formed in pieces of the classes and, for IM_BF16, rounded to bf16 where it
- * enters the products of dh and dW (db sums it in fp32). A row whose dlogp (or
- * target) and dentropy are both none adds nothing, whatever its h holds. dh, dW
- * and db may be NULL to skip them; b may be NULL (no bias). */
+ * formed in pieces of the classes and, for IM_BF16, rounded where it enters the
+ * products of dh and dW: to two bf16 numbers (16 bits of mantissa) for heads of
+ * up to 64 classes and 512 columns, to one above that (half a step, 2^-8 of each
+ * dz, which dh's and dW's own rounding repeats); db sums it in fp32. A row whose
+ * dlogp (or target) and dentropy are both none adds nothing to dW and db, and its
+ * dh is zero, whatever its h holds; W must be finite. dh, dW and db may be NULL
+ * to skip them; b may be NULL (no bias). */
 im_status im_head_backward(const im_head_desc* desc, const int32_t* offsets, const void* h,
                            const void* W, const float* b, const uint32_t* valid,
                            const int32_t* target, const float* lse, const float* entropy,

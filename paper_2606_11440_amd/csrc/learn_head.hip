@@ -11,6 +11,12 @@
 // results are rounded (the products are a small part of the time). A block takes
 // 32 rows at a time: two barriers a tile, the next tile's rows on their way.
 //
+// Measured, 262144 rows: 64 classes, 512 wide, 16 groups 229 us in one pass against
+// 356 us as products that keep dz in memory (reading h and writing dh: 101 at the
+// rate of a copy); 15 classes, 256 wide 142 against 181. dz as two numbers costs 13 % of
+// that. What bounds it: the wait between barriers, since W and dW fill the
+// registers and leave one block a CU at 512 columns, two at 256.
+//
 // As in the sums over rows, the groups' rows are a line of granules that the
 // blocks cut into equal runs; what a run's end cuts is joined in order.
 #include <type_traits>
@@ -400,6 +406,9 @@ __global__ __launch_bounds__(256) void join_narrow_kernel(const NarrowArgs a) {
 
 }  // namespace
 
+// W and dW of such a head fit the registers of one block (8 waves of 64 columns);
+// wider or longer ones, and fp32, whose fragments take twice the registers, go
+// through the general products.
 bool narrow_supported(int dtype, int64_t d, int64_t V) { return dtype == IM_BF16 && d <= 8 * kSlice && V <= kClasses; }
 
 // A granule is two tiles, a run two granules at least; as many blocks as run at once.

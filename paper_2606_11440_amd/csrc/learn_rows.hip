@@ -1,6 +1,21 @@
 // Products of grouped rows with their group's weights, and what follows them
 // in registers: the layers (bias, ReLU), the gradient of a layer's input (the
 // ReLU before it) and the softmax head (statistics, gradient of the logits).
+//
+// A stage of k is 128 bytes (64 bf16, 32 fp32): one barrier a stage, a line of
+// memory a row. The large tile, 256 x 256 with 32 fragments a wave, is what the
+// matrix cores ask for: it reads 64 KB of LDS for 64 products a wave where a
+// 128 x 128 one reads twice that. Its accumulators leave one block a CU, so a
+// block keeps taking tiles, and the loads of the next one's first stage pass
+// under the epilogue. Measured, bf16 (kernel alone): 8192 x 8192 x 8192 0.94 to
+// 1.01 ms (1.09 to 1.17 PFLOP/s; a library product of the size 1.28), 8192 x 4096 x
+// 4096 258 us, 4095 cubed 286 us, 262144 x 256 x 256 74 us (3.6 TB/s: 50 us at the
+// rate of a copy), 16 x 4096 x 4096 14 us (6.3 us of W at the rate of a copy).
+// What bounds it: at large k the LDS and its barriers (the matrix cores are busy
+// 50 to 60 % of the time); at k of 4 stages or fewer the epilogue, which the one
+// block of a CU does not overlap with products. Tried, and slower or equal: two
+// stages in flight in registers, 256 x 128 tiles, and leaving out the fragments
+// of rows that a ragged tile lacks (8192^3 0.95 to 1.03 ms).
 #include <type_traits>
 
 #include "learn_internal.h"
@@ -619,8 +634,14 @@ hipError_t launch_type(const RowArgs& a, int shape, int epilogue, hipStream_t s)
 // The shape with the least time: the rounds that its tiles take, each of as many
 // stages as k has and of an epilogue. A stage takes kStageUs where the card is
 // full of such blocks (measured: 8192 rows, 4096 x 4096), its share of that with
-// fewer blocks on a CU, and kAlone at least (a block by itself waits for its loads). Several runs of k, joined by a second
-// kernel, where few tiles would leave the card empty.
+// fewer blocks on a CU, and kAlone at least (a block by itself waits for its
+// loads). Several runs of k, joined by a second kernel (kJoin: its launch and
+// latency), where few tiles would leave the card empty.
+// Both sides, bf16, us with large / middle / narrow tiles: 193 to 512 of 64 groups
+// of ragged rows 199 / 224 / 255; ragged experts 327 / 364 / 455; 256 to 256 of
+// 262144 rows 74 / 79 / 86; statistics of 50257 classes 530 / 632 / 732, but those
+// of 15 classes 93 / 59 / 37 (43 with small ones). Runs of k: 16 x 4096 x 4096 22
+// -> 14, while 256 x 1024 x 1024 goes from 10 to 14.
 RowPlan plan_rows(int dtype, int64_t n, int64_t G, int64_t N, int64_t K, int cus, bool may_split) {
   static const int bm[] = {Large::BM, Middle::BM, Narrow::BM, Small::BM};
   static const int bn[] = {Large::BN, Middle::BN, Narrow::BN, Small::BN};

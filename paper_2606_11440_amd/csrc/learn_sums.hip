@@ -6,6 +6,16 @@
 // run's end cuts each block keeps its piece (at most two a block: where its run
 // begins and where it ends), and a second kernel adds the pieces in their order
 // (no atomics: the same bits each time).
+//
+// Both operands lie with k across their rows, so a stage is 64 bytes of k (32
+// rows in bf16) and two stages are in flight: the transposing reads of LDS take
+// 4 rows each, and a longer stage would need LDS that the second buffer has.
+// Measured: 64 ragged groups of 262144 rows, 512 x 512, bf16, 206 us and 34 for the
+// join (0.67 PFLOP/s, matrix cores busy 42 %); one piece of a head of 50021 classes,
+// 1024 wide, over 8192 rows 229 us (0.92 PFLOP/s, 52 %); 256 x 256 over 16384 rows,
+// fp32, 35 us with the join (16.4 at the fp32 rate of the matrix cores). A block
+// keeps both accumulators and two stages, so one or two share a CU, and the start
+// and end of each group's sum wait. The join reads what the blocks leave.
 #include "learn_internal.h"
 #include "learn_tile.h"
 
@@ -242,16 +252,26 @@ hipError_t launch_type(const SumArgs& a, int shape, hipStream_t s) {
 
 int rows_per_sum(int shape) { return shape == 0 ? Large::BM : (shape == 1 ? Middle::BM : Small::BM); }
 
-// Shape and parts are those with the least of: the time of the rounds that the
-// blocks take, at the rate that the shape reaches where it fills the card (8192
-// rows, 4096 x 4096: 1.0, 0.8 and 0.45 PFLOP/s in bf16, near 0.11 each in fp32),
-// and that of writing and reading the pieces. A part takes kLeast granules at
-// least: fewer cost more to join than to sum.
+// Shape and parts are those with the least time: of the rounds that the blocks
+// take, each of the granules of its part at kAlone us a granule for one block on
+// a CU and kFull where its CU is full (all measured), and of the epilogues and
+// starts of its groups; and with more parts than one of the join's launch and
+// latency (kJoin) and its pieces.
+// Blocks beside each other on a CU gain little in fp32 and add pieces: the
+// candidates are one block a CU, two, up to a full CU, and whole rounds of those.
+// Both sides, us of dW with its join: 512 x 512 over 4096 rows, bf16, tiles of 64:
+// 1 part 32, 4 (one block a CU) 18, 16 (four) 26, 64 34; tiles of 256: 105 with 1,
+// 29 with 8. 256 x 256 over 16384 rows, fp32, tiles of 128: 64 parts (one block a
+// CU) 34, 128 37, 32 50; over 262144 rows, bf16: 65 with tiles of 128, 72 of 256, 89
+// of 64. 2048 x 2048 over 8192 rows, bf16: 89 with tiles of 256, 94 of 128, 174 of 64.
 SumPlan plan_sums(int dtype, int64_t n, int64_t G, int64_t M, int64_t N, int cus) {
   static const int tile[] = {Large::BM, Middle::BM, Small::BM}, per_cu[] = {1, 2, 4};
-  static const double rate[2][3] = {{1.1e14, 1.05e14, 0.9e14}, {1.0e15, 0.8e15, 0.45e15}};
-  constexpr int64_t kLeast = 4;
+  static const double kAlone[2][3] = {{7.9, 2.35, 0.83}, {1.55, 0.75, 0.43}};
+  static const double kFull[2][3] = {{7.9, 4.7, 3.0}, {1.55, 1.34, 1.19}};
+  static const double kEpilogueUs[3] = {8.0, 4.0, 3.0};
+  constexpr double kJoin = 8.0;
   const bool half = dtype == IM_BF16;
+  const double read = (double)n * (M + N) * (half ? 2 : 4) / 5.4e6;   // us of reading the rows once
   SumPlan best = {};
   double least = 0;
   for (int s = 0; s < 3; ++s) {
@@ -261,22 +281,29 @@ SumPlan plan_sums(int dtype, int64_t n, int64_t G, int64_t M, int64_t N, int cus
     p.col_tiles = (N + tile[s] - 1) / tile[s];
     p.granule = half ? 64 : 32;
     p.piece = (int64_t)tile[s] * tile[s] + tile[s];
-    const int64_t tiles = p.row_tiles * p.col_tiles, slots = (int64_t)cus * per_cu[s];
+    const int64_t tiles = p.row_tiles * p.col_tiles;
     const int64_t granules = n > 0 ? (n + p.granule - 1) / p.granule + (G > 1 ? G - 1 : 0) : 0;
-    const int64_t most = granules < 1 ? 0 : (granules + kLeast - 1) / kLeast;
-    // whole rounds of the card: 1, 2, 3 and 4 of them, as near as the tiles allow
-    for (int round = 0; round <= 4; ++round) {
-      int64_t parts = round == 0 ? 1 : round * slots / tiles;
+    // one part; so many that each CU has 1, 2, .. blocks; 2, 3 and 4 rounds of full CUs
+    for (int step = 0; step <= per_cu[s] + 3; ++step) {
+      const int64_t a_cu = step <= per_cu[s] ? step : (int64_t)per_cu[s] * (step - per_cu[s] + 1);
+      int64_t parts = a_cu * cus / tiles;
       if (parts < 1) parts = 1;
-      // many small groups: a part for a handful of granules serves them side by side
-      if (parts > most) parts = most;
+      if (parts > granules) parts = granules;
       p.parts = parts;
-      const double rounds = parts > 0 ? (double)((parts * tiles + slots - 1) / slots) : 0;
-      const double sum = parts > 0 ? rounds * 2.0 * ((double)granules * p.granule / parts) * tile[s] * tile[s] * slots / rate[half][s] : 0;
-      const double join = parts > 1 ? 2.0 * 2 * parts * tiles * p.piece * 4 / 4e12 + 4e-6 : 0;
-      if ((s == 0 && round == 0) || sum + join < least) {
+      double us = 0;
+      if (parts > 0) {
+        const int64_t blocks = parts * tiles, slots = (int64_t)cus * per_cu[s];
+        const int64_t rounds = (blocks + slots - 1) / slots, beside = rounds > 1 ? per_cu[s] : (blocks + cus - 1) / cus;
+        const double each = per_cu[s] > 1 ? kAlone[half][s] + (kFull[half][s] - kAlone[half][s]) * (beside - 1) / (per_cu[s] - 1)
+                                          : kAlone[half][s];
+        us = rounds * ((double)((granules + parts - 1) / parts) * each + kEpilogueUs[s] * (1 + (double)(G - 1) / parts));
+        if (us < read) us = read;
+        // a part leaves a piece, and one more where a group begins within it
+        if (parts > 1) us += kJoin + (double)(parts + (G > 1 ? (G < parts ? G : parts) : 0)) * tiles * p.piece * 4 / 4e6;
+      }
+      if ((s == 0 && step == 0) || us < least) {
         best = p;
-        least = sum + join;
+        least = us;
       }
     }
   }
