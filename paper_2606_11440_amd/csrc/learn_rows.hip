@@ -4,12 +4,12 @@
 //
 // A stage of k is 128 bytes (64 bf16, 32 fp32): one barrier a stage, a line of
 // memory a row. The large tile, 256 x 256 with 32 fragments a wave, is what the
-// matrix cores ask for: it reads 64 KB of LDS for 64 products a wave where a
-// 128 x 128 one reads twice that. Its accumulators leave one block a CU, so a
+// matrix cores ask for: a wave reads 12 fragments of LDS for 32 products,
+// one of a 128 x 128 tile 8 for 16. Its accumulators leave one block a CU, so a
 // block keeps taking tiles, and the loads of the next one's first stage pass
 // under the epilogue. Measured, bf16 (kernel alone): 8192 x 8192 x 8192 0.94 to
 // 1.01 ms (1.09 to 1.17 PFLOP/s; a library product of the size 1.28), 8192 x 4096 x
-// 4096 258 us, 4095 cubed 286 us, 262144 x 256 x 256 74 us (3.6 TB/s: 50 us at the
+// 4096 258 us (286 with rows of 4095), 262144 x 256 x 256 74 us (3.6 TB/s: 50 us at the
 // rate of a copy), 16 x 4096 x 4096 14 us (6.3 us of W at the rate of a copy).
 // What bounds it: at large k the LDS and its barriers (the matrix cores are busy
 // 50 to 60 % of the time); at k of 4 stages or fewer the epilogue, which the one
@@ -637,11 +637,11 @@ hipError_t launch_type(const RowArgs& a, int shape, int epilogue, hipStream_t s)
 // fewer blocks on a CU, and kAlone at least (a block by itself waits for its
 // loads). Several runs of k, joined by a second kernel (kJoin: its launch and
 // latency), where few tiles would leave the card empty.
-// Both sides, bf16, us with large / middle / narrow tiles: 193 to 512 of 64 groups
-// of ragged rows 199 / 224 / 255; ragged experts 327 / 364 / 455; 256 to 256 of
-// 262144 rows 74 / 79 / 86; statistics of 50257 classes 530 / 632 / 732, but those
+// Both sides, bf16, us with large / middle / narrow tiles: 193 to 512 of 64
+// ragged groups 199 / 224 / 255; ragged experts 327 / 364 / 455; 256 to 256 of
+// 262144 rows 74 / 79 / 86; statistics of 50021 classes 530 / 632 / 732, but those
 // of 15 classes 93 / 59 / 37 (43 with small ones). Runs of k: 16 x 4096 x 4096 22
-// -> 14, while 256 x 1024 x 1024 goes from 10 to 14.
+// -> 14, while 256 x 1024 x 1024 goes from 9 to 11 with 4 runs, 13 with 8.
 RowPlan plan_rows(int dtype, int64_t n, int64_t G, int64_t N, int64_t K, int cus, bool may_split) {
   static const int bm[] = {Large::BM, Middle::BM, Narrow::BM, Small::BM};
   static const int bn[] = {Large::BN, Middle::BN, Narrow::BN, Small::BN};
