@@ -51,6 +51,7 @@ extern "C" {
 #define IM_MAX_LD     (1 << 22)   /* row strides (elements)                            */
 #define IM_MAX_CLASSES (1 << 22)  /* n_classes                                         */
 #define IM_MAX_TENSORS 65536      /* tensors of an im_adamw                            */
+#define IM_MAX_ELEMENTS (1LL << 37)  /* elements of an im_adamw's tensors together      */
 #define IM_STATE_BLOCK 256        /* elements of an 8-bit state that share a scale     */
 
 /* ---- grouped layers -------------------------------------------------------
@@ -154,7 +155,8 @@ im_status im_head_backward(const im_head_desc* desc, const int32_t* offsets, con
  *          computed, before they are rounded. One value that is not finite
  *          makes its block NaN.
  *   decay  1 = weight_decay applies to the tensor, 0 = it does not
- *   n >= 0. Tensors must not overlap. */
+ *   n >= 0. What is written must not overlap anything else of the list (refused);
+ *          gradients may be shared. */
 typedef struct {
   float* param;
   const void* grad;
@@ -181,7 +183,7 @@ im_status im_adamw_create(const im_adamw_tensor* tensors, int32_t n_tensors, int
  *          and stores t (so a captured step may be replayed)
  *   scale  device fp32 [1] multiplied into the gradients (the inverse of a loss
  *          scale, a clipping coefficient), or NULL
- * IM_EINVAL unless lr, eps, weight_decay >= 0 and both betas are in [0, 1). Two
+ * IM_EINVAL unless lr, eps, weight_decay are finite and >= 0 and both betas are in [0, 1). Two
  * steps of one plan must not run at the same time. */
 im_status im_adamw_step(im_adamw* opt, double lr, double beta1, double beta2, double eps,
                         double weight_decay, int64_t* step, const float* scale, void* stream);

@@ -1,4 +1,6 @@
 // C ABI of the learner's operators: checks of arguments, workspaces, launches.
+#include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <new>
@@ -579,6 +581,37 @@ im_status check_tensor(const im_adamw_tensor& t, int bits, int grad_dtype, int i
   return IM_OK;
 }
 
+// Whether something that a step writes lies in another buffer of the step.
+bool overlap(const std::vector<im_adamw_tensor>& list, int bits, int grad_dtype) {
+  struct Span {
+    uintptr_t at, end;
+    bool written;
+  };
+  std::vector<Span> spans;
+  const auto add = [&](const void* p, int64_t bytes, bool written) {
+    if (p && bytes) spans.push_back(Span{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, written});
+  };
+  for (const im_adamw_tensor& t : list) {
+    if (t.n == 0) continue;
+    const int64_t state = bits == 32 ? 4 : 1, blocks = (t.n + IM_STATE_BLOCK - 1) / IM_STATE_BLOCK;
+    add(t.param, 4 * t.n, true);
+    add(t.grad, (int64_t)size_of(grad_dtype) * t.n, false);
+    add(t.m, state * t.n, true);
+    add(t.v, state * t.n, true);
+    add(t.m_scale, 4 * blocks, true);
+    add(t.v_scale, 4 * blocks, true);
+    add(t.copy, 2 * t.n, true);
+  }
+  std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.at < b.at; });
+  uintptr_t any = 0, written = 0;   // ends of what came before
+  for (const Span& s : spans) {
+    if (s.at < (s.written ? any : written)) return true;
+    any = std::max(any, s.end);
+    if (s.written) written = std::max(written, s.end);
+  }
+  return false;
+}
+
 template <typename T>
 hipError_t upload(T** out, const std::vector<T>& from, hipStream_t s) {
   if (from.empty()) return hipSuccess;
@@ -627,13 +660,22 @@ im_status im_adamw_create(const im_adamw_tensor* tensors, int32_t n_tensors, int
   LEARN_CHECK(n_tensors == 0 || tensors, "tensors is NULL");
   LEARN_CHECK(state_bits == 32 || state_bits == 8, "state_bits is 32 or 8");
   LEARN_CHECK(grad_dtype == IM_F32 || grad_dtype == IM_BF16, "grad_dtype out of range");
-  for (int i = 0; i < n_tensors; ++i) LEARN_OK(check_tensor(tensors[i], state_bits, grad_dtype, i));
+  int64_t all = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    LEARN_OK(check_tensor(tensors[i], state_bits, grad_dtype, i));
+    LEARN_CHECK(tensors[i].n <= IM_MAX_ELEMENTS - all, "more than %lld elements", (long long)IM_MAX_ELEMENTS);
+    all += tensors[i].n;
+  }
   im_adamw* o = new (std::nothrow) im_adamw();
   if (!o) return fail(IM_ENOMEM, "out of host memory");
   hipError_t e = hipGetDevice(&o->device);
   try {
     std::vector<AdamwRun> runs;
     std::vector<im_adamw_tensor> list(tensors, tensors + n_tensors);
+    if (overlap(list, state_bits, grad_dtype)) {
+      free_adamw(o);
+      return fail(IM_EINVAL, "tensors overlap");
+    }
     for (int i = 0; i < n_tensors; ++i) {
       const im_adamw_tensor& t = list[i];
       const int64_t state = state_bits == 32 ? 16 : 4;
@@ -672,7 +714,8 @@ im_status im_adamw_step(im_adamw* o, double lr, double beta1, double beta2, doub
   LEARN_CHECK(o, "opt is NULL");
   LEARN_CHECK(step, "step is NULL");
   LEARN_CHECK(aligned(step, 8) && aligned(scale, 4), "a pointer is not aligned to its elements");
-  LEARN_CHECK(lr >= 0 && eps >= 0 && weight_decay >= 0, "lr, eps and weight_decay must be >= 0");
+  LEARN_CHECK(lr >= 0 && eps >= 0 && weight_decay >= 0 && std::isfinite(lr) && std::isfinite(eps) && std::isfinite(weight_decay),
+              "lr, eps and weight_decay must be finite and >= 0");
   LEARN_CHECK(beta1 >= 0 && beta1 < 1 && beta2 >= 0 && beta2 < 1, "betas must be in [0, 1)");
   AdamwArgs a = {};
   a.table = o->table;

@@ -147,6 +147,30 @@ def test_adamw_arguments():
     L().im_adamw_destroy(None)
 
 
+def test_adamw_buffers_do_not_overlap():
+    """A step's blocks run side by side: what one writes no other may touch."""
+    out = ctypes.c_void_p()
+
+    def at(first, n=300, **kw):        # five buffers of their own
+        step = 4096
+        t = dict(zip(("param", "grad", "m", "v", "copy"), range(first, first + 5 * step, step)), n=n)
+        return tensor(**(t | kw))
+
+    def create(*ts, bits=32):
+        return L().im_adamw_create((learn.ImAdamwTensor * len(ts))(*ts), len(ts), bits, 0, None, ctypes.byref(out))
+    base, far = 1 << 20, 1 << 24
+    for ts in ((at(base), at(base)),                                     # one tensor twice
+               (at(base), at(far, param=base + 299 * 4)), (at(base), at(far, v=base)), (at(base), at(far, copy=base)),
+               (at(base), at(far, grad=base)), (at(base, grad=base),), (at(base, m=base + 3 * 4096),),
+               (at(base, n=2000),)):
+        assert create(*ts) == EINVAL and "overlap" in P.im_learn_last_error(), ts
+    scales = dict(m_scale=far, v_scale=far + 4)
+    assert create(at(base, **scales), bits=8) == EINVAL and "overlap" in P.im_learn_last_error()
+    assert create(at(base, n=1 << 38)) == EINVAL and "elements" in P.im_learn_last_error()
+    assert create(at(base, n=1 << 36), at(far, n=(1 << 36) + 1)) == EINVAL and "elements" in P.im_learn_last_error()
+    assert not out.value
+
+
 def test_tensors_are_checked():
     """The binding refuses what the library cannot see: types, devices, shapes."""
     import torch
