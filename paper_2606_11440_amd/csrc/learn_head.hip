@@ -11,11 +11,15 @@
 // results are rounded (the products are a small part of the time). A block takes
 // 32 rows at a time: two barriers a tile, the next tile's rows on their way.
 //
-// Measured, 262144 rows: 64 classes, 512 wide, 16 groups 229 us in one pass against
+// Measured, 262144 rows: 64 classes, 512 wide, 16 groups 220 us in one pass against
 // 356 us as products that keep dz in memory (reading h and writing dh: 101 at the
-// rate of a copy); 15 classes, 256 wide 142 against 181. dz as two numbers costs 13 % of
-// that. What bounds it: the wait between barriers, since W and dW fill the
-// registers and leave one block a CU at 512 columns, two at 256.
+// rate of a copy); 15 classes, 256 wide 113 against 181 (51). dz as two numbers costs
+// 13 % of that. Up to 32 classes take a kernel of half the products and LDS: 135 ->
+// 113 us with 15 classes, 178 -> 156 with 32 and 512 columns. What bounds it: the chain
+// of LDS, products and dz within a tile, at two waves a SIMD (W and dW fill the
+// registers): without the loads 10 % less, without the stores 9, without dh 38. Also
+// tried: dz of the next tile beside the products of this one, each wave with all of k
+// for 16 classes, one long phase a tile: 277 us (registers spill), 138 at 256 columns.
 //
 // As in the sums over rows, the groups' rows are a line of granules that the
 // blocks cut into equal runs; what a run's end cuts is joined in order.
@@ -29,7 +33,7 @@ namespace im {
 namespace learn {
 namespace {
 
-constexpr int kRows = 32, kClasses = 64, kSlice = 64;
+constexpr int kRows = 32, kSlice = 64;
 
 struct NarrowRow {
   int y;
@@ -49,8 +53,11 @@ __device__ __forceinline__ int h_at(int row, int unit) {
 // LDS of dz [rows][classes], 128 bytes a row.
 __device__ __forceinline__ int dz_at(int row, int unit) { return row * 128 + ((unit ^ ((row >> 1) & 7)) << 4); }
 
-// LDS of a wave's part of the logits [rows][classes], 256 bytes a row.
-__device__ __forceinline__ int z_at(int row, int unit) { return row * 256 + ((unit ^ (row & 15)) << 4); }
+// LDS of a wave's part of the logits [rows][C classes], 128 or 256 bytes a row.
+template <int C>
+__device__ __forceinline__ int z_at(int row, int unit) {
+  return row * (C * 4) + ((unit ^ (C == 32 ? (row >> 1) & 7 : row & 15)) << 4);
+}
 
 // 16 columns (from c0) of 32 rows, as a fragment whose k are the rows 4 g + j and
 // 16 + 4 g + j of lane group g: with rows in fours every half wave reads 8 rows.
@@ -63,12 +70,14 @@ __device__ __forceinline__ u32x4 across_rows(const char* lds, int lane, int c0, 
   return __builtin_bit_cast(u32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-template <int NW>
+// NW waves, so NW * kSlice columns; C classes (32 or 64)
+template <int NW, int C>
 __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const NarrowArgs a) {
   using T = __bf16;
   constexpr int NT = NW * 64, kUnits = kRows * NW * 8 / NT, kHBytes = kRows * NW * 128;
-  constexpr int kPart = kRows * kClasses * 4, kQuads = kRows * 16 / NT;
-  static_assert(kUnits == 4 && kQuads >= 1, "");
+  constexpr int kPart = kRows * C * 4, kQuad = C / 4;   // quads of classes
+  constexpr int kQuads = kRows * kQuad > NT ? kRows * kQuad / NT : 1, CB = C / 16, CS = C / 32;
+  static_assert(kUnits == 4 && (C == 32 || C == 64) && kPart >= C * 128 && kPart >= kRows * 128, "");
   __shared__ __attribute__((aligned(16))) char h_lds[2][kHBytes];
   __shared__ __attribute__((aligned(16))) char parts[NW][kPart];   // of the logits; then a wave's dh
   __shared__ __attribute__((aligned(16))) char dz_lds[2][kRows * 128];   // dz rounded to bf16, and what that leaves
@@ -106,9 +115,9 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
 
     // W of the wave's columns: by columns (for the logits) and by classes (for dh)
     const T* const W = static_cast<const T*>(a.W) + g * (int64_t)a.V * a.d;
-    u32x4 wc[4][2], wv[4][2];
+    u32x4 wc[CB][2], wv[4][CS];
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+    for (int b = 0; b < CB; ++b)
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const int cls = b * 16 + l16, col = c_first + s * 32 + g4 * 8, left = a.d - col;
@@ -118,13 +127,13 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
     // by classes: through the wave's LDS (free here), turned on the way out
     __syncthreads();   // the LDS of the group before
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+    for (int b = 0; b < CB; ++b)
 #pragma unroll
       for (int s = 0; s < 2; ++s) *reinterpret_cast<u32x4*>(parts[wave] + dz_at(b * 16 + l16, s * 4 + g4)) = wc[b][s];
 #pragma unroll
     for (int b = 0; b < 4; ++b)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
+      for (int s = 0; s < CS; ++s) {
         typedef __attribute__((address_space(3))) s16x4 lds4;
         const int c = b * 16 + (l16 % 4) * 4, row = s * 32 + g4 * 8 + l16 / 4;
         const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(parts[wave] + dz_at(row, c / 8) + (c & 4) * 2));
@@ -132,15 +141,15 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
         wv[b][s] = __builtin_bit_cast(u32x4, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
       }
     // the biases of the thread's classes in the sum over the parts
-    const int quad = tid % 16;
+    const int quad = tid % kQuad;
     f32x4 plus = {0.f, 0.f, 0.f, 0.f}, colsum = {0.f, 0.f, 0.f, 0.f};
     if (a.bias)
 #pragma unroll
       for (int r = 0; r < 4; ++r) plus[r] = quad * 4 + r < a.V ? a.bias[(int64_t)g * a.V + quad * 4 + r] : 0.f;
 
-    f32x4 dw[4][4];   // [classes][columns]
+    f32x4 dw[CB][4];   // [classes][columns]
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < CB; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) dw[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
@@ -221,20 +230,20 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
       const char* const ht = h_lds[t & 1];
       {   // the logits over the wave's columns
         const int lane = fresh_thread() % 64, l16 = lane % 16, g4 = lane / 16;
-        f32x4 z[2][4];
+        f32x4 z[2][CB];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
 #pragma unroll
-          for (int b = 0; b < 4; ++b) z[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int b = 0; b < CB; ++b) z[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
             const u32x4 p = *reinterpret_cast<const u32x4*>(ht + h_at<NW>(i * 16 + l16, wave * 8 + s * 4 + g4));
 #pragma unroll
-            for (int b = 0; b < 4; ++b) z[i][b] = mma<T>(wc[b][s], p, z[i][b]);
+            for (int b = 0; b < CB; ++b) z[i][b] = mma<T>(wc[b][s], p, z[i][b]);
           }
 #pragma unroll
-          for (int b = 0; b < 4; ++b)
-            *reinterpret_cast<f32x4*>(parts[wave] + z_at(i * 16 + l16, b * 4 + g4)) = z[i][b];
+          for (int b = 0; b < CB; ++b)
+            *reinterpret_cast<f32x4*>(parts[wave] + z_at<C>(i * 16 + l16, b * 4 + g4)) = z[i][b];
         }
       }
       if (full || t + 1 < tiles) store_info(t + 1);
@@ -246,11 +255,12 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
       }
 #pragma unroll
       for (int e = 0; e < kQuads; ++e) {   // dz of four classes of a row
-        const int tid = fresh_thread(), quad = tid % 16;
-        const int row = tid / 16 + e * (NT / 16);
+        const int tid = fresh_thread(), quad = tid % kQuad;
+        const int row = tid / kQuad + e * (NT / kQuad);
+        if (kRows * kQuad < NT && row >= kRows) break;   // whole waves
         f32x4 z = {0.f, 0.f, 0.f, 0.f}, dz;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) z += *reinterpret_cast<const f32x4*>(parts[w] + z_at(row, quad));
+        for (int w = 0; w < NW; ++w) z += *reinterpret_cast<const f32x4*>(parts[w] + z_at<C>(row, quad));
         const NarrowRow& of = info[t & 1][row];
         const uint32_t bits = of.mask[quad / 8] >> (quad % 8 * 4);
         const float lse = of.lse, A = of.A, B = of.B, up = of.up;
@@ -278,14 +288,14 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
         const int lane = fresh_thread() % 64;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          u32x4 p[4];
+          u32x4 p[CB];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) p[i] = across_rows(dz_lds[half], lane, i * 16, dz_at);
+          for (int i = 0; i < CB; ++i) p[i] = across_rows(dz_lds[half], lane, i * 16, dz_at);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const u32x4 q = across_rows(ht, lane, c_first + j * 16, h_at<NW>);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) dw[i][j] = mma<T>(q, p[i], dw[i][j]);
+            for (int i = 0; i < CB; ++i) dw[i][j] = mma<T>(q, p[i], dw[i][j]);
           }
         }
       }
@@ -295,14 +305,16 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           f32x4 o[4];
+          u32x4 p[2 * CS];   // what the rounding left first
 #pragma unroll
           for (int j = 0; j < 4; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int s = 0; s < 4; ++s) {   // what the rounding left first
-            const u32x4 p = *reinterpret_cast<const u32x4*>(dz_lds[1 - s / 2] + dz_at(i * 16 + l16, s % 2 * 4 + g4));
+          for (int s = 0; s < 2 * CS; ++s)
+            p[s] = *reinterpret_cast<const u32x4*>(dz_lds[1 - s / CS] + dz_at(i * 16 + l16, s % CS * 4 + g4));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] = mma<T>(wv[j][s % 2], p, o[j]);
-          }
+          for (int s = 0; s < 2 * CS; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = mma<T>(wv[j][s % CS], p[s], o[j]);
           const int row = i * 16 + l16;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -310,22 +322,27 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
             bf16x4 v;
 #pragma unroll
             for (int r = 0; r < 4; ++r) v[r] = (T)o[j][r];
-            if (a.relu_in) {
-              const bf16x4 x =
-                  *reinterpret_cast<const bf16x4*>(ht + h_at<NW>(row, wave * 8 + c / 8) + (c & 4) * 2);
-#pragma unroll
-              for (int r = 0; r < 4; ++r) v[r] = (float)x[r] > 0.f ? v[r] : (T)0.f;
-            }
             *reinterpret_cast<bf16x4*>(parts[wave] + dz_at(row, c / 8) + (c & 4) * 2) = v;
           }
         }
         // a wave's LDS operations are done in their order
         const int c = c_first + lane % 8 * 8, left = a.d - c;
+        u32x4 out[kRows / 8];
+#pragma unroll
+        for (int i = 0; i < kRows / 8; ++i)
+          out[i] = *reinterpret_cast<const u32x4*>(parts[wave] + dz_at(i * 8 + lane / 8, lane % 8));
+        if (a.relu_in) {
+          u32x4 x[kRows / 8];
+#pragma unroll
+          for (int i = 0; i < kRows / 8; ++i)
+            x[i] = *reinterpret_cast<const u32x4*>(ht + h_at<NW>(i * 8 + lane / 8, wave * 8 + lane % 8));
+#pragma unroll
+          for (int i = 0; i < kRows / 8; ++i) out[i] = where_positive<T>(out[i], x[i]);
+        }
 #pragma unroll
         for (int i = 0; i < kRows / 8; ++i) {
-          const int row = i * 8 + lane / 8;
-          const int64_t at = (int64_t)lo + t * kRows + row;
-          const u32x4 v = *reinterpret_cast<const u32x4*>(parts[wave] + dz_at(row, lane % 8));
+          const int64_t at = (int64_t)lo + t * kRows + i * 8 + lane / 8;
+          const u32x4 v = out[i];
           T* const to = static_cast<T*>(a.dh) + at * a.ld_dh + c;
           if constexpr (full) {
             *reinterpret_cast<u32x4_any*>(to) = v;
@@ -347,7 +364,7 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
     float* const piece = all ? nullptr : a.pieces + (2 * (int64_t)run + (u == begin ? 0 : 1)) * a.piece;
     if (a.dW) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < CB; ++i) {
         const int cls = i * 16 + l16;
         if (cls >= a.V) continue;
 #pragma unroll
@@ -367,17 +384,16 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
     }
     if (a.db) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        colsum[r] += __shfl_xor(colsum[r], 16);
-        colsum[r] += __shfl_xor(colsum[r], 32);
-      }
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int o = kQuad; o < 64; o *= 2) colsum[r] += __shfl_xor(colsum[r], o);
       __syncthreads();   // dz has been read
-      f32x4* const across = reinterpret_cast<f32x4*>(dz_lds[0]);   // [NW][16]
-      if (lane < 16) across[wave * 16 + lane] = colsum;
+      f32x4* const across = reinterpret_cast<f32x4*>(dz_lds[0]);   // [NW][kQuad]
+      if (lane < kQuad) across[wave * kQuad + lane] = colsum;
       __syncthreads();
-      if (tid < 16) {
+      if (tid < kQuad) {
         f32x4 v = across[tid];
-        for (int w = 1; w < NW; ++w) v += across[w * 16 + tid];
+        for (int w = 1; w < NW; ++w) v += across[w * kQuad + tid];
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           if (tid * 4 + r < a.V)
@@ -409,7 +425,7 @@ __global__ __launch_bounds__(256) void join_narrow_kernel(const NarrowArgs a) {
 // W and dW of such a head fit the registers of one block (8 waves of 64 columns);
 // wider or longer ones, and fp32, whose fragments take twice the registers, go
 // through the general products.
-bool narrow_supported(int dtype, int64_t d, int64_t V) { return dtype == IM_BF16 && d <= 8 * kSlice && V <= kClasses; }
+bool narrow_supported(int dtype, int64_t d, int64_t V) { return dtype == IM_BF16 && d <= 8 * kSlice && V <= 64; }
 
 // A granule is two tiles, a run two granules at least; as many blocks as run at once.
 NarrowPlan plan_narrow(int64_t n, int64_t G, int64_t d, int64_t V, int cus) {
@@ -425,8 +441,10 @@ NarrowPlan plan_narrow(int64_t n, int64_t G, int64_t d, int64_t V, int cus) {
 
 hipError_t launch_narrow(const NarrowArgs& a, hipStream_t s) {
   if (a.parts > 0) {
-    if (a.d <= 4 * kSlice) hipLaunchKernelGGL(narrow_gradient_kernel<4>, dim3((unsigned)a.parts), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(narrow_gradient_kernel<8>, dim3((unsigned)a.parts), dim3(512), 0, s, a);
+    const bool thin = a.d <= 4 * kSlice;
+    const auto kernel = a.V <= 32 ? (thin ? narrow_gradient_kernel<4, 32> : narrow_gradient_kernel<8, 32>)
+                                  : (thin ? narrow_gradient_kernel<4, 64> : narrow_gradient_kernel<8, 64>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)a.parts), dim3(thin ? 256 : 512), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -46,18 +46,6 @@ __device__ __forceinline__ void store4(float* p, f32x4 v, int left) {
   }
 }
 
-// A unit of results where x is above zero, else zeros.
-template <typename T>
-__device__ __forceinline__ u32x4 where_positive(u32x4 v, u32x4 x) {
-  T e[kVec<T>], q[kVec<T>];
-  __builtin_memcpy(e, &v, 16);
-  __builtin_memcpy(q, &x, 16);
-#pragma unroll
-  for (int i = 0; i < kVec<T>; ++i) e[i] = (float)q[i] > 0.f ? e[i] : T(0.f);
-  __builtin_memcpy(&v, e, 16);
-  return v;
-}
-
 // Softmax statistics of some classes of a row, in powers of two (t = z log2 e):
 // the largest t, and with it subtracted sum 2^t and sum 2^t t. Nothing seen:
 // {-inf, 0, 0}.

@@ -34,6 +34,33 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 template <typename T> constexpr int kVec = 16 / (int)sizeof(T);   // elements of a 16-byte unit
 constexpr int kHalf = 64;                                          // bytes of k that a fragment covers
 
+// A unit of results where x is above zero (neither NaN), else zeros. bf16: the
+// numbers above zero are the 16-bit integers 1 .. 0x7f80 (infinity), so five
+// packed integer operations make a factor of 1 or 0 for the bits of two results.
+template <typename T>
+__device__ __forceinline__ u32x4 where_positive(u32x4 v, u32x4 x) {
+  if constexpr (sizeof(T) == 2) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    typedef short i16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t xi = x[i], vi = v[i];
+      const u16x2 m = __builtin_bit_cast(u16x2, __builtin_elementwise_max(__builtin_bit_cast(i16x2, xi), i16x2{0, 0}));
+      const u16x2 number = __builtin_elementwise_sub_sat(u16x2{0x7f81, 0x7f81}, m);   // 0: NaN
+      const u16x2 one = __builtin_elementwise_min(__builtin_elementwise_min(m, number), u16x2{1, 1});
+      const u16x2 out = __builtin_bit_cast(u16x2, vi) * one;
+      v[i] = __builtin_bit_cast(uint32_t, out);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t xi = x[i];
+      v[i] = __builtin_bit_cast(float, xi) > 0.f ? v[i] : 0u;
+    }
+  }
+  return v;
+}
+
 template <typename T>
 __device__ __forceinline__ u32x4 load16(const T* p) {
   return *reinterpret_cast<const u32x4_any*>(p);

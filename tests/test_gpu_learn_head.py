@@ -106,6 +106,15 @@ SHAPES = [  # n, dim, classes, group sizes
 ]
 
 
+@pytest.mark.parametrize("relu_in", [False, True])
+@pytest.mark.parametrize("n,d,V,sizes", [(20000, 512, 32, [9000, 11000]), (9000, 512, 31, None), (20000, 256, 32, None),
+                                         (9000, 256, 33, [4000, 0, 5000]), (9000, 256, 64, None), (700, 511, 17, None)])
+def test_narrow_heads_at_the_edges_of_their_blocks(n, d, V, sizes, relu_in):
+    c = make(n, d, V, sizes, BF16, seed=V, relu=relu_in)
+    o, r = check_forward(c)
+    check_backward(c, o, r, relu_in)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("mask", [False, True])
 @pytest.mark.parametrize("n,d,V,sizes", SHAPES)

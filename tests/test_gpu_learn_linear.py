@@ -183,6 +183,25 @@ def test_what_is_not_read_does_not_matter():
     assert all(bool(torch.isfinite(v).all()) for v in o.values())
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_the_relu_below_takes_what_is_above_zero(dtype):
+    """Zeros of both signs, the smallest and largest numbers, infinities and NaN in x."""
+    c = make(300, 64, 40, None, dtype, seed=3)
+    torch, f = c["torch"], getattr(c["torch"], dtype)
+    some = torch.tensor([0.0, -0.0, float("inf"), -float("inf"), float("nan"), -float("nan"), torch.finfo(f).max,
+                         torch.finfo(f).min, torch.finfo(f).tiny, -torch.finfo(f).tiny, 1.0, -1.0], device="cuda").to(f)
+    bits = torch.tensor([1, 2, 0x7f, 0x80], dtype=torch.int32 if f is torch.float32 else torch.int16, device="cuda").view(f)
+    some = torch.cat([some, bits, -bits])          # the smallest numbers
+    plain = run_backward(c, False, ("dx",))["dx"].clone()
+    at = torch.arange(300 * 64, device="cuda").view(300, 64) * 7 % len(some)
+    c["x"].copy_(some[at])
+    got = run_backward(c, True, ("dx",))["dx"]
+    # whether x is above zero, from its bits: the smallest numbers must count
+    raw = c["x"].contiguous().view(torch.int32 if f is torch.float32 else torch.int16).long()
+    top = 0x7f800000 if f is torch.float32 else 0x7f80
+    assert bool((got == torch.where((raw > 0) & (raw <= top), plain, torch.zeros_like(plain))).all())
+
+
 def test_values_that_are_not_finite_travel():
     c = make(100, 40, 50, None, F32, seed=9)
     torch = c["torch"]
