@@ -179,9 +179,14 @@ struct Step {
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float g = f.g[i] * scale;
-      f.m[i] = f.m[i] * a.beta1f + g * a.omb1;
-      f.v[i] = f.v[i] * a.beta2f + g * g * a.omb2;
+      {
+        // every product rounded by itself: a state on the border between two codes falls to
+        // the side where elementary fp32 operations put it (a flipped code is 6 % of it)
+#pragma clang fp contract(off)
+        const float g = f.g[i] * scale;
+        f.m[i] = f.m[i] * a.beta1f + g * a.omb1;
+        f.v[i] = f.v[i] * a.beta2f + g * g * a.omb2;
+      }
       // root and reciprocal to 1 unit: the parameter's own rounding is coarser
       const float d = __builtin_amdgcn_sqrtf(f.v[i] * r2) + a.eps;
       f.p[i] = f.p[i] * keep - f.m[i] * r1 * __builtin_amdgcn_rcpf(d) * a.lr;
