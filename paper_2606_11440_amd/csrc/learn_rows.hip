@@ -55,7 +55,9 @@ struct Stats {
 __device__ __forceinline__ Stats join(const Stats& a, const Stats& b) {
   Stats o;
   o.top = fmaxf(a.top, b.top);
-  const float da = a.top == -INFINITY ? 0.f : a.top - o.top, db = b.top == -INFINITY ? 0.f : b.top - o.top;
+  // at kLeast the exponential is 0; further down the distance times the sum would overflow (0 times infinity)
+  const float da = a.top == -INFINITY ? 0.f : fmaxf(a.top - o.top, kLeast);
+  const float db = b.top == -INFINITY ? 0.f : fmaxf(b.top - o.top, kLeast);
   const float ea = exp2_(da), eb = exp2_(db);   // a side that saw nothing has sums of zero (NaN sums stay)
   o.sum = a.sum * ea + b.sum * eb;
   o.tsum = (a.tsum + da * a.sum) * ea + (b.tsum + db * b.sum) * eb;

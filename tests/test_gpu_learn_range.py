@@ -1,0 +1,72 @@
+"""GPU: the softmax head on biases of any magnitude, as users mask classes with.
+
+Bounds are learn_util's with one difference: what a row's bound takes from its
+classes it takes from those with a share of 2^-60 or more. A class below that
+adds less than V 2^-60 (|ln p| + 1) |ln p| <= 2^-30 to no statistic, whatever
+the rounding of its own logit, so that a bias of -1e38 loosens nothing but the
+log-probability of its own class."""
+import math
+
+import pytest
+
+import learn_util as U
+from gpu_util import need_gpu, note
+from test_gpu_learn_head import make, run_backward, run_forward
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = "float32", "bfloat16"
+LEAST_SHARE = 2.0 ** -60
+
+
+class Head(U.Head):
+    def __init__(self, h, W, b, valid, target, offsets):
+        import torch
+        super().__init__(h, W, b, valid, target, offsets)
+        ez = torch.zeros_like(self.p)
+        for g, r in enumerate(self.spans):
+            ez[r] = U.gamma(self.d) * (self.h[r].abs() @ self.W[g].abs().T) + U.U * b[g].double().cpu().abs()
+        seen = self.p >= LEAST_SHARE
+        zero = torch.zeros_like(self.p)
+        far = torch.where(seen, self.lnp.abs(), zero).amax(1) + math.log(self.V + 1)
+        base = torch.where(self.lse == -math.inf, torch.zeros_like(self.lse), self.lse)
+        self.share = 2 * torch.where(seen, ez, zero).amax(1) + (far + 4) * 2.0 ** -22 + 4 * U.U * base.abs()
+        own = ez[torch.arange(self.n), self.y.clamp_min(0)]
+        self.e_logp = 2 * self.share + 2 * own + 4 * U.U * self.logp.nan_to_num(0, 0, 0).abs()
+        self.e_lse = 2 * self.share + 4 * U.U * base.abs()
+        self.e_H = 2 * self.share * (self.H.abs() + 2) + 2.0 ** -21 * (1 + math.log(self.V + 1))
+
+
+def check(c, ent=True):
+    torch = c["torch"]
+    o = run_forward(c)
+    assert o["error"] == 0
+    r = Head(c["h"], c["W"], c["b"], c["valid"], c["target"], c["off"])
+    assert float(torch.cat([r.share, r.e_lse, r.e_H]).max()) < 0.1   # they bound something
+    U.close(o["logp"], r.logp, r.e_logp, "logp")
+    U.close(o["lse"], r.lse, r.e_lse, "lse")
+    U.close(o["entropy"], r.H, r.e_H, "entropy")
+    q = run_backward(c, o, relu_in=True, ent=ent)
+    for k, (want, tol) in zip(("dh", "dW", "db"), r.grads(c["dlogp"], c["dent"] if ent else None, True)):
+        U.close(q[k], want, tol, k)
+
+
+# the last: tiles of 256 classes, of which some see masked classes only
+HEADS = [(15, 32, BF16), (15, 32, F32), (64, 96, BF16), (130, 40, BF16), (1000, 32, BF16), (1000, 32, F32), (4100, 24, BF16)]
+# what a lane's four classes, a lane's run of joined ones, a wave's columns and a tile of classes see
+MASKED = {"four": lambda V: slice(4, 8), "most": lambda V: slice(1, V), "half": lambda V: slice(0, V // 2),
+          "tile": lambda V: slice(V // 256 // 2 * 256, V // 256 // 2 * 256 + min(256, V - 5)), "odd": lambda V: slice(1, V, 2)}
+
+
+@pytest.mark.parametrize("far", [1e20, 1e30, 1e35, 1e36, 1e37, 1e38, 2e38])
+@pytest.mark.parametrize("which", list(MASKED))
+@pytest.mark.parametrize("V,d,dtype", HEADS)
+def test_classes_far_below_the_others(V, d, dtype, which, far):
+    note(f"[far below] V={V} d={d} {dtype} {which} {far}")
+    c = make(150, d, V, None, dtype, seed=V, mask=False)
+    masked = c["torch"].zeros(V, dtype=c["torch"].bool, device="cuda")
+    masked[MASKED[which](V)] = True
+    c["b"][0, masked] = -far
+    free = c["torch"].nonzero(~masked)[:, 0].int()
+    y = c["target"]
+    c["target"] = c["torch"].where(y >= 0, free[y.clamp_min(0).long() % len(free)], y)
+    check(c)
