@@ -267,7 +267,7 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
         const int y = of.y;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float zr = z[r] + plus[r], tr = fmaxf((zr - lse) * kLog2e, kLeast);
+          const float zr = z[r] + plus[r], tr = log2_share(zr - lse);
           float v = exp2_(tr) * fmaf(B, tr, A);
           v += quad * 4 + r == y && zr != -INFINITY ? up : 0.f;
           dz[r] = (bits >> r) & 1u && quad * 4 + r < a.V ? v : 0.f;

@@ -439,7 +439,9 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
             f32x4 dz;   // takes the logits' place
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const float t = fmaxf((acc[i][j][r] + (plus[j][r] - of.lse)) * kLog2e, kLeast);
+              // the logit is rounded as the statistics' is, before lse is taken from it: where a bias
+              // outweighs the products by far, lse holds nothing of them either
+              const float t = log2_share(acc[i][j][r] + plus[j][r] - of.lse);
               dz[r] = exp2_(t) * fmaf(of.B, t, of.A);
             }
             if (target && (unsigned)(y - n) < 4u) {

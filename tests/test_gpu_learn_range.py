@@ -19,7 +19,9 @@ LEAST_SHARE = 2.0 ** -60
 
 
 class Head(U.Head):
-    def __init__(self, h, W, b, valid, target, offsets):
+    def __init__(self, h, W, b, valid, target, offsets, top=None):
+        """top: a class whose share is 1 and whose logit is its bias, since its
+        products vanish in the sum's rounding: nothing of that rounding enters."""
         import torch
         super().__init__(h, W, b, valid, target, offsets)
         ez = torch.zeros_like(self.p)
@@ -29,19 +31,23 @@ class Head(U.Head):
         zero = torch.zeros_like(self.p)
         far = torch.where(seen, self.lnp.abs(), zero).amax(1) + math.log(self.V + 1)
         base = torch.where(self.lse == -math.inf, torch.zeros_like(self.lse), self.lse)
-        self.share = 2 * torch.where(seen, ez, zero).amax(1) + (far + 4) * 2.0 ** -22 + 4 * U.U * base.abs()
+        self.share = (far + 4) * 2.0 ** -22
         own = ez[torch.arange(self.n), self.y.clamp_min(0)]
+        if top is None:
+            self.share += 2 * torch.where(seen, ez, zero).amax(1) + 4 * U.U * base.abs()
+        else:   # another class's log-probability keeps the two logits' roundings
+            own = torch.where(self.y == top, 0, own + ez[:, top])
         self.e_logp = 2 * self.share + 2 * own + 4 * U.U * self.logp.nan_to_num(0, 0, 0).abs()
         self.e_lse = 2 * self.share + 4 * U.U * base.abs()
         self.e_H = 2 * self.share * (self.H.abs() + 2) + 2.0 ** -21 * (1 + math.log(self.V + 1))
 
 
-def check(c, ent=True):
+def check(c, ent=True, top=None):
     torch = c["torch"]
     o = run_forward(c)
     assert o["error"] == 0
-    r = Head(c["h"], c["W"], c["b"], c["valid"], c["target"], c["off"])
-    assert float(torch.cat([r.share, r.e_lse, r.e_H]).max()) < 0.1   # they bound something
+    r = Head(c["h"], c["W"], c["b"], c["valid"], c["target"], c["off"], top)
+    assert float(torch.cat([r.share, r.e_lse - 4 * U.U * r.lse.abs(), r.e_H]).max()) < 0.1   # they bound something
     U.close(o["logp"], r.logp, r.e_logp, "logp")
     U.close(o["lse"], r.lse, r.e_lse, "lse")
     U.close(o["entropy"], r.H, r.e_H, "entropy")
@@ -70,3 +76,17 @@ def test_classes_far_below_the_others(V, d, dtype, which, far):
     y = c["target"]
     c["target"] = c["torch"].where(y >= 0, free[y.clamp_min(0).long() % len(free)], y)
     check(c)
+
+
+@pytest.mark.parametrize("far", [1e8, 1e20, 1e37, 1e38, 2e38])
+@pytest.mark.parametrize("V,d,dtype", HEADS)
+def test_a_class_far_above_the_others(V, d, dtype, far):
+    """Its share is 1 in every row, and what it takes from the others is exactly dlogp."""
+    note(f"[far above] V={V} d={d} {dtype} {far}")
+    c = make(100, d, V, None, dtype, seed=V + 1, mask=False)
+    c["b"][0, 9] = far
+    c["W"][0, 9] *= 0.25
+    c["target"][:40] = 9
+    product = c["h"].double() @ c["W"][0, 9].double()
+    assert float(product.abs().max()) < 2 and float(product.abs().min()) > 0   # the spacing of floats at 1e8 is 8
+    check(c, top=9)
