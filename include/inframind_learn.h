@@ -100,8 +100,9 @@ im_status im_linear_backward(const im_linear_desc* desc, const int32_t* offsets,
  *   ld_h, ld_dh   row strides
  * valid: uint32 [n_rows x ceil(n_classes / 32)], class j of a row is valid when
  * bit j % 32 of its word j / 32 is set, or NULL (every class is). A class whose
- * logit is -infinity is not valid either. A row without a valid class has logp,
- * entropy and gradients 0 and lse -infinity. */
+ * logit is -infinity is not valid either; any finite logit is one like others, the
+ * lowest float too. A row without a valid class has logp, entropy and gradients 0
+ * and lse -infinity. */
 typedef struct {
   int32_t n_groups, n_rows, dim, n_classes;
   int32_t dtype, relu_in, reserved0, reserved1;
@@ -125,8 +126,11 @@ im_status im_head_forward(const im_head_desc* desc, const int32_t* offsets, cons
  *   dz_ij = dlogp_i ([j = target_i] - pi_ij) - dentropy_i pi_ij (ln pi_ij + entropy_i)
  *   dh_i = W_g^T dz_i, dW = sum_i dz_i h_i^T, db = sum_i dz_i
  * lse and entropy are the forward call's; dentropy NULL: no entropy term
- * (entropy may then be NULL); dlogp does not count where target is -1. dz is
- * formed in pieces of the classes and, for IM_BF16, rounded where it enters the
+ * (entropy may then be NULL); dlogp does not count where target is -1. pi is
+ * formed from fp32 logits and the fp32 lse, off by |lse| 2^-23 of itself
+ * (and is 1 at most), and a row whose lse is -1e30 or less, all of whose valid classes
+ * are masked by their biases then, has gradients 0 as one without a valid class.
+ * dz is formed in pieces of the classes and, for IM_BF16, rounded where it enters the
  * products of dh and dW: to two bf16 numbers (16 bits of mantissa) for heads of
  * up to 64 classes and 512 columns, to one above that (half a step, 2^-8 of each
  * dz, which dh's and dW's own rounding repeats); db sums it in fp32. A row whose

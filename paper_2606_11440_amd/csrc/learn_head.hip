@@ -206,7 +206,7 @@ __global__ __launch_bounds__(NW * 64, 2) void narrow_gradient_kernel(const Narro
         if (wrong && a.error) atomicOr(a.error, IM_ERR_ACTION);
         if (wrong) mine.y = -1;
         const float H = mine.A, ent = mine.B, lse = mine.lse, up = mine.y < 0 ? 0.f : mine.up;
-        mine.live = (up != 0.f || ent != 0.f) && lse != -INFINITY;
+        mine.live = (up != 0.f || ent != 0.f) && !(lse <= kMasked);
         mine.up = mine.live ? up : 0.f;
         mine.A = mine.live ? -up - ent * H + (lse - lse) : 0.f;   // an lse that is not finite makes the row NaN
         mine.B = mine.live ? -ent * kLn2 : 0.f;

@@ -46,21 +46,22 @@ __device__ __forceinline__ void store4(float* p, f32x4 v, int left) {
   }
 }
 
-// Softmax statistics of some classes of a row, in powers of two (t = z log2 e):
-// the largest t, and with it subtracted sum 2^t and sum 2^t t. Nothing seen:
-// {-inf, 0, 0}.
+// Softmax statistics of some classes of a row: the largest logit, and with it
+// subtracted sum e^z and sum e^z z. Nothing seen: {-inf, 0, 0}. Logits are scaled
+// by log2 e once the largest is taken from them, on the way into the exponential
+// only: a finite one stays finite down to the lowest float.
 struct Stats {
-  float top, sum, tsum;
+  float top, sum, zsum;
 };
 __device__ __forceinline__ Stats join(const Stats& a, const Stats& b) {
   Stats o;
   o.top = fmaxf(a.top, b.top);
-  // at kLeast the exponential is 0; further down the distance times the sum would overflow (0 times infinity)
-  const float da = a.top == -INFINITY ? 0.f : fmaxf(a.top - o.top, kLeast);
-  const float db = b.top == -INFINITY ? 0.f : fmaxf(b.top - o.top, kLeast);
-  const float ea = exp2_(da), eb = exp2_(db);   // a side that saw nothing has sums of zero (NaN sums stay)
+  // at kLeastE the exponential is 0; further down the distance times the sum would overflow (0 times infinity)
+  const float da = a.top == -INFINITY ? 0.f : fmaxf(a.top - o.top, kLeastE);
+  const float db = b.top == -INFINITY ? 0.f : fmaxf(b.top - o.top, kLeastE);
+  const float ea = exp_(da), eb = exp_(db);   // a side that saw nothing has sums of zero (NaN sums stay)
   o.sum = a.sum * ea + b.sum * eb;
-  o.tsum = (a.tsum + da * a.sum) * ea + (b.tsum + db * b.sum) * eb;
+  o.zsum = (a.zsum + da * a.sum) * ea + (b.zsum + db * b.sum) * eb;
   return o;
 }
 
@@ -71,13 +72,13 @@ __device__ __forceinline__ bool class_valid(const RowArgs& a, int64_t row, int j
 __device__ __forceinline__ bool target_wrong(const RowArgs& a, int64_t row, int y) {
   return y < -1 || y >= a.V || (y >= 0 && !class_valid(a, row, y));
 }
-// ty: t of the target
-__device__ __forceinline__ void put_row(const RowArgs& a, int64_t row, const Stats& s, int y, float ty) {
+// zy: logit of the target
+__device__ __forceinline__ void put_row(const RowArgs& a, int64_t row, const Stats& s, int y, float zy) {
   const bool some = !(s.sum == 0.f);
-  const float lg = some ? __builtin_amdgcn_logf(s.sum) : 0.f;   // log2
-  a.logp[row] = some && y >= 0 ? (ty - s.top - lg) * kLn2 : 0.f;
-  if (a.entropy) a.entropy[row] = some ? (lg - s.tsum / s.sum) * kLn2 : 0.f;
-  if (a.lse) a.lse[row] = some ? (s.top + lg) * kLn2 : -INFINITY;
+  const float lg = some ? __builtin_amdgcn_logf(s.sum) * kLn2 : 0.f;   // logf: log2
+  a.logp[row] = some && y >= 0 ? zy - s.top - lg : 0.f;
+  if (a.entropy) a.entropy[row] = some ? lg - s.zsum / s.sum : 0.f;
+  if (a.lse) a.lse[row] = some ? s.top + lg : -INFINITY;
 }
 
 // What a head's epilogue reads of a row. For the gradient, with t = log2 pi:
@@ -110,7 +111,7 @@ struct Row {
     if (!gradient) return wrong;
     if (y < 0) up = 0.f;
     const float H = A, ent = B;
-    live = (up != 0.f || ent != 0.f) && lse != -INFINITY;
+    live = (up != 0.f || ent != 0.f) && !(lse <= kMasked);
     up = live ? up : 0.f;
     A = live ? -up - ent * H + (lse - lse) : 0.f;   // an lse that is not finite makes the row NaN
     B = live ? -ent * kLn2 : 0.f;
@@ -330,12 +331,11 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
       const int n_wave = n_first + wn * S::NJ * 16;
       auto near = [&](int y) { return (unsigned)(y - n_wave) < (unsigned)(S::NJ * 16); };
       auto bits_of = [&](int i, int j) { return words[i][j / 2] >> ((j & 1) * 16 + g4); };
-      f32x4 plus[S::NJ];   // the classes' biases (for the statistics times log2 e)
+      f32x4 plus[S::NJ];   // the classes' biases
 #pragma unroll
       for (int j = 0; j < S::NJ; ++j) {
         plus[j] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (bias && n_at + j * 16 < a.N) plus[j] = load4(bias + n_at + j * 16, a.N - n_at - j * 16);
-        if constexpr (EPI == kStats) plus[j] *= kLog2e;
       }
 
       if constexpr (EPI == kStats) {
@@ -348,16 +348,14 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
           const int m = m_at + i * 16, y = rows[m].y;
           Stats s{-INFINITY, 0.f, 0.f};
 #pragma unroll
-          for (int j = 0; j < S::NJ; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(acc[i][j][r], kLog2e, plus[j][r]);
+          for (int j = 0; j < S::NJ; ++j) acc[i][j] += plus[j];
           if (__any(near(y))) {   // the target is in the wave's columns for some rows
 #pragma unroll
             for (int j = 0; j < S::NJ; ++j) {
               const int at = y - n_at - j * 16;
-              const f32x4 t = acc[i][j];
+              const f32x4 z = acc[i][j];
               if ((unsigned)at < 4u)
-                (whole ? taken[m] : a.taken[(int64_t)at_lo + m]) = at == 0 ? t[0] : (at == 1 ? t[1] : (at == 2 ? t[2] : t[3]));
+                (whole ? taken[m] : a.taken[(int64_t)at_lo + m]) = at == 0 ? z[0] : (at == 1 ? z[1] : (at == 2 ? z[2] : z[3]));
             }
           }
           if (a.valid) {
@@ -384,19 +382,19 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
             for (int j = 0; j < S::NJ; ++j)
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
-                const float d = acc[i][j][r] - ref, e = exp2_(d);
-                s.sum += e;                                   // NaN goes this way
-                s.tsum = fmaf(e, fmaxf(d, kLeast), s.tsum);   // no 0 times infinity
+                const float d = acc[i][j][r] - ref, e = exp_(d);
+                s.sum += e;                                    // NaN goes this way
+                s.zsum = fmaf(e, fmaxf(d, kLeastE), s.zsum);   // no 0 times infinity
               }
           } else {
 #pragma unroll
             for (int j = 0; j < S::NJ; ++j)
 #pragma unroll
-              for (int r = 0; r < 4; ++r) s.sum += exp2_(acc[i][j][r] - ref);
+              for (int r = 0; r < 4; ++r) s.sum += exp_(acc[i][j][r] - ref);
           }
 #pragma unroll
           for (int d = 16; d < 64; d *= 2) {
-            const Stats o{__shfl_xor(s.top, d), __shfl_xor(s.sum, d), __shfl_xor(s.tsum, d)};
+            const Stats o{__shfl_xor(s.top, d), __shfl_xor(s.sum, d), __shfl_xor(s.zsum, d)};
             s = join(s, o);
           }
           if (g4 == 0) across[wn * S::BM + m] = s;
@@ -413,7 +411,7 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
             put_row(a, row, s, rows[m].y, taken[m]);
           } else {
             float* to = a.stats + ((int64_t)at_ct * a.n + row) * 3;
-            to[0] = s.top, to[1] = s.sum, to[2] = s.tsum;
+            to[0] = s.top, to[1] = s.sum, to[2] = s.zsum;
           }
         }
         last(more);
@@ -514,7 +512,7 @@ __global__ __launch_bounds__(256) void join_kernel(const RowArgs a) {
       s = join(s, Stats{p[0], p[1], p[2]});
     }
 #pragma unroll
-  for (int d = 16; d < 64; d *= 2) s = join(s, Stats{__shfl_xor(s.top, d), __shfl_xor(s.sum, d), __shfl_xor(s.tsum, d)});
+  for (int d = 16; d < 64; d *= 2) s = join(s, Stats{__shfl_xor(s.top, d), __shfl_xor(s.sum, d), __shfl_xor(s.zsum, d)});
   if (threadIdx.x % 64 < 16) across[threadIdx.x / 64][r] = s;
   __syncthreads();
   if (threadIdx.x >= 16 || row >= end) return;

@@ -16,6 +16,7 @@ from test_gpu_learn_head import make, run_backward, run_forward
 pytestmark = pytest.mark.gpu
 F32, BF16 = "float32", "bfloat16"
 LEAST_SHARE = 2.0 ** -60
+LARGEST = 3.4028234e38      # rounds to the largest fp32
 
 
 class Head(U.Head):
@@ -63,7 +64,7 @@ MASKED = {"four": lambda V: slice(4, 8), "most": lambda V: slice(1, V), "half": 
           "tile": lambda V: slice(V // 256 // 2 * 256, V // 256 // 2 * 256 + min(256, V - 5)), "odd": lambda V: slice(1, V, 2)}
 
 
-@pytest.mark.parametrize("far", [1e20, 1e30, 1e35, 1e36, 1e37, 1e38, 2e38])
+@pytest.mark.parametrize("far", [1e20, 1e30, 1e35, 1e36, 1e37, 1e38, 2e38, LARGEST])
 @pytest.mark.parametrize("which", list(MASKED))
 @pytest.mark.parametrize("V,d,dtype", HEADS)
 def test_classes_far_below_the_others(V, d, dtype, which, far):
@@ -78,7 +79,7 @@ def test_classes_far_below_the_others(V, d, dtype, which, far):
     check(c)
 
 
-@pytest.mark.parametrize("far", [1e8, 1e20, 1e37, 1e38, 2e38])
+@pytest.mark.parametrize("far", [1e8, 1e20, 1e37, 1e38, 2e38, LARGEST])
 @pytest.mark.parametrize("V,d,dtype", HEADS)
 def test_a_class_far_above_the_others(V, d, dtype, far):
     """Its share is 1 in every row, and what it takes from the others is exactly dlogp."""
@@ -90,3 +91,71 @@ def test_a_class_far_above_the_others(V, d, dtype, far):
     product = c["h"].double() @ c["W"][0, 9].double()
     assert float(product.abs().max()) < 2 and float(product.abs().min()) > 0   # the spacing of floats at 1e8 is 8
     check(c, top=9)
+
+
+@pytest.mark.parametrize("far", [1e35, 1e38, 2.3e38, 2.5e38, LARGEST])
+@pytest.mark.parametrize("V,d,dtype", HEADS)
+def test_targets_far_below(V, d, dtype, far):
+    """A class that its bias masks is valid as long as its logit is finite: its
+    log-probability is about -far, and dlogp goes through it whole."""
+    note(f"[targets far below] V={V} d={d} {dtype} {far}")
+    c = make(120, d, V, None, dtype, seed=V + 2, mask=False)
+    c["b"][0, 2::3] = -far
+    c["target"][::2] = 5
+    check(c)
+
+
+@pytest.mark.parametrize("far", [2e30, 1e38, 2.3e38, 2.5e38, LARGEST])
+@pytest.mark.parametrize("V,d,dtype", HEADS)
+def test_rows_with_masked_classes_only(V, d, dtype, far):
+    """Rows whose valid classes all have the bias -far: with no products they are
+    equally likely. lse cannot hold that, so those rows have no gradient."""
+    note(f"[masked rows] V={V} d={d} {dtype} {far}")
+    c = make(120, d, V, None, dtype, seed=V + 3, mask=False)
+    torch = c["torch"]
+    masked = torch.zeros(V, dtype=torch.bool, device="cuda")
+    masked[2::3] = True
+    c["b"][0, masked] = -far
+    y = c["target"]
+    c["target"] = torch.where((y >= 0) & masked[y.clamp_min(0).long()], 0, y)
+    rows = torch.zeros(120, dtype=torch.bool, device="cuda")
+    rows[::4] = True
+    c["h"][rows] = 0
+    c["target"][rows] = 5
+    bits = torch.ones(120, (V + 31) // 32 * 32, dtype=torch.bool, device="cuda")
+    bits[:, :V][rows] = masked
+    w = (bits.view(120, -1, 32).long() << torch.arange(32, device="cuda")).sum(2)
+    c["valid"] = torch.where(w >= 2 ** 31, w - 2 ** 32, w).to(torch.int32)
+    o, k = run_forward(c), int(masked.sum())
+    assert o["error"] == 0
+    fit = 2.0 ** -21 * (1 + math.log(k))
+    assert float((o["logp"][rows].double() + math.log(k)).abs().max()) <= fit
+    assert float((o["entropy"][rows].double() - math.log(k)).abs().max()) <= fit
+    assert float((o["lse"][rows].double() + far).abs().max()) <= 2 * U.U * far
+    # the others are as they are without those rows
+    some = dict(c, **{key: c[key][~rows] for key in ("h", "target", "valid", "dlogp", "dent")})
+    check(some)
+    a = run_backward(c, o, relu_in=False)
+    assert bool((a["dh"][rows] == 0).all())
+    want = Head(some["h"], some["W"], some["b"], some["valid"], some["target"], None)
+    for key, (ref, tol) in zip(("dh", "dW", "db"), want.grads(some["dlogp"], some["dent"], False)):
+        U.close(a[key][~rows] if key == "dh" else a[key], ref, tol, key)
+
+
+@pytest.mark.parametrize("V,d,dtype", HEADS)
+def test_biases_from_end_to_end(V, d, dtype):
+    """The largest and the lowest float in one row: their difference is no float."""
+    note(f"[end to end] V={V} d={d} {dtype}")
+    c = make(100, d, V, None, dtype, seed=V + 4, mask=False)
+    c["b"][0, 3] = LARGEST
+    c["b"][0, 4:11] = -LARGEST
+    c["target"][:50] = 3
+    c["target"][50:] = 6
+    o = run_forward(c)
+    q = run_backward(c, o, relu_in=False)
+    assert bool((o["logp"][:50] == 0).all()) and bool(o["logp"][50:].isneginf().all()) and bool((o["entropy"] == 0).all())
+    # dz of rows 50..: dlogp at class 6, -dlogp at class 3
+    want = c["dlogp"][50:].double().sum()
+    tol = 2 * U.gamma(100) * float(c["dlogp"].double().abs().sum())
+    assert abs(float(q["db"][0, 6] - want)) <= tol and abs(float(q["db"][0, 3] + want)) <= tol
+    assert not bool(q["dh"].isnan().any()) and not bool(q["dW"].isnan().any())
