@@ -89,7 +89,9 @@ im_status check_launch(const RowPlan& p) {
   return IM_OK;
 }
 im_status check_grid(const SumPlan& p, int64_t groups) {
-  if (p.parts * p.row_tiles * p.col_tiles >= 1 << 30) return fail(IM_EUNSUPPORTED, "2^30 blocks or more");
+  // a launch has less than 2^32 threads in a dimension
+  if (p.parts * p.row_tiles * p.col_tiles * threads_per_sum(p.shape) >= (int64_t)1 << 32)
+    return fail(IM_EUNSUPPORTED, "2^32 threads or more");
   // tiles are the second dimension of the launch that joins
   if ((p.parts > 1 || groups > 1) && p.row_tiles * p.col_tiles > 65535)
     return fail(IM_EUNSUPPORTED, "more than 65535 tiles of a gradient in pieces");
@@ -688,7 +690,8 @@ im_status im_adamw_create(const im_adamw_tensor* tensors, int32_t n_tensors, int
     o->runs = (int64_t)runs.size();
     // 2^26 elements, a block a run against blocks that share the runs, 8 a CU: 353 and 367 us
     // with 32-bit states, 224 and 220 us with 8-bit ones
-    o->blocks = state_bits == 32 ? o->runs : 8 * (int64_t)compute_units();
+    // (a launch has less than 2^32 threads)
+    o->blocks = state_bits == 32 ? std::min<int64_t>(o->runs, 1 << 23) : 8 * (int64_t)compute_units();
     const hipStream_t s = (hipStream_t)stream;
     const std::vector<uint32_t> zero(1, 0);
     if (e == hipSuccess && o->runs > 0x7fffffff) e = hipErrorInvalidValue;

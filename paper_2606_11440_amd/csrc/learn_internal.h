@@ -125,6 +125,7 @@ hipError_t launch_bias_sum(const int32_t* offsets, int G, int n, int step, const
 int rows_per_tile(int shape);   // of a row product
 int cols_per_tile(int shape);
 int rows_per_sum(int shape);    // rows of W a tile of the sums covers
+int threads_per_sum(int shape);
 
 }  // namespace learn
 }  // namespace im

@@ -492,11 +492,10 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
   }
 }
 
-// Joins the column tiles' statistics of 16 rows a block: 16 threads a row.
+// Joins the column tiles' statistics, a block 16 rows at a time: 16 threads a row.
 __global__ __launch_bounds__(256) void join_kernel(const RowArgs a) {
   __shared__ Stats across[4][16];
   const int r = threadIdx.x % 16, part = threadIdx.x / 16;
-  const int64_t row = (int64_t)blockIdx.x * 16 + r;
   int end = a.n;
   if (a.offsets) {
     Part run;
@@ -505,21 +504,26 @@ __global__ __launch_bounds__(256) void join_kernel(const RowArgs a) {
     if (bad) return;
     end = a.offsets[a.G];
   }
-  Stats s{-INFINITY, 0.f, 0.f};
-  if (row < end)
-    for (int c = part; c < a.col_tiles; c += 16) {
-      const float* p = a.stats + ((int64_t)c * a.n + row) * 3;
-      s = join(s, Stats{p[0], p[1], p[2]});
-    }
+  for (int64_t first = (int64_t)blockIdx.x * 16; first < end; first += (int64_t)gridDim.x * 16) {
+    const int64_t row = first + r;
+    Stats s{-INFINITY, 0.f, 0.f};
+    if (row < end)
+      for (int c = part; c < a.col_tiles; c += 16) {
+        const float* p = a.stats + ((int64_t)c * a.n + row) * 3;
+        s = join(s, Stats{p[0], p[1], p[2]});
+      }
 #pragma unroll
-  for (int d = 16; d < 64; d *= 2) s = join(s, Stats{__shfl_xor(s.top, d), __shfl_xor(s.sum, d), __shfl_xor(s.zsum, d)});
-  if (threadIdx.x % 64 < 16) across[threadIdx.x / 64][r] = s;
-  __syncthreads();
-  if (threadIdx.x >= 16 || row >= end) return;
-  for (int w = 1; w < 4; ++w) s = join(s, across[w][r]);
-  const int y = a.target[row];
-  const bool none = y < 0 || target_wrong(a, row, y);
-  put_row(a, row, s, none ? -1 : y, none ? 0.f : a.taken[row]);
+    for (int d = 16; d < 64; d *= 2) s = join(s, Stats{__shfl_xor(s.top, d), __shfl_xor(s.sum, d), __shfl_xor(s.zsum, d)});
+    if (threadIdx.x % 64 < 16) across[threadIdx.x / 64][r] = s;
+    __syncthreads();
+    if (threadIdx.x < 16 && row < end) {
+      for (int w = 1; w < 4; ++w) s = join(s, across[w][r]);
+      const int y = a.target[row];
+      const bool none = y < 0 || target_wrong(a, row, y);
+      put_row(a, row, s, none ? -1 : y, none ? 0.f : a.taken[row]);
+    }
+    __syncthreads();   // the next rows take the LDS
+  }
 }
 
 // Joins the runs of k and finishes as kStore (STORE) or kStoreInput do: four
@@ -586,7 +590,9 @@ hipError_t launch(const RowArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((rows_kernel<T, S, COLUMNS, EPI>), dim3((unsigned)(tiles < most ? tiles : most)), dim3(S::NT), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && EPI == kStats && a.col_tiles > 1) {
-    hipLaunchKernelGGL(join_kernel, dim3((unsigned)((a.n + 15) / 16)), dim3(256), 0, s, a);
+    // a launch has less than 2^32 threads in a dimension: past 2^24 rows the blocks take more of them each
+    const int blocks = (a.n + 15) / 16, at_most = 1 << 20;
+    hipLaunchKernelGGL(join_kernel, dim3((unsigned)(blocks < at_most ? blocks : at_most)), dim3(256), 0, s, a);
     e = hipGetLastError();
   }
   return e;
@@ -604,6 +610,7 @@ template <typename T, bool COLUMNS>
 hipError_t launch_split(const RowArgs& a, int shape, hipStream_t s) {
   hipError_t e = shape == 1 ? launch<T, Middle, COLUMNS, kPartial>(a, s) : launch<T, Small, COLUMNS, kPartial>(a, s);
   if (e != hipSuccess) return e;
+  // k is cut only where the results are two rounds of tiles at most: some millions of them
   const int64_t quads = (int64_t)a.n * ((a.N + 3) / 4);
   hipLaunchKernelGGL((join_k_kernel<T, !COLUMNS>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, a);
   return hipGetLastError();

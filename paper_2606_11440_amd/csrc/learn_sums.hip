@@ -251,6 +251,7 @@ hipError_t launch_type(const SumArgs& a, int shape, hipStream_t s) {
 }  // namespace
 
 int rows_per_sum(int shape) { return shape == 0 ? Large::BM : (shape == 1 ? Middle::BM : Small::BM); }
+int threads_per_sum(int shape) { return shape == 0 ? Large::NT : (shape == 1 ? Middle::NT : Small::NT); }
 
 // Shape and parts are those with the least time: of the rounds that the blocks
 // take, each of the granules of its part at kAlone us a granule for one block on
