@@ -88,13 +88,10 @@ im_status check_launch(const RowPlan& p) {
   if (p.row_tiles * p.col_tiles * p.splits >= 1 << 30) return fail(IM_EUNSUPPORTED, "2^30 tiles or more");
   return IM_OK;
 }
-im_status check_grid(const SumPlan& p, int64_t groups) {
+im_status check_grid(const SumPlan& p) {
   // a launch has less than 2^32 threads in a dimension
   if (p.parts * p.row_tiles * p.col_tiles * threads_per_sum(p.shape) >= (int64_t)1 << 32)
     return fail(IM_EUNSUPPORTED, "2^32 threads or more");
-  // tiles are the second dimension of the launch that joins
-  if ((p.parts > 1 || groups > 1) && p.row_tiles * p.col_tiles > 65535)
-    return fail(IM_EUNSUPPORTED, "more than 65535 tiles of a gradient in pieces");
   return IM_OK;
 }
 #define LEARN_OK(call)                       \
@@ -127,8 +124,9 @@ SumWork sum_work(int dtype, int64_t n, int64_t G, int64_t M, int64_t N, void* ws
   SumWork w;
   w.plan = plan_sums(dtype, n, G, M, N, compute_units());
   Sections s(ws);
+  // one part cuts no group: it leaves no pieces, only which groups are empty
   const bool joined = w.plan.parts > 1 || (w.plan.parts == 1 && G > 1);
-  w.part = s.take<float>(joined ? 2 * w.plan.parts * w.plan.row_tiles * w.plan.col_tiles * w.plan.piece : 0);
+  w.part = s.take<float>(w.plan.parts > 1 ? 2 * w.plan.parts * w.plan.row_tiles * w.plan.col_tiles * w.plan.piece : 0);
   w.cuts = s.take<int4>(joined ? G : 0);
   if (!joined) w.cuts = nullptr;
   w.bytes = s.used;
@@ -243,7 +241,7 @@ im_status im_linear_backward(const im_linear_desc* d, const int32_t* offsets, co
   const LinearBackward w = linear_backward(*d, ws);
   LEARN_OK(check_work(ws, ws_bytes, w.bytes));
   LEARN_OK(check_launch(w.input.plan));
-  LEARN_OK(check_grid(w.sums.plan, d->n_groups));
+  LEARN_OK(check_grid(w.sums.plan));
   if (dx && some) {
     RowArgs a = row_args(offsets, d->n_groups, d->n_rows, w.input.plan, error);
     a.part = w.input.part;
@@ -479,7 +477,7 @@ im_status im_head_backward(const im_head_desc* d, const int32_t* offsets, const 
   LEARN_OK(check_work(ws, ws_bytes, w.bytes));
   LEARN_OK(check_launch(w.logits));
   LEARN_OK(check_launch(w.input.plan));
-  LEARN_OK(check_grid(w.sums.plan, d->n_groups));
+  LEARN_OK(check_grid(w.sums.plan));
   if (!dh && !dW && !db) return IM_OK;
   const hipStream_t s = (hipStream_t)stream;
   const int64_t V = d->n_classes;

@@ -157,13 +157,13 @@ template <typename T, class S>
 __global__ __launch_bounds__(256) void join_pieces_kernel(const SumArgs a, int share) {
   __shared__ f32x4 sums[256];
   constexpr int kQuads = (S::BM * S::BN + S::BM) / 4, kTile = S::BM * S::BN / 4;
-  const int tiles = a.row_tiles * a.col_tiles, g = blockIdx.z, tile = blockIdx.y;
+  const int tiles = a.row_tiles * a.col_tiles, g = blockIdx.z, tile = blockIdx.x;   // only x holds more than 65535
   const int4 cut = a.cuts ? a.cuts[g] : int4{0, -1, 0, 0};   // no rows at all: zeros
   const int p0 = cut.x, p1 = cut.y, from = cut.z;   // its parts; 1: the first of them begins in a group before it
   if (p0 == p1) return;   // stored already
   const int wide = 256 / share, at = (int)threadIdx.x % wide, turn = threadIdx.x / wide;
   const int rt = tile / a.col_tiles, ct = tile % a.col_tiles;
-  for (int q0 = blockIdx.x * wide; q0 < kQuads; q0 += gridDim.x * wide) {
+  for (int q0 = blockIdx.y * wide; q0 < kQuads; q0 += gridDim.y * wide) {
     const int q = q0 + at;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     const bool in = q < kTile ? a.dW != nullptr : (q < kQuads && a.db && ct == 0);
@@ -235,7 +235,7 @@ hipError_t launch(const SumArgs& a, hipStream_t s) {
   // blocks for a tile: some thousands in all
   const int quads = (S::BM * S::BN + S::BM) / 4, wide = 256 / share, most = (quads + wide - 1) / wide;
   const int64_t each = 4096 / ((int64_t)tiles * a.G) + 1;
-  hipLaunchKernelGGL((join_pieces_kernel<T, S>), dim3((unsigned)(each < most ? each : most), (unsigned)tiles, (unsigned)a.G),
+  hipLaunchKernelGGL((join_pieces_kernel<T, S>), dim3((unsigned)tiles, (unsigned)(each < most ? each : most), (unsigned)a.G),
                      dim3(256), 0, s, a, share);
   return hipGetLastError();
 }

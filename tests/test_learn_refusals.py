@@ -97,6 +97,16 @@ def test_layer_arguments():
     assert f(R(big), None, A, A, A, A, None, 0, None, None) == P._lib.IM_EUNSUPPORTED
 
 
+@pytest.mark.parametrize("G,n,k,m", [(8, 16384, 4096, 16384), (2, 4096, 16384, 16384), (64, 64, 2048, 4096)])
+def test_gradients_that_no_run_cuts_need_no_pieces(G, n, k, m):
+    """As many tiles as fill the card: every group's sum is one block's, and the
+    workspace is the groups' records (16 bytes each) alone."""
+    need = ctypes.c_int64(0)
+    d = linear_desc(n_groups=G, n_rows=n, in_dim=k, out_dim=m, ld_x=k, ld_y=m, ld_dx=k)
+    assert L().im_linear_workspace(ctypes.byref(d), 1, ctypes.byref(need)) == 0
+    assert 0 < need.value <= (16 * G + 255) // 256 * 256
+
+
 def test_head_arguments():
     R = ctypes.byref
     d = head_desc()
