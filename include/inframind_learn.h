@@ -17,7 +17,9 @@
  * Conventions for every call:
  *   - Pointers are device memory of the current device unless marked "host";
  *     caller-owned buffers must stay valid until the stream work that uses
- *     them has finished. Outputs must not overlap inputs or one another.
+ *     them has finished. What a call writes (outputs, workspace, error) must not
+ *     overlap what it reads or one another (refused); views of the same rows that
+ *     take different columns do not overlap.
  *   - Matrices are row-major. ld_* are row strides in elements (at least the
  *     row's width, at most IM_MAX_LD); weights and their gradients are contiguous. 16-bit data
  *     needs 2-byte, 32-bit data 4-byte alignment, nothing more.

@@ -4,6 +4,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "learn_adamw.h"
@@ -94,6 +95,49 @@ im_status check_grid(const SumPlan& p) {
     return fail(IM_EUNSUPPORTED, "2^32 threads or more");
   return IM_OK;
 }
+// Memory that a call reads or writes: rows of `width` bytes, `stride` bytes apart.
+struct Area {
+  const char* name;
+  const void* at;
+  int64_t rows, width, stride;
+  bool written;
+};
+Area flat(const char* name, const void* p, int64_t bytes, bool written) { return Area{name, p, 1, bytes, bytes, written}; }
+Area matrix(const char* name, const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t e, bool written) {
+  if (rows > 1 && ld > cols) return Area{name, p, rows, cols * e, ld * e, written};
+  return flat(name, p, rows * cols * e, written);
+}
+
+// Whether two areas share a byte. Views of the same rows that take different
+// columns do not.
+bool meet(const Area* a, const Area* b) {
+  if (reinterpret_cast<uintptr_t>(a->at) > reinterpret_cast<uintptr_t>(b->at)) std::swap(a, b);
+  if (!a->at || !b->at || a->rows * a->width == 0 || b->rows * b->width == 0) return false;
+  const int64_t by = (int64_t)(reinterpret_cast<uintptr_t>(b->at) - reinterpret_cast<uintptr_t>(a->at));
+  if (by >= (a->rows - 1) * a->stride + a->width) return false;
+  if (a->rows == 1) return true;   // b begins in it
+  if (b->rows == 1 || b->stride == a->stride) {   // b's first row: in a row of a, or behind it and into the next
+    const int64_t row = by / a->stride, column = by % a->stride;
+    return column < a->width || (column + b->width > a->stride && row + 1 < a->rows);
+  }
+  for (int64_t i = 0, j = 0; i < a->rows && j < b->rows;) {   // rows of both in their order
+    const int64_t x = i * a->stride, y = by + j * b->stride;
+    if (x + a->width <= y) ++i;
+    else if (y + b->width <= x) ++j;
+    else return true;
+  }
+  return false;
+}
+
+// Nothing that a call writes lies in anything else of the call: its blocks run side by side.
+template <size_t N>
+im_status check_areas(const Area (&areas)[N]) {
+  for (size_t i = 0; i < N; ++i)
+    for (size_t j = areas[i].written && areas[i].at ? 0 : N; j < N; ++j)
+      if (i != j && meet(&areas[i], &areas[j])) return fail(IM_EINVAL, "%s overlaps %s", areas[i].name, areas[j].name);
+  return IM_OK;
+}
+
 #define LEARN_OK(call)                       \
   do {                                       \
     const im_status _s = (call);             \
@@ -202,9 +246,16 @@ im_status im_linear_forward(const im_linear_desc* d, const int32_t* offsets, con
   LEARN_CHECK(aligned(x, e) && aligned(W, e) && aligned(y, e) && aligned(b, 4) && aligned(error, 4),
               "a pointer is not aligned to its elements");
   const RowWork w = linear_forward(*d, ws);
+  const int64_t n = d->n_rows, G = d->n_groups, k = d->in_dim, m = d->out_dim;
+  if (n > 0) {
+    LEARN_OK(check_launch(w.plan));
+    LEARN_OK(check_areas({flat("offsets", offsets, 4 * (G + 1), false), matrix("x", x, n, k, d->ld_x, e, false),
+                          flat("W", W, G * m * k * e, false), flat("b", b, 4 * G * m, false),
+                          matrix("y", y, n, m, d->ld_y, e, true), flat("workspace", ws, w.bytes, true),
+                          flat("error", error, 4, true)}));
+  }
   LEARN_OK(check_work(ws, ws_bytes, w.bytes));
-  if (d->n_rows == 0) return IM_OK;
-  LEARN_OK(check_launch(w.plan));
+  if (n == 0) return IM_OK;
   RowArgs a = row_args(offsets, d->n_groups, d->n_rows, w.plan, error);
   a.part = w.part;
   a.K = d->in_dim;
@@ -239,9 +290,16 @@ im_status im_linear_backward(const im_linear_desc* d, const int32_t* offsets, co
                   aligned(error, 4),
               "a pointer is not aligned to its elements");
   const LinearBackward w = linear_backward(*d, ws);
-  LEARN_OK(check_work(ws, ws_bytes, w.bytes));
   LEARN_OK(check_launch(w.input.plan));
   LEARN_OK(check_grid(w.sums.plan));
+  const int64_t n = d->n_rows, G = d->n_groups, k = d->in_dim, m = d->out_dim;
+  const bool reads_x = dW || (dx && d->relu_in);
+  LEARN_OK(check_areas({flat("offsets", offsets, 4 * (G + 1), false), matrix("dy", dy, n, m, d->ld_y, e, false),
+                        matrix("x", reads_x ? x : nullptr, n, k, d->ld_x, e, false),
+                        flat("W", dx ? W : nullptr, G * m * k * e, false), matrix("dx", dx, n, k, d->ld_dx, e, true),
+                        flat("dW", dW, G * m * k * e, true), flat("db", db, 4 * G * m, true),
+                        flat("workspace", ws, w.bytes, true), flat("error", error, 4, true)}));
+  LEARN_OK(check_work(ws, ws_bytes, w.bytes));
   if (dx && some) {
     RowArgs a = row_args(offsets, d->n_groups, d->n_rows, w.input.plan, error);
     a.part = w.input.part;
@@ -398,8 +456,15 @@ im_status im_head_forward(const im_head_desc* d, const int32_t* offsets, const v
               "a pointer is not aligned to its elements");
   if (d->n_rows == 0) return IM_OK;
   const HeadForward w = head_forward(*d, ws);
-  LEARN_OK(check_work(ws, ws_bytes, w.bytes));
   LEARN_OK(check_launch(w.plan));
+  const int64_t n = d->n_rows, G = d->n_groups, k = d->dim, V = d->n_classes;
+  LEARN_OK(check_areas({flat("offsets", offsets, 4 * (G + 1), false), matrix("h", h, n, k, d->ld_h, e, false),
+                        flat("W", W, G * V * k * e, false), flat("b", b, 4 * G * V, false),
+                        flat("valid", valid, 4 * n * ((V + 31) / 32), false), flat("target", target, 4 * n, false),
+                        flat("logp", logp, 4 * n, true), flat("entropy", entropy, 4 * n, true),
+                        flat("lse", lse, 4 * n, true), flat("workspace", ws, w.bytes, true),
+                        flat("error", error, 4, true)}));
+  LEARN_OK(check_work(ws, ws_bytes, w.bytes));
   RowArgs a = row_args(offsets, d->n_groups, d->n_rows, w.plan, error);
   a.K = d->dim;
   a.N = a.V = d->n_classes;
@@ -437,8 +502,21 @@ im_status im_head_backward(const im_head_desc* d, const int32_t* offsets, const 
                   aligned(target, 4) && aligned(lse, 4) && aligned(entropy, 4) && aligned(dlogp, 4) &&
                   aligned(dentropy, 4) && aligned(db, 4) && aligned(error, 4),
               "a pointer is not aligned to its elements");
+  const int64_t V = d->n_classes;
+  const auto check_outputs = [&](int64_t ws_need) {
+    const int64_t n = d->n_rows, G = d->n_groups, k = d->dim;
+    return check_areas({flat("offsets", offsets, 4 * (G + 1), false), matrix("h", h, n, k, d->ld_h, e, false),
+                        flat("W", W, G * V * k * e, false), flat("b", b, 4 * G * V, false),
+                        flat("valid", valid, 4 * n * ((V + 31) / 32), false), flat("target", target, 4 * n, false),
+                        flat("lse", lse, 4 * n, false), flat("entropy", dentropy ? entropy : nullptr, 4 * n, false),
+                        flat("dlogp", dlogp, 4 * n, false), flat("dentropy", dentropy, 4 * n, false),
+                        matrix("dh", dh, n, k, d->ld_dh, e, true), flat("dW", dW, G * V * k * e, true),
+                        flat("db", db, 4 * G * V, true), flat("workspace", ws, ws_need, true),
+                        flat("error", error, 4, true)});
+  };
   if (narrow(*d)) {
     const NarrowWork w = narrow_work(*d, ws);
+    LEARN_OK(check_outputs(w.bytes));
     LEARN_OK(check_work(ws, ws_bytes, w.bytes));
     if (!dh && !dW && !db) return IM_OK;
     NarrowArgs a = {};
@@ -474,13 +552,13 @@ im_status im_head_backward(const im_head_desc* d, const int32_t* offsets, const 
     return IM_OK;
   }
   const HeadBackward w = head_backward(*d, ws);
-  LEARN_OK(check_work(ws, ws_bytes, w.bytes));
   LEARN_OK(check_launch(w.logits));
   LEARN_OK(check_launch(w.input.plan));
   LEARN_OK(check_grid(w.sums.plan));
+  LEARN_OK(check_outputs(w.bytes));
+  LEARN_OK(check_work(ws, ws_bytes, w.bytes));
   if (!dh && !dW && !db) return IM_OK;
   const hipStream_t s = (hipStream_t)stream;
-  const int64_t V = d->n_classes;
   for (int64_t piece = 0; piece < w.pieces; ++piece) {
     const int64_t c0 = piece * w.width, width = V - c0 < w.width ? V - c0 : w.width;
     const char* Wp = static_cast<const char*>(W) + c0 * d->dim * e;

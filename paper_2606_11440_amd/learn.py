@@ -7,7 +7,8 @@ handle) is given, on torch's current stream of that device. `workspace` is
 taken from torch's allocator where it is not given; calls that may run at the
 same time need one each. `error` is a device int32 tensor [1] that collects
 IM_ERR_* bits. Invalid arguments raise IMError with status IM_EINVAL and change
-nothing.
+nothing; outputs that overlap an input or one another are such (columns side by
+side in one buffer are not).
 
 The functions keep the C names (im_linear_forward, im_linear_backward,
 im_head_forward, im_head_backward); AdamW holds an im_adamw plan."""

@@ -131,6 +131,76 @@ def test_head_arguments():
     assert b(R(head_desc(ld_dh=2)), *ok[1:]) == EINVAL
 
 
+def at(p):
+    return None if p is None else ctypes.c_void_p(p)
+
+
+FAR = 1 << 30     # between buffers that do not overlap
+
+
+def test_matrices_overlap_only_where_they_share_a_byte():
+    """Views of one buffer, against a count of their elements. Calls that are not
+    refused for an overlap are for their missing workspace: nothing runs."""
+    import random
+    rng, seen = random.Random(3), [0, 0]
+
+    def cells(first, rows, cols, ld):
+        return {first + r * ld + c for r in range(rows) for c in range(cols)}
+    for _ in range(4000):
+        n, k, m = rng.randint(1, 7), rng.randint(1, 5), rng.randint(1, 5)
+        lds = [rng.randint(w, 14) for w in (m, k, k)]
+        if rng.random() < 0.6:
+            lds = [max(lds)] * 3
+        place = [rng.randint(0, 70) for _ in range(3)]
+        dy, x, dx = (cells(a, n, w, ld) for a, w, ld in zip(place, (m, k, k), lds))
+        d = linear_desc(n_groups=2, n_rows=n, in_dim=k, out_dim=m, dtype=P._lib.IM_F32, relu_in=1, ld_y=lds[0], ld_x=lds[1],
+                        ld_dx=lds[2])
+        pdy, px, pdx = (at((1 << 20) + 4 * a) for a in place)
+        status = L().im_linear_backward(ctypes.byref(d), at(FAR), pdy, px, at(2 * FAR), pdx, None, None, None, 0, None, None)
+        assert status == EINVAL
+        msg, want = P.im_learn_last_error(), bool(dx & (dy | x))
+        assert ("overlaps" if want else "workspace") in msg, (n, k, m, lds, place, msg)
+        seen[want] += 1
+    assert min(seen) > 1000
+
+
+def test_outputs_do_not_overlap_anything():
+    """Each output, the workspace and the error word on each other buffer of the call;
+    buffers that a call does not read may lie anywhere."""
+    R, n, k, m, G = ctypes.byref, 40, 16, 24, 2
+
+    def refused(f, desc, names, outputs, unused=(), more=()):
+        base = {name: (i + 1) * FAR for i, name in enumerate(names)}
+        def call(over, ws=0):    # noqa: E306
+            p = {k: at(v) for k, v in (base | over).items()}
+            return f(R(desc), *[p[name] for name in names[:-1]], ws, p["error"], None)
+        # nothing overlaps: the call ends at its workspace's size
+        assert call({}) == EINVAL and "workspace of" in P.im_learn_last_error()
+        for a in outputs:
+            for b in names:
+                if a == b or base[b] is None:
+                    continue
+                status = call({a: base[b]}, 1 << 40)
+                assert status == EINVAL and "overlaps" in P.im_learn_last_error(), (a, b, P.im_learn_last_error())
+        for a, b in unused:
+            assert call({a: base[b]} | dict(more)) == EINVAL and "workspace of" in P.im_learn_last_error(), (a, b)
+
+    layer = linear_desc(n_groups=G, n_rows=n, in_dim=4096, out_dim=m, ld_x=4096)       # in runs of k: a workspace
+    refused(L().im_linear_forward, layer, ["offsets", "x", "W", "b", "y", "workspace", "error"], ["y", "workspace", "error"])
+    back = linear_desc(n_groups=G, n_rows=n, relu_in=1)
+    names = ["offsets", "dy", "x", "W", "dx", "dW", "db", "workspace", "error"]
+    refused(L().im_linear_backward, back, names, ["dx", "dW", "db", "workspace", "error"])
+    refused(L().im_linear_backward, back, names, [], unused=[("db", "W"), ("db", "x")], more=[("dx", None), ("dW", None)])
+    names = ["offsets", "h", "W", "b", "valid", "target", "logp", "entropy", "lse", "workspace", "error"]
+    refused(L().im_head_forward, head_desc(n_groups=G, n_rows=n, n_classes=1000), names,
+            ["logp", "entropy", "lse", "workspace", "error"])
+    names = ["offsets", "h", "W", "b", "valid", "target", "lse", "entropy", "dlogp", "dentropy", "dh", "dW", "db", "workspace",
+             "error"]
+    for V in (24, 100):     # in one pass, and in pieces of the classes
+        refused(L().im_head_backward, head_desc(n_groups=G, n_rows=n, n_classes=V), names, ["dh", "dW", "db", "workspace", "error"],
+                unused=[("dh", "entropy")], more=[("dentropy", None)])
+
+
 def tensor(**kw):
     t = learn.ImAdamwTensor(4096, 4096, 4096, 4096, None, None, None, 10, 1, 0)
     for k, v in kw.items():
