@@ -194,7 +194,8 @@ im_status im_adamw_create(const im_adamw_tensor* tensors, int32_t n_tensors, int
 im_status im_adamw_step(im_adamw* opt, double lr, double beta1, double beta2, double eps,
                         double weight_decay, int64_t* step, const float* scale, void* stream);
 
-/* Free the plan (synchronises; the tensors stay). NULL is ignored. */
+/* Free the plan (synchronises the device, so not while a graph is captured; the
+ * tensors stay). NULL is ignored. */
 void im_adamw_destroy(im_adamw* opt);
 
 /* Description of the calling thread's last failed call of this header. Never NULL. */

@@ -3,7 +3,8 @@ learner's operators. Argument checks and marshalling only; the work is done by
 the library's HIP kernels, on torch tensors that the caller owns.
 
 A call runs on its tensors' device and, unless `stream` (a raw HIP stream
-handle) is given, on torch's current stream of that device. `workspace` is
+handle) is given, on torch's current stream of that device; tensors used on
+another stream than their own have to be kept until that work is done. `workspace` is
 taken from torch's allocator where it is not given; calls that may run at the
 same time need one each. `error` is a device int32 tensor [1] that collects
 IM_ERR_* bits. Invalid arguments raise IMError with status IM_EINVAL and change
@@ -293,6 +294,17 @@ def im_head_backward(h, W, b, target, lse, dlogp, dh=None, dW=None, db=None, val
                                  _stream(stream)))
 
 
+# Plans whose AdamW was dropped. To free one synchronises the device, which would spoil a graph
+# capture wherever the garbage collector happens to run: the next plan's creation, which
+# synchronises itself, frees them.
+_dropped = []
+
+
+def _free_dropped():
+    while _dropped:
+        load_learn().im_adamw_destroy(_dropped.pop())
+
+
 class AdamW:
     """AdamW over a list of tensors, one launch a step.
 
@@ -305,7 +317,8 @@ class AdamW:
       copy    optional bfloat16 tensor that receives the rounded parameters
       decay   whether weight decay applies (default True)
     They are kept alive by this object and keep their places. States that are all
-    zero start a run."""
+    zero start a run. Creating a plan and close() synchronise (not while a graph is
+    captured); a graph with a step in it needs the plan for its replays."""
 
     def __init__(self, tensors, bits=32, stream=None):
         self.h = None
@@ -335,6 +348,7 @@ class AdamW:
                                      1 if t.get("decay", True) else 0, 0)
         self.tensors, self.device, self.bits = tensors, dev, bits
         out = _P()
+        _free_dropped()
         with _On(_index(dev)):
             _done(L.im_adamw_create(table, len(tensors), bits, kind, _stream(stream), ctypes.byref(out)))
         self.h = out
@@ -352,15 +366,14 @@ class AdamW:
                                        _flat(scale, "scale", _KINDS["f32"], dev, 1), _stream(stream)))
 
     def close(self):
-        if getattr(self, "h", None):
+        if self.h:
             load_learn().im_adamw_destroy(self.h)
             self.h = None
 
     def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
+        if getattr(self, "h", None) and _dropped is not None:   # None: the interpreter ends
+            _dropped.append(self.h)
+            self.h = None
 
 
 def _bf16():

@@ -209,3 +209,33 @@ def test_refusals():
     opt.close()
     with pytest.raises(P.IMError):
         opt.step(step, **HYPER)
+
+
+def test_a_plan_dropped_while_a_graph_is_captured():
+    import gc
+
+    import paper_2606_11440_amd as P
+    torch = need_gpu()
+    note("[adamw dropped]")
+    ts = tensors([5000, 300], 32, False, seed=9)
+    start, step = clone(ts), torch.zeros(1, dtype=torch.int64, device="cuda")
+    opt, other = P.AdamW(ts), P.AdamW(tensors([100], 8, True, seed=10), bits=8)
+    other.step(torch.zeros(1, dtype=torch.int64, device="cuda"), **HYPER)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step(step, **HYPER)
+        del other
+        gc.collect()
+    for k in range(3):
+        old = clone(ts)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(step) == k + 1
+        check(ts, old, 32, k + 1, 1.0)
+    again, count = clone(start), torch.zeros(1, dtype=torch.int64, device="cuda")
+    eager = P.AdamW(again)
+    for _ in range(3):
+        eager.step(count, **HYPER)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a["param"], b["param"]) for a, b in zip(again, ts))

@@ -264,3 +264,24 @@ def test_tensors_are_checked():
         P.AdamW([dict(param=x, grad=x, m=x, v=x)])
     with pytest.raises(P.IMError):
         P.AdamW([], bits=4)
+
+
+def test_dropped_plans_wait_for_the_next(monkeypatch):
+    """The garbage collector frees no plan: that synchronises, and would spoil a capture."""
+    freed = []
+
+    class Library:
+        @staticmethod
+        def im_adamw_destroy(h):
+            freed.append(h.value)
+    monkeypatch.setattr(learn, "_learn", Library)
+    monkeypatch.setattr(learn, "_dropped", [])
+    for h in (16, 32, 48):
+        opt = P.AdamW.__new__(P.AdamW)
+        opt.h = ctypes.c_void_p(h)
+        if h == 32:
+            opt.close()
+        del opt
+    assert freed == [32]
+    learn._free_dropped()
+    assert sorted(freed) == [16, 32, 48] and not learn._dropped
