@@ -25,7 +25,8 @@ from ._lib import (EXPORTED, IMError, im_clear_error, im_destroy, im_dual_update
                    make_arrivals,
                    make_desc)
 from .learn import (LEARN_EXPORTED, AdamW, im_head_backward, im_head_forward,  # noqa: F401
-                    im_learn_last_error, im_linear_backward, im_linear_forward)
+                    im_head_workspace, im_learn_last_error, im_linear_backward, im_linear_forward,
+                    im_linear_workspace)
 
 
 def device_arrivals(arr: dict, device="cuda"):

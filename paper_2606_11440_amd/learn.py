@@ -12,7 +12,8 @@ nothing; outputs that overlap an input or one another are such (columns side by
 side in one buffer are not).
 
 The functions keep the C names (im_linear_forward, im_linear_backward,
-im_head_forward, im_head_backward); AdamW holds an im_adamw plan."""
+im_head_forward, im_head_backward, and im_linear_workspace and im_head_workspace
+for the size of a workspace that a program keeps); AdamW holds an im_adamw plan."""
 from __future__ import annotations
 
 import ctypes
@@ -191,6 +192,41 @@ def _workspace(query, desc, key, backward, workspace, device, stream):
         with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=device)):
             t = torch.empty(need, dtype=torch.uint8, device=device)
     return t, t.data_ptr(), need
+
+
+def _size_of(query, desc, backward, device):
+    out = _I64(0)
+    if device is None:
+        _done(query(ctypes.byref(desc), 1 if backward else 0, ctypes.byref(out)))
+    else:
+        import torch
+        device = torch.device(device)
+        if device.type != "cuda":
+            _bad(f"device is {device}, a GPU is expected")
+        with _On(torch.cuda.current_device() if device.index is None else device.index):
+            _done(query(ctypes.byref(desc), 1 if backward else 0, ctypes.byref(out)))
+    return out.value
+
+
+def _kind_of(dtype):
+    import torch
+    if dtype not in (torch.float32, torch.bfloat16):
+        _bad(f"dtype is {dtype}: float32 or bfloat16 expected")
+    return IM_F32 if dtype is torch.float32 else IM_BF16
+
+
+def im_linear_workspace(n_rows, in_dim, out_dim, dtype, n_groups=1, backward=False, device=None):
+    """Bytes of workspace of im_linear_forward, or im_linear_backward, on `device`
+    (None: the current one). A buffer for several calls takes the largest of
+    theirs: fewer rows may need more."""
+    d = ImLinearDesc(n_groups, n_rows, in_dim, out_dim, _kind_of(dtype), 0, 0, 0, in_dim, out_dim, in_dim)
+    return _size_of((_learn or load_learn()).im_linear_workspace, d, backward, device)
+
+
+def im_head_workspace(n_rows, dim, n_classes, dtype, n_groups=1, backward=False, device=None):
+    """Bytes of workspace of im_head_forward, or im_head_backward; as im_linear_workspace."""
+    d = ImHeadDesc(n_groups, n_rows, dim, n_classes, _kind_of(dtype), 0, 0, 0, dim, dim)
+    return _size_of((_learn or load_learn()).im_head_workspace, d, backward, device)
 
 
 def im_linear_forward(x, W, b, y, offsets=None, relu=False, workspace=None, error=None, stream=None):

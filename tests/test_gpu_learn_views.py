@@ -1,5 +1,6 @@
-"""GPU: outputs and inputs in one buffer: side by side they give what separate
-buffers give, bit for bit; on one another the call is refused."""
+"""GPU: buffers that the caller lays out. Outputs and inputs in one buffer: side
+by side they give what separate buffers give, bit for bit; on one another the
+call is refused. Workspaces of just the size that a call asks for."""
 import pytest
 
 from gpu_util import need_gpu, note
@@ -51,3 +52,49 @@ def test_overlaps_are_refused():
         assert e.value.status == P._lib.IM_EINVAL and "overlaps" in str(e.value)
     torch.cuda.synchronize()
     assert torch.equal(x, keep)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,G,k,V", [(16, 1, 4096, 256), (3000, 5, 256, 15), (900, 3, 200, 700)])
+def test_workspaces_of_just_their_size(n, G, k, V, dtype):
+    """One call of each after the other in one buffer: its end stays as it was, and
+    a byte less is refused."""
+    import paper_2606_11440_amd as P
+    torch = need_gpu()
+    note(f"[workspaces] n={n} G={G} {k} -> {V} {dtype}")
+    g = torch.Generator(device="cuda").manual_seed(n)
+    dt = getattr(torch, dtype)
+    x, dy, W = (torch.randn(*s, device="cuda", generator=g).to(dt) for s in ((n, k), (n, V), (G, V, k)))
+    b, target = torch.randn(G, V, device="cuda", generator=g), torch.randint(V, (n,), device="cuda", generator=g, dtype=torch.int32)
+    off = torch.arange(G + 1, device="cuda", dtype=torch.int32) * (n // G)
+    f = [torch.zeros(n, device="cuda") for _ in range(6)]
+    f[3].normal_(generator=g)
+    f[4].normal_(generator=g)
+    out = {}
+
+    def calls(tag, buffer):
+        y, dx, dW, db, dh = (torch.zeros_like(t) for t in (dy, x, W, b, x))
+        kw = lambda size: dict(offsets=off, workspace=buffer(size))  # noqa: E731
+        P.im_linear_forward(x, W, b, y, **kw(P.im_linear_workspace(n, k, V, dt, G)))
+        P.im_linear_backward(dy, x, W, dx, dW, db, **kw(P.im_linear_workspace(n, k, V, dt, G, backward=True, device=x.device)))
+        out[tag] = [y, dx, dW.clone(), db.clone()]
+        P.im_head_forward(x, W, b, target, f[0], f[1], f[2], **kw(P.im_head_workspace(n, k, V, dt, G)))
+        P.im_head_backward(x, W, b, target, f[2], f[3], dh, dW, db, entropy=f[1], dentropy=f[4],
+                           **kw(P.im_head_workspace(n, k, V, dt, G, backward=True, device="cuda")))
+        torch.cuda.synchronize()
+        out[tag] += [dh, dW, db] + [t.clone() for t in f[:3]]
+    whole = torch.empty(1 << 27, dtype=torch.uint8, device="cuda")
+
+    def exact(size):
+        assert size < len(whole)
+        whole[size:].fill_(77)
+        sizes.append(size)
+        return whole[:size]
+    sizes = []
+    calls("own", lambda size: None)
+    calls("exact", exact)
+    assert all(torch.equal(a, b) for a, b in zip(out["own"], out["exact"]))
+    assert bool((whole[sizes[-1]:] == 77).all()) and max(sizes) > 0
+    with pytest.raises(P.IMError) as e:
+        P.im_head_backward(x, W, b, target, f[2], f[3], torch.zeros_like(x), offsets=off, workspace=whole[:sizes[-1] - 1])
+    assert "workspace" in str(e.value)

@@ -285,3 +285,21 @@ def test_dropped_plans_wait_for_the_next(monkeypatch):
     assert freed == [32]
     learn._free_dropped()
     assert sorted(freed) == [16, 32, 48] and not learn._dropped
+
+
+def test_workspace_sizes():
+    import torch
+    out = ctypes.c_int64(0)
+    for G, n, dt in ((1, 16, torch.bfloat16), (3, 5000, torch.float32), (64, 20000, torch.bfloat16)):
+        for back in (0, 1):
+            d = linear_desc(n_groups=G, n_rows=n, in_dim=4096, out_dim=256, dtype=int(dt is torch.bfloat16), ld_x=4096, ld_y=256)
+            assert L().im_linear_workspace(ctypes.byref(d), back, ctypes.byref(out)) == 0
+            assert P.im_linear_workspace(n, 4096, 256, dt, G, backward=bool(back)) == out.value
+            d = head_desc(n_groups=G, n_rows=n, dim=96, n_classes=5000, dtype=int(dt is torch.bfloat16), ld_h=96, ld_dh=96)
+            assert L().im_head_workspace(ctypes.byref(d), back, ctypes.byref(out)) == 0
+            assert P.im_head_workspace(n, 96, 5000, dt, G, backward=bool(back)) == out.value > 0
+    for call in (lambda: P.im_linear_workspace(-1, 8, 8, torch.float32), lambda: P.im_linear_workspace(1, 8, 8, torch.float16),
+                 lambda: P.im_head_workspace(1, 8, 0, torch.float32), lambda: P.im_head_workspace(1, 8, 8, torch.float32, device="cpu")):
+        with pytest.raises(P.IMError) as e:
+            call()
+        assert e.value.status == EINVAL
