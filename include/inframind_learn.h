@@ -149,7 +149,8 @@ im_status im_head_backward(const im_head_desc* desc, const int32_t* offsets, con
  * One step over many tensors in one launch:
  *   g = scale grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
  *   param = (1 - lr weight_decay) param - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
- * in fp32 (root and quotient of the last line to 2 units); t is the step's number.
+ * in fp32 (root and quotient of the last line to 2 units, an eps above 0 is 2^-126 at
+ * least); t is the step's number.
  *   param  fp32 [n]; grad fp32 or bf16 [n]; copy bf16 [n] (the parameters
  *          rounded for the bf16 products), or NULL
  *   state_bits 32: m, v fp32 [n]; m_scale, v_scale NULL

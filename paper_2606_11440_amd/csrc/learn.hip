@@ -1,5 +1,6 @@
 // C ABI of the learner's operators: checks of arguments, workspaces, launches.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -811,7 +812,7 @@ im_status im_adamw_step(im_adamw* o, double lr, double beta1, double beta2, doub
   a.omb1 = (float)(1.0 - beta1);
   a.beta2f = (float)beta2;
   a.omb2 = (float)(1.0 - beta2);
-  a.eps = (float)eps;
+  a.eps = eps > 0 ? std::max((float)eps, FLT_MIN) : 0.f;   // subnormal: zero states would give 0 times infinity
   a.keep = (float)(1.0 - lr * weight_decay);
   const OnDevice on(o->device);
   LEARN_HIP(on.err);

@@ -111,6 +111,14 @@ __device__ __forceinline__ uint32_t encode(f32x4 y, bool least, float& scale) {
   return to_e4m3(x);
 }
 
+// Square root to 1 unit. The instruction takes what lies below 2^-126 for 0 (there
+// a v is of gradients below 1e-19, and their quotient would be infinite): such go in scaled.
+__device__ __forceinline__ float root(float x) {
+  const bool small = x < 0x1p-96f;
+  const float r = __builtin_amdgcn_sqrtf(small ? x * 0x1p64f : x);
+  return small ? r * 0x1p-32f : r;
+}
+
 // x^t by squaring: relative error below t 2^-52, and t x^t is bounded.
 __device__ __forceinline__ double power(double x, int64_t t) {
   double y = 1.0;
@@ -188,7 +196,7 @@ struct Step {
         f.v[i] = f.v[i] * a.beta2f + g * g * a.omb2;
       }
       // root and reciprocal to 1 unit: the parameter's own rounding is coarser
-      const float d = __builtin_amdgcn_sqrtf(f.v[i] * r2) + a.eps;
+      const float d = root(f.v[i] * r2) + a.eps;   // 0 or 2^-126 at least: the reciprocal takes those
       f.p[i] = f.p[i] * keep - f.m[i] * r1 * __builtin_amdgcn_rcpf(d) * a.lr;
     }
     store_f(param + e, f.p, left, al);
@@ -211,7 +219,7 @@ struct Step {
       f32x4 r;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        r[i] = i < left ? __builtin_amdgcn_sqrtf(f.v[i]) : 0.f;
+        r[i] = i < left ? root(f.v[i]) : 0.f;
         f.m[i] = i < left ? f.m[i] : 0.f;
       }
       float ms, vs;

@@ -239,3 +239,53 @@ def test_a_plan_dropped_while_a_graph_is_captured():
         eager.step(count, **HYPER)
     torch.cuda.synchronize()
     assert all(torch.equal(a["param"], b["param"]) for a, b in zip(again, ts))
+
+
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-45])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_gradients_whose_squares_are_subnormal(bits, eps, half):
+    """Gradients of 1e-20 to 1e-17 have v down to 1e-42, which the formula divides by
+    like any other. There a rounding is half of 2^-149: up to four of those in v
+    (the square, its product with 1 - beta2, the state's with beta2, a decoded
+    state's square), half of their share of v in its root."""
+    import paper_2606_11440_amd as P
+    torch = need_gpu()
+    note(f"[adamw subnormal] bits={bits} eps={eps} half={half}")
+    t = tensors([3000], bits, half, seed=3)[0]
+    g = torch.Generator(device="cuda").manual_seed(4)
+    size = 10.0 ** (-20 + 3 * torch.rand(3000, device="cuda", generator=g, dtype=torch.float64))
+    t["grad"] = (size * t["grad"].double().sign()).to(t["grad"].dtype)
+    t["grad"][t["grad"] == 0] = 1e-18
+    for k in ("m", "v", "m_scale", "v_scale"):
+        if k in t:
+            t[k].view(torch.uint8).zero_() if t[k].dtype == torch.float8_e4m3fn else t[k].zero_()
+    opt, step, h = P.AdamW([t], bits=bits), torch.zeros(1, dtype=torch.int64, device="cuda"), HYPER | dict(eps=eps)
+    lost = 4 * 2.0 ** -150
+    for k in range(1, 4):
+        old = clone([t])[0]
+        opt.step(step, **h)
+        torch.cuda.synchronize()
+        r = expected(old, bits, k, 1.0, h)
+        up = (r["p"] - old["param"].double() * (1 - h["lr"] * h["weight_decay"])).abs()
+        U.close(t["param"], r["p"], r["ep"] + up * lost / (2 * r["v"] - lost), f"param, step {k}")
+        if bits == 32:
+            U.close(t["v"], r["v"], r["ev"] + lost, "v")
+        else:
+            assert bool((t["v"].float() > 0).all())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_zero_states_and_gradients_with_the_least_eps(bits):
+    """0 / eps is 0 for every eps above 0."""
+    import paper_2606_11440_amd as P
+    torch = need_gpu()
+    for eps in (5e-324, 1e-45, 1e-39, 1e-38):
+        t = tensors([600], bits, False, seed=5)[0]
+        for k in ("m", "v", "m_scale", "v_scale", "grad"):
+            if k in t:
+                t[k].view(torch.uint8).zero_() if t[k].dtype == torch.float8_e4m3fn else t[k].zero_()
+        before = t["param"].clone()
+        P.AdamW([t], bits=bits).step(torch.zeros(1, dtype=torch.int64, device="cuda"), lr=0.01, eps=eps, weight_decay=0.0)
+        torch.cuda.synchronize()
+        assert torch.equal(t["param"], before), eps
