@@ -498,10 +498,7 @@ __global__ __launch_bounds__(256) void join_kernel(const RowArgs a) {
   const int r = threadIdx.x % 16, part = threadIdx.x / 16;
   int end = a.n;
   if (a.offsets) {
-    Part run;
-    bool bad;
-    find_part(a.offsets, a.G, a.n, 1, 0, run, bad);
-    if (bad) return;
+    if (!csr_holds(a.offsets, a.G, a.n)) return;
     end = a.offsets[a.G];
   }
   for (int64_t first = (int64_t)blockIdx.x * 16; first < end; first += (int64_t)gridDim.x * 16) {
@@ -533,10 +530,7 @@ __global__ __launch_bounds__(256) void join_k_kernel(const RowArgs a) {
   const int across = (a.N + 3) / 4;
   int end = a.n;
   if (a.offsets) {
-    Part run;
-    bool bad;
-    find_part(a.offsets, a.G, a.n, 1, 0, run, bad);
-    if (bad) return;
+    if (!csr_holds(a.offsets, a.G, a.n)) return;
     end = a.offsets[a.G];
   }
   const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x, row = idx / across;

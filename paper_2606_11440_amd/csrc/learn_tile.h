@@ -473,62 +473,28 @@ __device__ __forceinline__ void store_few(U* p, u32x4 x, int n) {
 }
 // ---- groups ----------------------------------------------------------------
 
-struct Part {          // a run of `step` rows of a group
-  int g, index, count;   // its group; its place among the group's runs, and how many those are
-  int before;            // runs of the groups before it
-  int lo, hi;            // its rows
+struct Part {     // the runs of `step` rows of a group
+  int count;      // how many
+  int before;     // runs of the groups before it
 };
 
-// Run `want` of the groups' rows cut into runs of `step`, counted through the
-// groups in order; also looks the whole CSR over. False: there is no such run,
-// or the CSR is broken (`bad`). Every wave finds it for itself, 64 groups at a
-// time; the answer is the same in all lanes.
-__device__ __forceinline__ bool find_part(const int32_t* off, int G, int n, int step, int want, Part& part, bool& bad) {
-  bad = false;
-  if (!off) {
-    part = Part{0, want, (int)(((int64_t)n + step - 1) / step), 0, 0, 0};
-    if (want >= part.count) return false;
-    part.lo = want * step;
-    part.hi = n - part.lo > step ? part.lo + step : n;
-    return true;
-  }
+// Whether offsets are a CSR of n rows at most. Every wave looks for itself, 64
+// groups at a time; the answer is the same in all lanes.
+__device__ __forceinline__ bool csr_holds(const int32_t* off, int G, int n) {
   const int lane = (int)threadIdx.x % 64;
-  int total = 0;
-  bool found = false;
   for (int base = 0; base < G; base += 64) {
     const int g = base + lane;
     const int a = g < G ? off[g] : 0, b = g < G ? off[g + 1] : 0;
     const bool wrong = a < 0 || b < a || b > n || (g == 0 && a != 0);
-    bad |= __ballot(wrong) != 0;
-    if (bad) return false;
-    const int t = (int)(((int64_t)(b - a) + step - 1) / step);
-    int s = t;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int o = __shfl_up(s, d);
-      if (lane >= d) s += o;
-    }
-    const uint64_t hit = __ballot(want < total + s);
-    if (!found && hit) {
-      found = true;
-      const int l = (int)__builtin_ctzll(hit);
-      const int lo = __builtin_amdgcn_readlane(a, l), hi = __builtin_amdgcn_readlane(b, l);
-      part.g = base + l;
-      part.count = __builtin_amdgcn_readlane(t, l);
-      part.before = total + __builtin_amdgcn_readlane(s, l) - part.count;
-      part.index = want - part.before;
-      part.lo = lo + part.index * step;
-      part.hi = hi - part.lo > step ? part.lo + step : hi;
-    }
-    total += __builtin_amdgcn_readlane(s, 63);
+    if (__ballot(wrong) != 0) return false;
   }
-  return found;
+  return true;
 }
 
 // Runs of group g (part.before, part.count); false where the CSR is broken.
 __device__ __forceinline__ bool find_group(const int32_t* off, int G, int n, int step, int g, Part& part) {
   if (!off) {
-    part = Part{0, 0, (int)(((int64_t)n + step - 1) / step), 0, 0, n};
+    part = Part{(int)(((int64_t)n + step - 1) / step), 0};
     return true;
   }
   const int lane = (int)threadIdx.x % 64;
@@ -545,13 +511,12 @@ __device__ __forceinline__ bool find_group(const int32_t* off, int G, int n, int
     before += s;
     if (g >= base && g < base + 64) part.count = __builtin_amdgcn_readlane(t, g - base);
   }
-  part.g = g;
   part.before = before;
   return true;
 }
 
-// The groups' rows cut into runs of `step`, as find_part counts them, kept in
-// LDS by a block that takes many of them.
+// The groups' rows cut into runs of `step`, counted through the groups in order,
+// kept in LDS by a block that takes many of them.
 struct Groups {
   int start[IM_MAX_GROUPS + 1];   // runs before group g
   int total;                      // runs; -1: the CSR is broken
