@@ -276,3 +276,26 @@ def test_same_bits_each_time():
     assert all(c["torch"].equal(a[k], b[k]) for k in ("logp", "lse", "entropy"))
     x, y = run_backward(c, a, True), run_backward(c, a, True)
     assert all(c["torch"].equal(x[k], y[k]) for k in x)
+
+
+@pytest.mark.parametrize("n,d,V", [(40, 8, 15), (60, 8, 32), (40, 300, 24), (60, 8, 64), (40, 300, 50)])
+def test_dz_of_narrow_heads_has_sixteen_bits(n, d, V):
+    """Narrow heads' dz enters the products as two bf16 numbers: the first is off by
+    2^-8 of dz, and the second by 2^-8 of that. Sums that cancel show it: there the
+    results' own rounding hides neither a second number left out nor one subtracted."""
+    note(f"[two numbers] n={n} d={d} V={V}")
+    c = make(n, d, V, None, BF16, seed=V, mask=False, relu=False, scale=0.05)   # small products: fp32 errors far below 2^-16
+    torch = c["torch"]
+    o, r = check_forward(c)
+    q = run_backward(c, o, False)
+    (dh, eh), (dW, eW), _ = r.grads(c["dlogp"], c["dent"], False)
+    dz, h, W = r.dz, r.h, r.W[0]
+    less = U.ROUND[torch.bfloat16] - 2.0 ** -16
+    eh = eh - less * (dz.abs() @ W.abs())
+    eW = eW[0] - less * (dz.abs().T @ h.abs())
+    U.close(q["dh"], dh, eh, "dh")
+    U.close(q["dW"][0], dW[0], eW, "dW")
+    first = dz.bfloat16().double()
+    for wrong in (first, 2 * first - dz):       # without the second number, and with its sign turned
+        assert int(((wrong @ W - dh).abs() > eh).sum()) >= 5
+        assert int(((wrong.T @ h - dW[0]).abs() > eW).sum()) >= 5
