@@ -12,7 +12,8 @@
  * int32) is their CSR: group g has rows [offsets[g], offsets[g+1]),
  * offsets[0] = 0, offsets[n_groups] <= n_rows; a group may be empty. Rows
  * behind offsets[n_groups] are not read, and their outputs are left as they
- * were. offsets NULL: one group that holds every row (n_groups = 1).
+ * were. offsets NULL: one group that holds every row (n_groups = 1). With n_rows = 0
+ * offsets are not read.
  *
  * Conventions for every call:
  *   - Pointers are device memory of the current device unless marked "host";
@@ -115,7 +116,7 @@ im_status im_head_workspace(const im_head_desc* desc, int32_t backward, int64_t*
 
 /*   target   int32 [n_rows]: a class, or -1 (none: logp = 0). IM_ERR_ACTION: a
  *            target outside [-1, n_classes) or masked by `valid`; it counts as -1
- *   logp     fp32 [n_rows] out: ln pi(target)
+ *   logp     fp32 [n_rows] out: ln pi(target) (-infinity where the target's logit is)
  *   entropy  fp32 [n_rows] out: -sum pi ln pi, or NULL
  *   lse      fp32 [n_rows] out: ln sum exp z over the valid classes (im_head_backward
  *            reads it), or NULL */

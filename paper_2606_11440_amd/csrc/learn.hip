@@ -637,7 +637,7 @@ im_status im_head_backward(const im_head_desc* d, const int32_t* offsets, const 
     }
   }
   if (db)
-    LEARN_HIP(launch_bias_sum(offsets, d->n_groups, d->n_rows, rows_per_tile(w.logits.shape), w.db_part, V, db, s));
+    LEARN_HIP(launch_bias_sum(some ? offsets : nullptr, d->n_groups, d->n_rows, rows_per_tile(w.logits.shape), w.db_part, V, db, s));
   return IM_OK;
 }
 

@@ -468,6 +468,9 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
               if (lane % 16 == 0) across[wm * S::BN + n_at - n_first + j * 16 + r] = v;
             }
         }
+        // dz leaves rounded once to the products' type, half a step of dh's and dW's own: measured on
+        // a head with entropy, errors of 0.0024 of the norm against 0.0017. Two bf16 numbers, as
+        // narrow heads keep on the chip, would write and read twice as much here.
         __syncthreads();   // the rows are read: the results take the LDS
         auto value = [&](int i, int j) { return acc[i][j]; };
         auto sums = [&] {   // behind the barrier of the pass through LDS

@@ -299,3 +299,12 @@ def test_dz_of_narrow_heads_has_sixteen_bits(n, d, V):
     for wrong in (first, 2 * first - dz):       # without the second number, and with its sign turned
         assert int(((wrong @ W - dh).abs() > eh).sum()) >= 5
         assert int(((wrong.T @ h - dW[0]).abs() > eW).sum()) >= 5
+
+
+@pytest.mark.parametrize("V,dtype", [(30, BF16), (30, F32), (300, BF16)])
+def test_no_rows_whatever_the_offsets_hold(V, dtype):
+    """Without rows offsets are not read: the gradients of every group are zero."""
+    c = make(0, 20, V, [0, 0], dtype, mask=False)
+    c["dev"] = c["torch"].tensor([0, 5, 3], dtype=c["torch"].int32, device="cuda")
+    q = run_backward(c, run_forward(c), True)
+    assert bool((q["dW"] == 0).all()) and bool((q["db"] == 0).all())
