@@ -13,8 +13,11 @@
 //
 // Measured, 262144 rows: 64 classes, 512 wide, 16 groups 220 us in one pass against
 // 356 us as products that keep dz in memory (reading h and writing dh: 101 at the
-// rate of a copy); 15 classes, 256 wide 113 against 181 (51). dz as two numbers costs
-// 13 % of that. Up to 32 classes take a kernel of half the products and LDS: 135 ->
+// rate of a copy); 15 classes, 256 wide 113 against 181 (51). (All in the first calls after
+// a pause; once the clock has settled they are 184 and 85.) Other widths than 256 and 512 have
+// branches around every store and take the next larger of the two: with 64 classes 384
+// columns 204 us, 500 220; 264 191; 200 124 where 256 take 113. dz as two numbers costs
+// 13 %. Up to 32 classes take a kernel of half the products and LDS: 135 ->
 // 113 us with 15 classes, 178 -> 156 with 32 and 512 columns. What bounds it: the chain
 // of LDS, products and dz within a tile, at two waves a SIMD (W and dW fill the
 // registers): without the loads 10 % less, without the stores 9, without dh 38. Also

@@ -10,10 +10,10 @@
 // Both operands lie with k across their rows, so a stage is 64 bytes of k (32
 // rows in bf16) and two stages are in flight: the transposing reads of LDS take
 // 4 rows each, and a longer stage would need LDS that the second buffer has.
-// Measured: 64 ragged groups of 262144 rows, 512 x 512, bf16, 206 us and 34 for the
-// join (0.67 PFLOP/s, matrix cores busy 42 %); one piece of a head of 50021 classes,
-// 1024 wide, over 8192 rows 229 us (0.92 PFLOP/s, 52 %); 256 x 256 over 16384 rows,
-// fp32, 35 us with the join (16.4 at the fp32 rate of the matrix cores). A block
+// Measured, once the clock has settled: 64 ragged groups of 262144 rows, 512 x 512, bf16,
+// 170 us and 29 for the join (0.81 PFLOP/s, matrix cores busy 42 %); one piece of a head of
+// 50021 classes, 1024 wide, over 8192 rows 212 us (0.99 PFLOP/s, 52 %); 256 x 256 over 16384 rows,
+// fp32, 34 us with the join (16.4 at the fp32 rate of the matrix cores). A block
 // keeps both accumulators and two stages, so one or two share a CU, and the start
 // and end of each group's sum wait. The join reads what the blocks leave.
 #include "learn_internal.h"
