@@ -200,6 +200,128 @@ im_status im_adamw_step(im_adamw* opt, double lr, double beta1, double beta2, do
  * tensors stay). NULL is ignored. */
 void im_adamw_destroy(im_adamw* opt);
 
+/* ---- routing to experts ------------------------------------------------------
+ * Each row chooses top_k of n_experts from its logits z (a layer's outputs):
+ *   s_j = softmax of z over the row's valid experts, or sigmoid(z_j)
+ *   choice by c_j = s_j + bias_j, or by z_j without bias (which orders as s_j does);
+ *   with n_sets > 1 the experts are n_sets equal ranges, and only those of the
+ *   top_sets best sets may be chosen: a set's value is its best c (set_best = 1)
+ *   or the sum of its two best, of s + bias or of s (set_best = 2; a set with
+ *   one valid expert has that one's)
+ *   weight = scale s of the chosen experts, with renorm divided by the sum of theirs
+ * c is compared as computed in 64 bits; of equal ones the lowest index is best.
+ * Experts come in the order of their c. An expert is valid where `valid` (uint32
+ * [n_rows x ceil(n_experts / 32)], as for the softmax head, or NULL) has its bit and
+ * its z is neither NaN nor -infinity; +infinity counts as the largest float. One
+ * whose c is then NaN or -infinity cannot be chosen (a bias of -infinity shuts an
+ * expert off; it stays part of the softmax). Where a row has fewer to choose, the
+ * rest of its experts are -1, their weights 0.
+ *   n_rows in [0, IM_MAX_ROWS]; n_experts in [1, IM_MAX_GROUPS]; top_k in [1,
+ *   IM_MAX_TOP_K], at most the experts of top_sets sets; n_sets divides n_experts;
+ *   top_sets in [1, n_sets]
+ *   dtype  im_dtype of z and dz; score IM_SOFTMAX or IM_SIGMOID
+ *   ld_z, ld_dz   row strides */
+#define IM_MAX_TOP_K 32
+#define IM_SOFTMAX 0
+#define IM_SIGMOID 1
+typedef struct {
+  int32_t n_rows, n_experts, top_k, n_sets, top_sets, set_best;
+  int32_t dtype, score, renorm;
+  float scale;
+  int64_t ld_z, ld_dz;
+} im_router_desc;
+
+/*   bias fp32 [n_experts] or NULL; expert int32 [n_rows x top_k] out; weight fp32
+ *   [n_rows x top_k] out */
+im_status im_router_forward(const im_router_desc* desc, const void* z, const float* bias, const uint32_t* valid,
+                            int32_t* expert, float* weight, void* stream);
+
+/* dz of sum weight dweight, for the experts as given (the choice has no gradient; the
+ * sets and the bias do not count). Experts are those of the forward call, or any
+ * others: one listed twice counts twice. IM_ERR_ACTION: an expert outside [-1,
+ * n_experts) or not valid; it counts as -1, whose dweight does not count. dz is
+ * zero for experts that are not valid. */
+im_status im_router_backward(const im_router_desc* desc, const void* z, const uint32_t* valid,
+                             const int32_t* expert, const float* dweight, void* dz, int32_t* error, void* stream);
+
+/* ---- rows to experts and back --------------------------------------------------
+ * The grouped layers take each expert's rows in one range. A pair is a row i and
+ * its choice c; im_dispatch_plan orders the pairs by expert (those of one expert
+ * by i, then c) and tells each its place:
+ *   expert  int32 [n_rows x top_k]: -1 goes nowhere; the same expert may come twice
+ *   offsets int32 [n_experts + 1] out: the groups' CSR
+ *   slot    int32 [n_rows x top_k] out: place of the pair, or -1
+ * IM_ERR_ACTION: an expert outside [-1, n_experts); it counts as -1.
+ *   n_rows in [0, IM_MAX_ROWS], n_rows top_k at most IM_MAX_ROWS; top_k in [1,
+ *   IM_MAX_TOP_K]; n_experts in [1, IM_MAX_GROUPS] (the plan's only); dim in [1, IM_MAX_DIM]
+ *   dtype   of rows: IM_F32, IM_BF16, or IM_CODES for the int8 codes of packed
+ *           rows (im_dispatch_forward only; their scales go as rows of one float)
+ *   ld_row  row stride of what has n_rows rows (x, dx, y, dy)
+ *   ld_slot row stride of what has n_slots rows (xs, dxs, ys), ld_dslot of dys
+ *   n_slots rows of those, in [0, IM_MAX_ROWS]
+ * In the other calls slots are the plan's: no place twice. IM_ERR_ACTION: a slot
+ * outside [-1, n_slots); it counts as -1. Places that no slot names are neither read
+ * nor written. Sums run over c in order, in fp32. */
+#define IM_CODES 2
+typedef struct {
+  int32_t n_rows, top_k, n_experts, n_slots, dim, dtype;
+  int64_t ld_row, ld_slot, ld_dslot;
+} im_dispatch_desc;
+
+im_status im_dispatch_workspace(const im_dispatch_desc* desc, int64_t* bytes);
+im_status im_dispatch_plan(const im_dispatch_desc* desc, const int32_t* expert, int32_t* offsets, int32_t* slot,
+                           void* workspace, int64_t workspace_bytes, int32_t* error, void* stream);
+/* xs[slot_ic] = x_i */
+im_status im_dispatch_forward(const im_dispatch_desc* desc, const void* x, const int32_t* slot, void* xs,
+                              int32_t* error, void* stream);
+/* dx_i = sum_c dxs[slot_ic] */
+im_status im_dispatch_backward(const im_dispatch_desc* desc, const void* dxs, const int32_t* slot, void* dx,
+                               int32_t* error, void* stream);
+/* y_i = sum_c weight_ic ys[slot_ic] (a row with no slot: 0); weight fp32 [n_rows x top_k] */
+im_status im_combine_forward(const im_dispatch_desc* desc, const void* ys, const int32_t* slot, const float* weight,
+                             void* y, int32_t* error, void* stream);
+/* dys[slot_ic] = weight_ic dy_i, dweight_ic = dy_i . ys[slot_ic] (0 without a slot);
+ * dys or dweight may be NULL to skip it (ys is read for dweight only, weight for dys) */
+im_status im_combine_backward(const im_dispatch_desc* desc, const void* dy, const void* ys, const int32_t* slot,
+                              const float* weight, void* dys, float* dweight, int32_t* error, void* stream);
+
+/* ---- rows in 8 bits -----------------------------------------------------------
+ * A packed row is int8 codes in [-127, 127] and a scale: x_j = scale code_j.
+ *   scale = max |x_j| / 127 (at least 2^-126), code = x_j (1 / scale), rounded to
+ *   nearest even, every operation in fp32
+ * so that |x_j - scale code_j| <= scale / 2 (and a few units of fp32). keep: what is not
+ * zero gets the code 1 or -1 at least, so that a kept ReLU output says where it was above
+ * zero (off by less than a scale there). A row with a value that is not finite has
+ * the scale NaN and codes 0.
+ * Weights are packed by their outputs: [n_groups out_dim] rows of in_dim.
+ *   n_rows in [0, IM_MAX_ROWS]; dim in [1, IM_MAX_DIM]; dtype im_dtype of x
+ *   ld_x, ld_codes   row strides (elements) */
+typedef struct {
+  int32_t n_rows, dim, dtype, keep;
+  int64_t ld_x, ld_codes;
+} im_rows_desc;
+
+im_status im_rows_pack(const im_rows_desc* desc, const void* x, int8_t* codes, float* scale, void* stream);
+/* x = scale code in fp32, rounded to its type */
+im_status im_rows_unpack(const im_rows_desc* desc, const int8_t* codes, const float* scale, void* x, void* stream);
+
+/* The grouped layers on packed rows. desc as for im_linear_*, with dtype that of what
+ * is not packed (y; dy, W, dx, dW) and ld_x the row stride of the codes.
+ * forward: y_i = act(x_scale_i W_scale_gj (sum_k x_ik W_gjk) + b_gj), a product of
+ * 8-bit integers whose sum is exact; x and W are codes, W [n_groups x out_dim x in_dim]
+ * contiguous, W_scale fp32 [n_groups x out_dim].
+ * backward: the gradients of im_linear_backward with x in 8 bits, as it was kept
+ * (IM_BF16: scale code is rounded to bf16 where it enters the product of dW, 2^-8 of it at
+ * most, which rounding to the code left already of the largest); relu_in: dx is zero where the code is not above 0. */
+im_status im_linear_workspace_packed(const im_linear_desc* desc, int32_t backward, int64_t* bytes);
+im_status im_linear_forward_packed(const im_linear_desc* desc, const int32_t* offsets, const int8_t* x,
+                                   const float* x_scale, const int8_t* W, const float* W_scale, const float* b,
+                                   void* y, void* workspace, int64_t workspace_bytes, int32_t* error, void* stream);
+im_status im_linear_backward_packed(const im_linear_desc* desc, const int32_t* offsets, const void* dy,
+                                    const int8_t* x, const float* x_scale, const void* W, void* dx, void* dW,
+                                    float* db, void* workspace, int64_t workspace_bytes, int32_t* error,
+                                    void* stream);
+
 /* Description of the calling thread's last failed call of this header. Never NULL. */
 const char* im_learn_last_error(void);
 

@@ -24,9 +24,12 @@ from ._lib import (EXPORTED, IMError, im_clear_error, im_destroy, im_dual_update
                    im_write_state,
                    make_arrivals,
                    make_desc)
-from .learn import (LEARN_EXPORTED, AdamW, im_head_backward, im_head_forward,  # noqa: F401
-                    im_head_workspace, im_learn_last_error, im_linear_backward, im_linear_forward,
-                    im_linear_workspace)
+from .learn import (LEARN_EXPORTED, AdamW, im_combine_backward, im_combine_forward,  # noqa: F401
+                    im_dispatch_backward, im_dispatch_forward, im_dispatch_plan, im_dispatch_workspace,
+                    im_head_backward, im_head_forward, im_head_workspace, im_learn_last_error,
+                    im_linear_backward, im_linear_backward_packed, im_linear_forward,
+                    im_linear_forward_packed, im_linear_workspace, im_linear_workspace_packed,
+                    im_router_backward, im_router_forward, im_rows_pack, im_rows_unpack)
 
 
 def device_arrivals(arr: dict, device="cuda"):

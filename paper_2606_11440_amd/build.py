@@ -14,7 +14,8 @@ LIB = os.path.join(HERE, "libinframind.so")
 SOURCES = ["route.hip", "schedule.hip", "rows.hip", "pool.hip"]
 # the learner's operators: a library of their own
 LEARN_LIB = os.path.join(HERE, "libinframind_learn.so")
-LEARN_SOURCES = ["learn.hip", "learn_rows.hip", "learn_sums.hip", "learn_head.hip", "learn_adamw.hip"]
+LEARN_SOURCES = ["learn.hip", "learn_rows.hip", "learn_sums.hip", "learn_head.hip", "learn_adamw.hip",
+                 "learn_experts.hip", "learn_router.hip", "learn_dispatch.hip", "learn_packed.hip"]
 # measurement probe used by the benchmark only (not part of the tick's library)
 PROBE_LIB = os.path.join(HERE, "libimprobe.so")
 PROBE_SOURCES = ["peak_probe.hip"]

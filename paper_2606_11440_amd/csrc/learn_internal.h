@@ -12,6 +12,7 @@ namespace learn {
 enum Epilogue {
   kStore = 0,     // y = act(sum + b)
   kStoreInput,    // dx = sum, zero where x <= 0 with relu_in
+  kStoreInputCodes,   // dx = sum, zero where x, in int8 codes, is <= 0
   kStats,         // per row and column tile: largest logit, sum exp, sum exp (z - largest)
   kGradLogits,    // dz of a piece of the classes
   kPartial        // the sums of a run of k, in fp32 (joined by a kernel of their own)
@@ -64,6 +65,7 @@ struct SumArgs {
   int64_t ldp;
   const void* Q;
   int64_t ldq;
+  const float* scale;         // Q is int8 codes, and this their rows' scales
   const uint8_t* live;        // rows of Q to take, or NULL (all)
   void* dW;                   // [G x w_group], rows of N
   int64_t w_group;
@@ -122,6 +124,77 @@ hipError_t launch_sums(const SumArgs& a, int dtype, int shape, hipStream_t s);
 // db_g = sum of the column sums of the group's row tiles (of `step` rows).
 hipError_t launch_bias_sum(const int32_t* offsets, int G, int n, int step, const float* part, int64_t width, float* db,
                            hipStream_t s);
+// Routing to experts.
+struct RouterArgs {
+  int32_t n, E, k, sets, top_sets, best, renorm;
+  float scale;
+  const void* z;
+  int64_t ld_z;
+  const float* bias;
+  const uint32_t* valid;
+  int32_t words;              // mask words of a row
+  int32_t* expert;            // forward: out; backward: in
+  float* weight;
+  const float* dweight;
+  void* dz;
+  int64_t ld_dz;
+  int32_t* error;
+};
+hipError_t launch_router_forward(const RouterArgs& a, int dtype, int score, hipStream_t s);
+hipError_t launch_router_backward(const RouterArgs& a, int dtype, int score, hipStream_t s);
+
+// Rows to experts and back.
+struct PlanArgs {
+  const int32_t* expert;
+  int64_t pairs;
+  int32_t E, blocks;          // blocks that share the pairs
+  int64_t each;               // pairs of a block, a multiple of 64
+  int32_t* count;             // [blocks][E]: pairs of an expert in a block, then in the blocks before it
+  int32_t* total;             // [E]
+  int32_t* offsets;
+  int32_t* slot;
+  int32_t* error;
+};
+int64_t plan_blocks(int64_t pairs, int64_t E, int cus, int64_t& each);
+hipError_t launch_dispatch_plan(const PlanArgs& a, hipStream_t s);
+
+struct ExchangeArgs {
+  int32_t n, k, n_slots, dim;
+  const int32_t* slot;
+  const float* weight;        // NULL: 1
+  const void* from;           // what is sent: rows (dispatch, combine_backward) or slots (the sums)
+  int64_t ld_from;
+  void* to;
+  int64_t ld_to;
+  const void* ys;             // combine_backward
+  int64_t ld_ys;
+  float* dweight;
+  int32_t* error;
+};
+hipError_t launch_send(const ExchangeArgs& a, int dtype, hipStream_t s);            // to[slot] = from_i
+hipError_t launch_gather(const ExchangeArgs& a, int dtype, hipStream_t s);          // to_i = sum weight from[slot]
+hipError_t launch_combine_backward(const ExchangeArgs& a, int dtype, hipStream_t s);
+
+// Rows in 8 bits.
+struct PackArgs {
+  int32_t n, dim, keep;
+  const void* x;
+  int64_t ld_x;
+  int8_t* codes;
+  int64_t ld_codes;
+  float* scale;
+  void* out;                  // unpack: ld_x
+};
+hipError_t launch_pack(const PackArgs& a, int dtype, hipStream_t s);
+hipError_t launch_unpack(const PackArgs& a, int dtype, hipStream_t s);
+// y = act(sx sw (codes . codes) + b): RowArgs with A and B codes, and
+struct PackedScales {
+  const float* x;             // [n]
+  const float* W;             // [G x N]
+};
+RowPlan plan_packed(int64_t n, int64_t G, int64_t N, int64_t K, int cus);
+hipError_t launch_packed_product(const RowArgs& a, const PackedScales& p, int dtype, int shape, hipStream_t s);
+
 int rows_per_tile(int shape);   // of a row product
 int cols_per_tile(int shape);
 int rows_per_sum(int shape);    // rows of W a tile of the sums covers

@@ -1,0 +1,438 @@
+// Rows in 8 bits: packing, unpacking, and the product of packed rows with packed weights.
+//
+// Pack and unpack are one pass over memory. The product goes as that of bf16 rows does
+// (tiles, stages of 128 bytes, blocks that keep taking tiles), on v_mfma_i32_16x16x64_i8: twice the
+// operations a byte of LDS, and an exact sum (127^2 65536 is below 2^31), which the
+// scales of its row and column multiply once.
+#include "learn_internal.h"
+#include "learn_tile.h"
+#include "wave.h"
+
+namespace im {
+namespace learn {
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// a launch has less than 2^32 threads in a dimension: past this many blocks they take more rows each
+unsigned blocks_of(int64_t n, int rows) {
+  const int64_t blocks = (n + rows - 1) / rows, most = 1 << 20;
+  return (unsigned)(blocks < most ? blocks : most);
+}
+
+template <typename T>
+__device__ __forceinline__ void widen(u32x4 v, float (&f)[kVec<T>]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = v[i];
+    if constexpr (sizeof(T) == 2) {
+      f[2 * i] = __builtin_bit_cast(float, w << 16);
+      f[2 * i + 1] = __builtin_bit_cast(float, w & 0xffff0000u);
+    } else {
+      f[i] = __builtin_bit_cast(float, w);
+    }
+  }
+}
+
+// First element of unit u of a row: the last unit ends with the row (with some elements that the
+// one before it has too); a row shorter than a unit is one, taken element by element.
+template <typename T>
+__device__ __forceinline__ int unit_at(int u, int dim) {
+  const int first = u * kVec<T>;
+  return first + kVec<T> <= dim || dim < kVec<T> ? first : dim - kVec<T>;
+}
+template <typename T>
+__device__ __forceinline__ u32x4 unit_load(const T* row, int u, int dim) {
+  return dim < kVec<T> ? load_few(row, dim) : load16(row + unit_at<T>(u, dim));
+}
+
+// Largest magnitude of a unit, as the bits of a float: they order as magnitudes do, NaN above infinity.
+template <typename T>
+__device__ __forceinline__ uint32_t most_bits(u32x4 v, uint32_t most) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = v[i];
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t lo = (w << 16) & 0x7fffffffu, hi = w & 0x7fff0000u;
+      most = lo > most ? lo : most;
+      most = hi > most ? hi : most;
+    } else {
+      const uint32_t b = w & 0x7fffffffu;
+      most = b > most ? b : most;
+    }
+  }
+  return most;
+}
+
+struct Scale {
+  float scale, inverse;   // not finite: NaN and 0
+  __device__ __forceinline__ explicit Scale(uint32_t most) {
+    const float top = __builtin_bit_cast(float, most);
+    scale = fmaxf(top / 127.f, 0x1p-126f);
+    inverse = 1.f / scale;
+    if (most >= 0x7f800000u) {
+      scale = __builtin_nanf("");
+      inverse = 0.f;
+    }
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void put_codes(int8_t* row, int u, int dim, u32x4 v, const Scale& s, bool keep) {
+  float f[kVec<T>];
+  widen<T>(v, f);
+  int8_t q[kVec<T>];
+#pragma unroll
+  for (int i = 0; i < kVec<T>; ++i) {
+    const float x = s.inverse == 0.f ? 0.f : f[i];   // no infinity times 0
+    int c = (int)rintf(x * s.inverse);               // 127 at most: scale and inverse are off by half a unit each
+    if (keep && c == 0) c = x > 0.f ? 1 : (x < 0.f ? -1 : 0);
+    q[i] = (int8_t)c;
+  }
+  if (dim < kVec<T>) {
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i)
+      if (i < dim) row[i] = q[i];
+  } else {
+    __builtin_memcpy(row + unit_at<T>(u, dim), q, kVec<T>);
+  }
+}
+
+// L lanes a row, N units a lane, kept in registers between the largest magnitude and the codes.
+template <typename T, int L, int N>
+__global__ __launch_bounds__(256) void pack_kernel(const PackArgs a) {
+  constexpr int kRows = 256 / L;
+  const int l = (int)threadIdx.x % L, units = (a.dim + kVec<T> - 1) / kVec<T>;
+  for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.n; first += (int64_t)gridDim.x * kRows) {
+    const int64_t at = first + (int)threadIdx.x / L, row = at < a.n ? at : a.n - 1;
+    const T* from = static_cast<const T*>(a.x) + row * a.ld_x;
+    u32x4 v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int u = l + i * L;
+      v[i] = u < units ? unit_load<T>(from, u, a.dim) : u32x4{0, 0, 0, 0};
+    }
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) most = most_bits<T>(v[i], most);
+#pragma unroll
+    for (int d = 1; d < L; d *= 2) {
+      const uint32_t o = (uint32_t)__shfl_xor((int)most, d);
+      most = o > most ? o : most;
+    }
+    if (at >= a.n) continue;   // the last block's other lanes
+    const Scale s(most);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int u = l + i * L;
+      if (u < units) put_codes<T>(a.codes + row * a.ld_codes, u, a.dim, v[i], s, a.keep != 0);
+    }
+    if (l == 0) a.scale[row] = s.scale;
+  }
+}
+
+// A block a row, for long rows: they are read again for the codes (from the L2).
+template <typename T>
+__global__ __launch_bounds__(1024) void pack_long_kernel(const PackArgs a) {
+  __shared__ uint32_t across[16];
+  const int units = (a.dim + kVec<T> - 1) / kVec<T>;
+  for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+    const T* from = static_cast<const T*>(a.x) + row * a.ld_x;
+    uint32_t most = 0;
+#pragma unroll 4
+    for (int u = threadIdx.x; u < units; u += 1024) most = most_bits<T>(unit_load<T>(from, u, a.dim), most);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const uint32_t o = (uint32_t)__shfl_xor((int)most, d);
+      most = o > most ? o : most;
+    }
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) across[threadIdx.x / 64] = most;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 16; ++w) most = across[w] > most ? across[w] : most;
+    const Scale s(most);
+#pragma unroll 4
+    for (int u = threadIdx.x; u < units; u += 1024)
+      put_codes<T>(a.codes + row * a.ld_codes, u, a.dim, unit_load<T>(from, u, a.dim), s, a.keep != 0);
+    if (threadIdx.x == 0) a.scale[row] = s.scale;
+  }
+}
+
+// x = scale code, L lanes a row.
+template <typename T, int L>
+__global__ __launch_bounds__(256) void unpack_kernel(const PackArgs a) {
+  constexpr int kRows = 256 / L;
+  const int l = (int)threadIdx.x % L, units = (a.dim + kVec<T> - 1) / kVec<T>;
+  for (int64_t row = (int64_t)blockIdx.x * kRows + (int)threadIdx.x / L; row < a.n; row += (int64_t)gridDim.x * kRows) {
+    const float scale = a.scale[row];
+    const int8_t* from = a.codes + row * a.ld_codes;
+    T* const to = static_cast<T*>(a.out) + row * a.ld_x;
+    for (int u = l; u < units; u += L) {
+      int8_t q[kVec<T>];
+      if (a.dim < kVec<T>) {
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) q[i] = i < a.dim ? from[i] : 0;
+      } else {
+        __builtin_memcpy(q, from + unit_at<T>(u, a.dim), kVec<T>);
+      }
+      T o[kVec<T>];
+#pragma unroll
+      for (int i = 0; i < kVec<T>; ++i) o[i] = (T)(scale * (float)q[i]);
+      u32x4 v;
+      __builtin_memcpy(&v, o, 16);
+      if (a.dim < kVec<T>) store_few(to, v, a.dim);
+      else *reinterpret_cast<u32x4_any*>(to + unit_at<T>(u, a.dim)) = v;
+    }
+  }
+}
+
+// ---- the product -----------------------------------------------------------------
+
+__device__ __forceinline__ f32x4 load4(const float* p, int left) {
+  typedef f32x4 any __attribute__((aligned(4)));
+  if (left >= 4) return *reinterpret_cast<const any*>(p);
+  f32x4 v;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v[r] = r < left ? p[r] : 0.f;
+  return v;
+}
+
+// y = act(sx sw sum + b) of one result.
+__device__ __forceinline__ float finish(int sum, float sx, float sw, float b, float least) {
+  const float v = fmaf((float)sum * sx, sw, b);
+  return v < least ? least : v;   // NaN stays
+}
+
+template <typename U, class S, bool PARTIAL>
+__global__ __launch_bounds__(S::NT, S::kWaves) void packed_kernel(const RowArgs a, const PackedScales scales) {
+  using T = int8_t;
+  using P = RowTile<T, S::BM, S::NT, S::D, S::SB>;
+  using Q = RowTile<T, S::BN, S::NT, S::D, S::SB>;
+  using Product = Sum<T, S, P, Q, false>;
+  __shared__ __attribute__((aligned(16))) char lds[2 * Product::kBuf];
+  __shared__ Groups groups;
+  groups.init(a.offsets, a.G, a.n, S::BM);
+  __syncthreads();
+  if (groups.total < 0) {
+    if (blockIdx.x == 0 && threadIdx.x == 0 && a.error) atomicOr(a.error, IM_ERR_COUNT);
+    return;
+  }
+  // with several runs of k a tile is as many units of work, one after the other
+  const int row_tiles = groups.total, splits = PARTIAL ? a.splits : 1, total = row_tiles * a.col_tiles * splits;
+  int tile = blockIdx.x;
+  if (tile >= total) return;
+  Product x;
+  x.lds = lds;
+  x.steps = (a.K + P::kStage - 1) / P::kStage;
+  int rt, ct, g, lo, hi, split = 0;
+  auto enter = [&](int t) {   // takes tile t: its first loads are on their way
+    const int tid = fresh_thread();
+    int k0 = 0, K = a.K;
+    if constexpr (PARTIAL) {
+      split = t % splits;
+      t /= splits;
+      k0 = split * a.split_k;
+      K = a.K - k0 < a.split_k ? a.K - k0 : a.split_k;
+      x.steps = (K + P::kStage - 1) / P::kStage;
+    }
+    tile_of(t, row_tiles, a.col_tiles, rt, ct);
+    groups.find(a.offsets, a.G, a.n, S::BM, rt, g, lo, hi);
+    x.p.init(static_cast<const T*>(a.A) + k0, a.lda, lo, hi - 1, K, tid);
+    x.q.init(static_cast<const T*>(a.B) + g * a.b_group + k0, a.ldb, ct * S::BN, a.N - 1, K, tid);
+    x.begin();
+  };
+  enter(tile);
+  x.first_stage();
+  while (true) {
+    x.run();
+    auto& acc = x.acc;
+    const int tid = fresh_thread(), lane = tid % 64, wave = tid / 64, g4 = (lane / 16) * 4;
+    const int wm = wave / S::WN, wn = wave % S::WN, m_at = wm * S::MI * 16 + lane % 16;
+    const int at_lo = lo, at_hi = hi, at_g = g, at_split = split, n_first = ct * S::BN;
+    tile += gridDim.x;
+    const bool more = tile < total;
+    auto next = [&] {
+      if (more) enter(tile);
+    };
+    auto last = [&](bool on) {   // the next tile's first stage takes the LDS that the epilogue has read
+      if (!on) return;
+      __syncthreads();
+      x.first_stage();
+    };
+    if constexpr (PARTIAL) {
+      using F = Out<float, S, (int)sizeof(lds)>;
+      float* const part = a.part + (int64_t)at_split * a.n * a.N;
+      // the sums' bits, moved only
+      F::run(lds, tid, [&](int i, int j) { return __builtin_bit_cast(f32x4, acc[i][j]); }, next,
+             [&](int, int m, int c, u32x4 v) {
+        const int64_t row = (int64_t)at_lo + m;
+        const int n = n_first + c, left = a.N - n;
+        if (row >= at_hi || left <= 0) return;
+        uint32_t* const to = reinterpret_cast<uint32_t*>(part + row * a.N + n);
+        if (left >= 4) *reinterpret_cast<u32x4_any*>(to) = v;
+        else store_few(to, v, left);
+      });
+      last(more);
+    } else {
+      const int n_at = n_first + wn * S::NJ * 16 + g4;
+      const float* bias = a.bias ? a.bias + at_g * a.bias_group : nullptr;
+      const float* sw = scales.W + at_g * (int64_t)a.N;
+      f32x4 plus[S::NJ], times[S::NJ];
+      float sx[S::MI];
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) {
+        plus[j] = times[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (n_at + j * 16 < a.N) {
+          times[j] = load4(sw + n_at + j * 16, a.N - n_at - j * 16);
+          if (bias) plus[j] = load4(bias + n_at + j * 16, a.N - n_at - j * 16);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < S::MI; ++i) {
+        const int64_t row = (int64_t)at_lo + m_at + i * 16;
+        sx[i] = scales.x[row < at_hi ? row : at_hi - 1];
+      }
+      const float least = a.relu ? 0.f : -INFINITY;
+      auto value = [&](int i, int j) {
+        f32x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = finish(acc[i][j][r], sx[i], times[j][r], plus[j][r], least);
+        return v;
+      };
+      using O = Out<U, S, (int)sizeof(lds)>;
+      char* const C = reinterpret_cast<char*>(static_cast<U*>(a.C) + (int64_t)at_lo * a.ldc + n_first);
+      auto place = [&](int m, int c) { return ((uint32_t)m * (uint32_t)a.ldc + (uint32_t)c) * (uint32_t)sizeof(U); };
+      if (at_hi - at_lo == S::BM && n_first + S::BN <= a.N) {   // no branch on the way out
+        O::run(lds, tid, value, next, [&](int, int m, int c, u32x4 v) { *reinterpret_cast<u32x4_any*>(C + place(m, c)) = v; });
+        last(more);
+      } else {
+        O::run(lds, tid, value, next, [&](int, int m, int c, u32x4 v) {
+          const int left = a.N - n_first - c;
+          if (at_lo + m >= at_hi || left <= 0) return;
+          U* const to = reinterpret_cast<U*>(C + place(m, c));
+          if (left >= kVec<U>) *reinterpret_cast<u32x4_any*>(to) = v;
+          else store_few(to, v, left);
+        });
+        last(more);
+      }
+    }
+    if (!more) break;
+  }
+}
+
+// Joins the runs of k: four columns of a row a thread.
+template <typename U>
+__global__ __launch_bounds__(256) void join_packed_kernel(const RowArgs a, const PackedScales scales) {
+  const int quads = (a.N + 3) / 4;
+  int end = a.n;
+  if (a.offsets) {
+    if (!csr_holds(a.offsets, a.G, a.n)) return;
+    end = a.offsets[a.G];
+  }
+  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x, row = idx / quads;
+  if (row >= end) return;
+  const int n = (int)(idx % quads) * 4, left = a.N - n;
+  const int64_t step = (int64_t)a.n * a.N;
+  const float* part = a.part + row * a.N + n;
+  i32x4 sum = __builtin_bit_cast(i32x4, load4(part, left));
+#pragma unroll 4
+  for (int s = 1; s < a.splits; ++s) sum += __builtin_bit_cast(i32x4, load4(part + s * step, left));
+  int g = 0, over = a.offsets ? a.G : 1;   // the last group that begins at or before the row
+  while (over - g > 1) {
+    const int mid = (g + over) / 2;
+    if (a.offsets[mid] <= row) g = mid;
+    else over = mid;
+  }
+  const f32x4 times = load4(scales.W + (int64_t)g * a.N + n, left);
+  const f32x4 plus = a.bias ? load4(a.bias + g * a.bias_group + n, left) : f32x4{0.f, 0.f, 0.f, 0.f};
+  const float sx = scales.x[row], least = a.relu ? 0.f : -INFINITY;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (r < left) static_cast<U*>(a.C)[row * a.ldc + n + r] = (U)finish(sum[r], sx, times[r], plus[r], least);
+}
+
+using Large = Shape<2, 4, 8, 4, 1, 128>;    // 256 x 256, 512 threads
+using Middle = Shape<2, 2, 4, 4, 1, 128>;   // 128 x 128
+using Narrow = Shape<4, 1, 2, 4, 1, 128>;   // 128 x 64
+using Small = Shape<2, 2, 2, 2, 2, 128>;    // 64 x 64
+
+template <typename U, class S, bool PARTIAL>
+hipError_t launch(const RowArgs& a, const PackedScales& p, hipStream_t s) {
+  const int tiles = a.row_tiles * a.col_tiles * (PARTIAL ? a.splits : 1), most = a.cus * S::kBlocks;
+  hipLaunchKernelGGL((packed_kernel<U, S, PARTIAL>), dim3((unsigned)(tiles < most ? tiles : most)), dim3(S::NT), 0, s, a, p);
+  return hipGetLastError();
+}
+template <typename U>
+hipError_t launch_type(const RowArgs& a, const PackedScales& p, int shape, hipStream_t s) {
+  if (a.splits > 1) {
+    const hipError_t e = shape == 1 ? launch<U, Middle, true>(a, p, s) : launch<U, Small, true>(a, p, s);
+    if (e != hipSuccess) return e;
+    const int64_t quads = (int64_t)a.n * ((a.N + 3) / 4);
+    hipLaunchKernelGGL(join_packed_kernel<U>, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, a, p);
+    return hipGetLastError();
+  }
+  switch (shape) {
+    case 0: return launch<U, Large, false>(a, p, s);
+    case 1: return launch<U, Middle, false>(a, p, s);
+    case 2: return launch<U, Narrow, false>(a, p, s);
+    default: return launch<U, Small, false>(a, p, s);
+  }
+}
+
+template <typename T, int L>
+hipError_t pack_rows(const PackArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((pack_kernel<T, L, 1>), dim3(blocks_of(a.n, 256 / L)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <typename T, int N>
+hipError_t pack_wide(const PackArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((pack_kernel<T, 64, N>), dim3(blocks_of(a.n, 4)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t pack(const PackArgs& a, hipStream_t s) {
+  const int units = (a.dim + kVec<T> - 1) / kVec<T>;
+  if (units <= 4) return pack_rows<T, 4>(a, s);
+  if (units <= 8) return pack_rows<T, 8>(a, s);
+  if (units <= 16) return pack_rows<T, 16>(a, s);
+  if (units <= 32) return pack_rows<T, 32>(a, s);
+  if (units <= 64) return pack_rows<T, 64>(a, s);
+  if (units <= 128) return pack_wide<T, 2>(a, s);
+  if (units <= 256) return pack_wide<T, 4>(a, s);
+  if (units <= 512) return pack_wide<T, 8>(a, s);
+  hipLaunchKernelGGL(pack_long_kernel<T>, dim3(blocks_of(a.n, 1)), dim3(1024), 0, s, a);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t unpack(const PackArgs& a, hipStream_t s) {
+  const int units = (a.dim + kVec<T> - 1) / kVec<T>;
+  const dim3 block(256);
+  if (units <= 4) hipLaunchKernelGGL((unpack_kernel<T, 4>), dim3(blocks_of(a.n, 64)), block, 0, s, a);
+  else if (units <= 16) hipLaunchKernelGGL((unpack_kernel<T, 16>), dim3(blocks_of(a.n, 16)), block, 0, s, a);
+  else hipLaunchKernelGGL((unpack_kernel<T, 64>), dim3(blocks_of(a.n, 4)), block, 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_pack(const PackArgs& a, int dtype, hipStream_t s) {
+  return dtype == IM_BF16 ? pack<__bf16>(a, s) : pack<float>(a, s);
+}
+hipError_t launch_unpack(const PackArgs& a, int dtype, hipStream_t s) {
+  return dtype == IM_BF16 ? unpack<__bf16>(a, s) : unpack<float>(a, s);
+}
+
+// A stage holds twice the k of a bf16 one and takes as long.
+RowPlan plan_packed(int64_t n, int64_t G, int64_t N, int64_t K, int cus) {
+  RowPlan p = plan_rows(IM_BF16, n, G, N, (K + 1) / 2, cus, true);
+  p.split_k *= 2;
+  return p;
+}
+
+hipError_t launch_packed_product(const RowArgs& a, const PackedScales& p, int dtype, int shape, hipStream_t s) {
+  return dtype == IM_BF16 ? launch_type<__bf16>(a, p, shape, s) : launch_type<float>(a, p, shape, s);
+}
+
+}  // namespace learn
+}  // namespace im

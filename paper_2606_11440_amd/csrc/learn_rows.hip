@@ -120,6 +120,24 @@ struct Row {
   }
 };
 
+// The layer's input that a gradient passes: a unit of T, or of as many int8 codes.
+template <typename T, bool CODES>
+struct InputMask {
+  using element = T;
+  using unit = u32x4;
+  static __device__ __forceinline__ unit load(const T* p) { return load16(p); }
+  static __device__ __forceinline__ unit load_few(const T* p, int n) { return learn::load_few(p, n); }
+  static __device__ __forceinline__ u32x4 apply(u32x4 v, unit x) { return where_positive<T>(v, x); }
+};
+template <typename T>
+struct InputMask<T, true> {
+  using element = int8_t;
+  using unit = typename CodeUnit<T>::type;
+  static __device__ __forceinline__ unit load(const int8_t* p) { return load_codes<T>(p); }
+  static __device__ __forceinline__ unit load_few(const int8_t* p, int n) { return load_few_codes<T>(p, n); }
+  static __device__ __forceinline__ u32x4 apply(u32x4 v, unit x) { return where_code_positive<T>(v, x); }
+};
+
 template <typename T, class S, bool COLUMNS, int EPI>
 __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a) {
   using P = RowTile<T, S::BM, S::NT, S::D, S::SB>;
@@ -248,9 +266,10 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
       }
     }
 
-    if constexpr (EPI == kStoreInput) {
+    if constexpr (EPI == kStoreInput || EPI == kStoreInputCodes) {
+      constexpr bool kCodes = EPI == kStoreInputCodes;
       auto value = [&](int i, int j) { return acc[i][j]; };
-      if (a.sum) {   // a piece of a head's classes
+      if (!kCodes && a.sum) {   // a piece of a head's classes
         using F = Out<float, S, (int)sizeof(lds)>;
         F::run(lds, tid, value, [] {}, [&](int, int m, int c, u32x4 x) {
           const int64_t row = (int64_t)at_lo + m;
@@ -271,7 +290,7 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
         });
         next();
         last(more);
-      } else if (!a.X) {
+      } else if (!kCodes && !a.X) {
         if (full) {
           O::run(lds, tid, value, next, put);
           last(more);
@@ -281,23 +300,25 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
         }
       } else {
         // the layer's input, loaded before the results that it lets through are read
-        const char* const X = reinterpret_cast<const char*>(static_cast<const T*>(a.X) + (int64_t)at_lo * a.ldx + n_first);
+        using Mask = InputMask<T, kCodes>;
+        using X_t = typename Mask::element;
+        const char* const X = reinterpret_cast<const char*>(static_cast<const X_t*>(a.X) + (int64_t)at_lo * a.ldx + n_first);
         auto x_at = [&](int k) {
           const int m = O::row_of(k / O::kUnits, k % O::kUnits, tid), c = O::column_of(tid);
-          return ((uint32_t)m * (uint32_t)a.ldx + (uint32_t)c) * (uint32_t)sizeof(T);
+          return reinterpret_cast<const X_t*>(X + ((uint32_t)m * (uint32_t)a.ldx + (uint32_t)c) * (uint32_t)sizeof(X_t));
         };
         constexpr int kAll = O::kUnits * O::kPasses, kAhead = kAll < 8 ? kAll : 8;
-        u32x4 xs[kAhead];
+        typename Mask::unit xs[kAhead];
         if (full) {
           O::run(lds, tid, value,
                  [&] {
                    if (O::kPasses == 1) next();
 #pragma unroll
-                   for (int k = 0; k < kAhead; ++k) xs[k] = *reinterpret_cast<const u32x4_any*>(X + x_at(k));
+                   for (int k = 0; k < kAhead; ++k) xs[k] = Mask::load(x_at(k));
                  },
                  [&](int k, int m, int c, u32x4 v) {
-                   put(k, m, c, where_positive<T>(v, xs[k % kAhead]));
-                   if (k + kAhead < kAll) xs[k % kAhead] = *reinterpret_cast<const u32x4_any*>(X + x_at(k + kAhead));
+                   put(k, m, c, Mask::apply(v, xs[k % kAhead]));
+                   if (k + kAhead < kAll) xs[k % kAhead] = Mask::load(x_at(k + kAhead));
                  });
           if (O::kPasses > 1) next();
           last(more);
@@ -305,8 +326,8 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void rows_kernel(const RowArgs a)
           O::run(lds, tid, value, next, [&](int k, int m, int c, u32x4 v) {
             const int left = a.N - n_first - c;
             if (at_lo + m >= at_hi || left <= 0) return;
-            const T* const from = reinterpret_cast<const T*>(X + x_at(k));
-            put_some(k, m, c, where_positive<T>(v, left >= kVec<T> ? load16(from) : load_few(from, left)));
+            const X_t* const from = x_at(k);
+            put_some(k, m, c, Mask::apply(v, left >= kVec<T> ? Mask::load(from) : Mask::load_few(from, left)));
           });
           last(more);
         }
@@ -526,10 +547,12 @@ __global__ __launch_bounds__(256) void join_kernel(const RowArgs a) {
   }
 }
 
-// Joins the runs of k and finishes as kStore (STORE) or kStoreInput do: four
+// Joins the runs of k and finishes as kStore, kStoreInput or kStoreInputCodes do: four
 // columns of a row a thread.
-template <typename T, bool STORE>
+template <typename T, int EPI>
 __global__ __launch_bounds__(256) void join_k_kernel(const RowArgs a) {
+  constexpr bool STORE = EPI == kStore;
+  using X_t = typename std::conditional<EPI == kStoreInputCodes, int8_t, T>::type;
   const int across = (a.N + 3) / 4;
   int end = a.n;
   if (a.offsets) {
@@ -570,7 +593,7 @@ __global__ __launch_bounds__(256) void join_k_kernel(const RowArgs a) {
   for (int r = 0; r < 4; ++r) {
     if (r >= left) break;
     const float y = v[r];
-    const bool keep = STORE || !a.X || (float)static_cast<const T*>(a.X)[row * a.ldx + n + r] > 0.f;
+    const bool keep = STORE || !a.X || (float)static_cast<const X_t*>(a.X)[row * a.ldx + n + r] > 0.f;
     static_cast<T*>(a.C)[row * a.ldc + n + r] = (T)(keep ? y : 0.f);
   }
 }
@@ -603,21 +626,26 @@ hipError_t launch_shape(const RowArgs& a, int shape, hipStream_t s) {
     default: return launch<T, Small, COLUMNS, EPI>(a, s);
   }
 }
-template <typename T, bool COLUMNS>
+template <typename T, bool COLUMNS, int EPI>
 hipError_t launch_split(const RowArgs& a, int shape, hipStream_t s) {
   hipError_t e = shape == 1 ? launch<T, Middle, COLUMNS, kPartial>(a, s) : launch<T, Small, COLUMNS, kPartial>(a, s);
   if (e != hipSuccess) return e;
   // k is cut only where the results are two rounds of tiles at most: some millions of them
   const int64_t quads = (int64_t)a.n * ((a.N + 3) / 4);
-  hipLaunchKernelGGL((join_k_kernel<T, !COLUMNS>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((join_k_kernel<T, EPI>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 template <typename T>
 hipError_t launch_type(const RowArgs& a, int shape, int epilogue, hipStream_t s) {
   switch (epilogue) {
-    case kStore: return a.splits > 1 ? launch_split<T, false>(a, shape, s) : launch_shape<T, false, kStore>(a, shape, s);
+    case kStore:
+      return a.splits > 1 ? launch_split<T, false, kStore>(a, shape, s) : launch_shape<T, false, kStore>(a, shape, s);
     case kStoreInput:
-      return a.splits > 1 ? launch_split<T, true>(a, shape, s) : launch_shape<T, true, kStoreInput>(a, shape, s);
+      return a.splits > 1 ? launch_split<T, true, kStoreInput>(a, shape, s)
+                          : launch_shape<T, true, kStoreInput>(a, shape, s);
+    case kStoreInputCodes:
+      return a.splits > 1 ? launch_split<T, true, kStoreInputCodes>(a, shape, s)
+                          : launch_shape<T, true, kStoreInputCodes>(a, shape, s);
     case kStats: return launch_shape<T, false, kStats>(a, shape, s);
     default: return launch_shape<T, false, kGradLogits>(a, shape, s);
   }

@@ -16,6 +16,8 @@
 // fp32, 34 us with the join (16.4 at the fp32 rate of the matrix cores). A block
 // keeps both accumulators and two stages, so one or two share a CU, and the start
 // and end of each group's sum wait. The join reads what the blocks leave.
+#include <type_traits>
+
 #include "learn_internal.h"
 #include "learn_tile.h"
 
@@ -39,10 +41,12 @@ __device__ __forceinline__ void store_some(T* p, f32x4 v, int left) {
   }
 }
 
-template <typename T, class S>
+// CODES: Q is int8 codes with a scale a row.
+template <typename T, class S, bool CODES>
 __global__ __launch_bounds__(S::NT, S::MI * S::NJ >= 32 ? 2 : 3) void sums_kernel(const SumArgs a) {
   using P = ColTile<T, S::BM, S::NT, S::D, S::SB>;
-  using Q = ColTile<T, S::BN, S::NT, S::D, S::SB>;
+  using Q = typename std::conditional<CODES, CodeTile<T, S::BN, S::NT, S::D, S::SB>,
+                                      ColTile<T, S::BN, S::NT, S::D, S::SB>>::type;
   using Product = Sum<T, S, P, Q, true>;
   __shared__ __attribute__((aligned(16))) char lds[2 * Product::kBuf];
   __shared__ Groups groups;
@@ -95,7 +99,7 @@ __global__ __launch_bounds__(S::NT, S::MI * S::NJ >= 32 ? 2 : 3) void sums_kerne
     const bool bias = a.db && ct == 0 && wn == 0;
     // rows to leave out are looked at one by one only where there are any
     const uint8_t* live = nullptr;
-    if (a.live) {
+    if (!CODES && a.live) {
       int out = 0;
       for (int i = lo + tid; i < hi; i += S::NT) out |= !a.live[i];
       if (__syncthreads_or(out)) live = a.live;
@@ -105,7 +109,8 @@ __global__ __launch_bounds__(S::NT, S::MI * S::NJ >= 32 ? 2 : 3) void sums_kerne
     x.steps = (hi - lo + P::kStage - 1) / P::kStage;
     x.alone = bias;
     x.p.init(static_cast<const T*>(a.P), a.ldp, m_first, a.M, lo, hi, tid);
-    x.q.init(static_cast<const T*>(a.Q), a.ldq, n_first, a.N, lo, hi, tid, live);
+    if constexpr (CODES) x.q.init(static_cast<const int8_t*>(a.Q), a.scale, a.ldq, n_first, a.N, lo, hi, tid);
+    else x.q.init(static_cast<const T*>(a.Q), a.ldq, n_first, a.N, lo, hi, tid, live);
     x.begin();   // a part of the line is not empty
     x.first_stage();
     x.run();
@@ -221,11 +226,11 @@ using Large = Shape<2, 4, 8, 4, 2, 64>;    // 256 x 256, 512 threads
 using Middle = Shape<2, 2, 4, 4, 2, 64>;   // 128 x 128
 using Small = Shape<2, 2, 2, 2, 4, 64>;    // 64 x 64
 
-template <typename T, class S>
+template <typename T, class S, bool CODES>
 hipError_t launch(const SumArgs& a, hipStream_t s) {
   const int tiles = a.row_tiles * a.col_tiles;
   if (a.parts > 0) {
-    hipLaunchKernelGGL((sums_kernel<T, S>), dim3((unsigned)(a.parts * tiles)), dim3(S::NT), 0, s, a);
+    hipLaunchKernelGGL((sums_kernel<T, S, CODES>), dim3((unsigned)(a.parts * tiles)), dim3(S::NT), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -239,12 +244,12 @@ hipError_t launch(const SumArgs& a, hipStream_t s) {
                      dim3(256), 0, s, a, share);
   return hipGetLastError();
 }
-template <typename T>
+template <typename T, bool CODES>
 hipError_t launch_type(const SumArgs& a, int shape, hipStream_t s) {
   switch (shape) {
-    case 0: return launch<T, Large>(a, s);
-    case 1: return launch<T, Middle>(a, s);
-    default: return launch<T, Small>(a, s);
+    case 0: return launch<T, Large, CODES>(a, s);
+    case 1: return launch<T, Middle, CODES>(a, s);
+    default: return launch<T, Small, CODES>(a, s);
   }
 }
 
@@ -312,7 +317,8 @@ SumPlan plan_sums(int dtype, int64_t n, int64_t G, int64_t M, int64_t N, int cus
 }
 
 hipError_t launch_sums(const SumArgs& a, int dtype, int shape, hipStream_t s) {
-  return dtype == IM_BF16 ? launch_type<__bf16>(a, shape, s) : launch_type<float>(a, shape, s);
+  if (a.scale) return dtype == IM_BF16 ? launch_type<__bf16, true>(a, shape, s) : launch_type<float, true>(a, shape, s);
+  return dtype == IM_BF16 ? launch_type<__bf16, false>(a, shape, s) : launch_type<float, false>(a, shape, s);
 }
 
 hipError_t launch_bias_sum(const int32_t* offsets, int G, int n, int step, const float* part, int64_t width, float* db,

@@ -10,9 +10,9 @@
 //
 // A stage is SB = 64 or 128 bytes of k. Fragments are those of
 // v_mfma_f32_16x16x32_bf16: lane l holds row l % 16, 8 values of k from
-// 8 (l / 16). For fp32 a fragment is 4 values of k from 4 (l / 16), used by
-// four v_mfma_f32_16x16x4_f32 in turn (the sum runs over the same k in another
-// order). Products go in with the operands swapped, so that a lane's four
+// 8 (l / 16); for int8 v_mfma_i32_16x16x64_i8, 16 values from 16 (l / 16). For
+// fp32 a fragment is 4 values of k from 4 (l / 16), used by four
+// v_mfma_f32_16x16x4_f32 in turn (the sum runs over the same k in another order). Products go in with the operands swapped, so that a lane's four
 // results are four neighbouring n of one m.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -26,6 +26,7 @@ namespace learn {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));   // gfx950 loads 16 bytes from any address
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -63,7 +64,12 @@ __device__ __forceinline__ u32x4 where_positive(u32x4 v, u32x4 x) {
 
 template <typename T>
 __device__ __forceinline__ u32x4 load16(const T* p) {
-  return *reinterpret_cast<const u32x4_any*>(p);
+  if constexpr (sizeof(T) == 1) {
+    typedef u32x4 any __attribute__((aligned(1)));
+    return *reinterpret_cast<const any*>(p);
+  } else {
+    return *reinterpret_cast<const u32x4_any*>(p);
+  }
 }
 
 // The last `n` elements of a unit, moved to its front; zeros behind them.
@@ -265,10 +271,144 @@ struct ColTile {
   }
 };
 
+// Codes of a 16-byte unit of T: as many int8 as it has elements.
+template <typename T> struct CodeUnit { using type = uint32_t; };
+template <> struct CodeUnit<__bf16> { using type = uint64_t; };
+
+template <typename T>
+__device__ __forceinline__ typename CodeUnit<T>::type load_codes(const int8_t* p) {
+  typename CodeUnit<T>::type v;
+  __builtin_memcpy(&v, p, sizeof(v));
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ typename CodeUnit<T>::type load_few_codes(const int8_t* p, int n) {
+  typename CodeUnit<T>::type v = 0;
+#pragma unroll
+  for (int i = 0; i < kVec<T>; ++i)
+    if (i < n) v |= (typename CodeUnit<T>::type)(uint8_t)p[i] << (8 * i);
+  return v;
+}
+// A unit of scale times code in fp32, for bf16 rounded once more. That is 2^-8 of a value at
+// most, which rounding to the code left already of the largest (and more of the others: measured on
+// normal rows 0.0017 of the norm against 0.011); a scale that is a power of two would need no
+// rounding here, but up to doubles the codes' own error.
+template <typename T>
+__device__ __forceinline__ u32x4 decode(typename CodeUnit<T>::type q, float scale) {
+  T o[kVec<T>];
+#pragma unroll
+  for (int i = 0; i < kVec<T>; ++i) o[i] = (T)(scale * (float)(int8_t)(q >> (8 * i)));
+  u32x4 v;
+  __builtin_memcpy(&v, o, 16);
+  return v;
+}
+// A unit of results where the code is above zero, else zeros. bf16: a code in the upper byte of
+// 16 bits has its sign and is zero with it.
+template <typename T>
+__device__ __forceinline__ u32x4 where_code_positive(u32x4 v, typename CodeUnit<T>::type q) {
+  if constexpr (sizeof(T) == 2) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    typedef short i16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = i < 2 ? (uint32_t)q : (uint32_t)(q >> 32), vi = v[i];
+      // bytes 0 and 1, or 2 and 3, of w above zero bytes
+      const uint32_t spread = __builtin_amdgcn_perm(w, 0u, (i & 1) ? 0x07000600u : 0x05000400u);
+      const u16x2 m = __builtin_bit_cast(u16x2, __builtin_elementwise_max(__builtin_bit_cast(i16x2, spread), i16x2{0, 0}));
+      const u16x2 out = __builtin_bit_cast(u16x2, vi) * __builtin_elementwise_min(m, u16x2{1, 1});
+      v[i] = __builtin_bit_cast(uint32_t, out);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (int8_t)(q >> (8 * i)) > 0 ? v[i] : 0u;
+  }
+  return v;
+}
+
+// A column tile (as ColTile, and with its place in LDS) of T whose memory rows are int8 codes, each
+// with a scale: they become T on the way to LDS.
+template <typename T, int COLS, int NT, int D, int SB>
+struct CodeTile {
+  using To = ColTile<T, COLS, NT, D, SB>;
+  using Unit = typename CodeUnit<T>::type;
+  static constexpr int kRowUnits = To::kRowUnits, kStage = To::kStage, kUnits = To::kUnits, kEvery = To::kEvery,
+                       kBytes = To::kBytes;
+  const int8_t* p;       // as in ColTile
+  const float* scale;    // of the thread's first row of k
+  int64_t ld;
+  int first, n;
+  bool edge, narrow;
+  int k0, k_end;
+  Unit r[D][kUnits];
+  float s[D][kUnits];
+  int tid;
+
+  __device__ __forceinline__ void init(const int8_t* base, const float* scales, int64_t ld_, int from, int C, int k0_,
+                                       int k_end_, int tid_) {
+    ld = ld_;
+    tid = tid_;
+    k0 = k0_;
+    k_end = k_end_;
+    first = tid / kRowUnits;
+    const int c = from + (tid % kRowUnits) * kVec<T>;
+    n = clamp_units(C - c, kVec<T>);
+    edge = from + COLS > C;
+    narrow = C < kVec<T>;
+    p = base + (k0 + first) * ld + (n == kVec<T> ? c : (narrow ? 0 : C - kVec<T>));
+    scale = scales + k0 + first;
+  }
+  __device__ __forceinline__ int whole() const { return narrow ? 0 : (k_end - k0) / kStage; }
+  template <int SLOT>
+  __device__ __forceinline__ void load_whole(int kt) {
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      const int k = kt * kStage + i * kEvery;
+      r[SLOT][i] = load_codes<T>(p + (int64_t)k * ld);
+      s[SLOT][i] = scale[k];
+    }
+  }
+  template <int SLOT>
+  __device__ __forceinline__ void load(int kt) {
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      const int k = kt * kStage + i * kEvery, last = k_end - 1 - k0 - first;   // k to read, and the last there is
+      const int at = k < last ? k : last;
+      const int8_t* q = p + (int64_t)at * ld;
+      if (narrow) r[SLOT][i] = n > 0 ? load_few_codes<T>(q, n) : 0;
+      else r[SLOT][i] = load_codes<T>(q);
+      s[SLOT][i] = scale[at];
+    }
+  }
+  template <int SLOT>
+  __device__ __forceinline__ void store(int kt, char* lds) {
+    if (edge && !narrow) {   // what exists, moved to the front
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) r[SLOT][i] = n > 0 ? r[SLOT][i] >> (8 * (kVec<T> - n)) : 0;
+    }
+    const bool end = k0 + (kt + 1) * kStage > k_end;
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      const int idx = tid + i * NT;
+      u32x4 v = decode<T>(r[SLOT][i], s[SLOT][i]);
+      if (end && k0 + first + kt * kStage + i * kEvery >= k_end) v = u32x4{0, 0, 0, 0};
+      *reinterpret_cast<u32x4*>(lds + To::at(idx / kRowUnits) + (idx % kRowUnits) * 16) = v;
+    }
+  }
+  static __device__ __forceinline__ u32x4 frag(const char* lds, int m0, int s, int lane) {
+    return To::frag(lds, m0, s, lane);
+  }
+};
+
+// Four results of a lane.
+template <typename T> struct Results { using type = f32x4; };
+template <> struct Results<int8_t> { using type = i32x4; };
+
 // acc[r] += sum over the fragment's k of Q[4 (lane / 16) + r] P[lane % 16]
 template <typename T>
-__device__ __forceinline__ f32x4 mma(u32x4 q, u32x4 p, f32x4 acc) {
-  if constexpr (sizeof(T) == 2) {
+__device__ __forceinline__ typename Results<T>::type mma(u32x4 q, u32x4 p, typename Results<T>::type acc) {
+  if constexpr (sizeof(T) == 1) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, q), __builtin_bit_cast(i32x4, p), acc, 0, 0, 0);
+  } else if constexpr (sizeof(T) == 2) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, q), __builtin_bit_cast(bf16x8, p), acc, 0,
                                                    0, 0);
   } else {
@@ -316,7 +456,7 @@ struct Sum {
   char* lds;
   int steps;
   bool alone;
-  f32x4 acc[S::MI][S::NJ];
+  typename Results<T>::type acc[S::MI][S::NJ];
   float sum[ALONE ? S::MI : 1];
 
   template <int SLOT, bool WHOLE>
@@ -389,7 +529,7 @@ struct Sum {
 #pragma unroll
     for (int i = 0; i < S::MI; ++i) {
 #pragma unroll
-      for (int j = 0; j < S::NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < S::NJ; ++j) acc[i][j] = typename Results<T>::type{};
       if constexpr (ALONE) sum[i] = 0.f;
     }
     __syncthreads();

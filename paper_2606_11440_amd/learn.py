@@ -13,7 +13,11 @@ side in one buffer are not).
 
 The functions keep the C names (im_linear_forward, im_linear_backward,
 im_head_forward, im_head_backward, and im_linear_workspace and im_head_workspace
-for the size of a workspace that a program keeps); AdamW holds an im_adamw plan."""
+for the size of a workspace that a program keeps); AdamW holds an im_adamw plan.
+Around experts: im_router_forward, im_router_backward, im_dispatch_plan,
+im_dispatch_forward, im_dispatch_backward, im_combine_forward, im_combine_backward.
+Rows in 8 bits: im_rows_pack, im_rows_unpack, im_linear_forward_packed,
+im_linear_backward_packed (their codes are int8 tensors, the scales float32)."""
 from __future__ import annotations
 
 import ctypes
@@ -24,7 +28,12 @@ from ._lib import HERE, IM_BF16, IM_EINVAL, IM_F32, IM_OK, IMError, _stream
 LEARN_PATH = os.path.join(HERE, "libinframind_learn.so")
 LEARN_EXPORTED = ("im_linear_workspace", "im_linear_forward", "im_linear_backward", "im_head_workspace",
                   "im_head_forward", "im_head_backward", "im_adamw_create", "im_adamw_step", "im_adamw_destroy",
-                  "im_learn_last_error")
+                  "im_learn_last_error", "im_router_forward", "im_router_backward", "im_dispatch_workspace",
+                  "im_dispatch_plan", "im_dispatch_forward", "im_dispatch_backward", "im_combine_forward",
+                  "im_combine_backward", "im_rows_pack", "im_rows_unpack", "im_linear_workspace_packed",
+                  "im_linear_forward_packed", "im_linear_backward_packed")
+IM_CODES = 2
+SCORES = {"softmax": 0, "sigmoid": 1}
 IM_MAX_GROUPS, IM_MAX_DIM, IM_MAX_CLASSES, IM_STATE_BLOCK = 1024, 65536, 1 << 22, 256
 
 _P, _I32, _I64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
@@ -38,6 +47,21 @@ class ImLinearDesc(ctypes.Structure):
 class ImHeadDesc(ctypes.Structure):
     _fields_ = [("n_groups", _I32), ("n_rows", _I32), ("dim", _I32), ("n_classes", _I32), ("dtype", _I32),
                 ("relu_in", _I32), ("reserved0", _I32), ("reserved1", _I32), ("ld_h", _I64), ("ld_dh", _I64)]
+
+
+class ImRouterDesc(ctypes.Structure):
+    _fields_ = [("n_rows", _I32), ("n_experts", _I32), ("top_k", _I32), ("n_sets", _I32), ("top_sets", _I32),
+                ("set_best", _I32), ("dtype", _I32), ("score", _I32), ("renorm", _I32), ("scale", ctypes.c_float),
+                ("ld_z", _I64), ("ld_dz", _I64)]
+
+
+class ImDispatchDesc(ctypes.Structure):
+    _fields_ = [("n_rows", _I32), ("top_k", _I32), ("n_experts", _I32), ("n_slots", _I32), ("dim", _I32),
+                ("dtype", _I32), ("ld_row", _I64), ("ld_slot", _I64), ("ld_dslot", _I64)]
+
+
+class ImRowsDesc(ctypes.Structure):
+    _fields_ = [("n_rows", _I32), ("dim", _I32), ("dtype", _I32), ("keep", _I32), ("ld_x", _I64), ("ld_codes", _I64)]
 
 
 class ImAdamwTensor(ctypes.Structure):
@@ -69,6 +93,19 @@ def load_learn() -> ctypes.CDLL:
     L.im_adamw_destroy.argtypes = [_P]
     L.im_adamw_destroy.restype = None
     L.im_learn_last_error.restype = ctypes.c_char_p
+    L.im_router_forward.argtypes = [_P] * 7
+    L.im_router_backward.argtypes = [_P] * 8
+    L.im_dispatch_workspace.argtypes = [_P, _P]
+    L.im_dispatch_plan.argtypes = [_P] * 5 + [_I64, _P, _P]
+    L.im_dispatch_forward.argtypes = [_P] * 6
+    L.im_dispatch_backward.argtypes = [_P] * 6
+    L.im_combine_forward.argtypes = [_P] * 7
+    L.im_combine_backward.argtypes = [_P] * 9
+    L.im_rows_pack.argtypes = [_P] * 5
+    L.im_rows_unpack.argtypes = [_P] * 5
+    L.im_linear_workspace_packed.argtypes = [_P, _I32, _P]
+    L.im_linear_forward_packed.argtypes = [_P] * 9 + [_I64, _P, _P]
+    L.im_linear_backward_packed.argtypes = [_P] * 10 + [_I64, _P, _P]
     _learn = L
     return L
 
@@ -135,12 +172,16 @@ def _flat(t, name, dtype, device, count):
 _KINDS = {}
 
 
+def _kinds():
+    import torch
+    _KINDS.update({torch.float32: IM_F32, torch.bfloat16: IM_BF16, "f32": torch.float32, "i32": torch.int32,
+                   "i64": torch.int64, "u8": torch.uint8, "i8": torch.int8, "fp8": torch.float8_e4m3fn})
+
+
 def _kind(t, name):
     """im_dtype of a tensor on a GPU."""
     if not _KINDS:
-        import torch
-        _KINDS.update({torch.float32: IM_F32, torch.bfloat16: IM_BF16, "f32": torch.float32, "i32": torch.int32,
-                       "i64": torch.int64, "u8": torch.uint8, "fp8": torch.float8_e4m3fn})
+        _kinds()
     if t.device.type != "cuda":
         _bad(f"{name} is on {t.device}, a GPU is expected")
     k = _KINDS.get(t.dtype)
@@ -328,6 +369,228 @@ def im_head_backward(h, W, b, target, lse, dlogp, dh=None, dW=None, db=None, val
                                  None if dh is None else dh.data_ptr(), _flat(dW, "dW", dt, dev, G * V * k),
                                  _flat(db, "db", f32, dev, G * V), at, size, _flat(error, "error", i32, dev, 1),
                                  _stream(stream)))
+
+
+def _mask(valid, n, classes, dev):
+    """Pointer of the words of a mask [n, ceil(classes / 32)], or None."""
+    if valid is None:
+        return None
+    if valid.dtype is not _KINDS["i32"] and str(valid.dtype) != "torch.uint32":
+        _bad(f"valid is {valid.dtype}: int32 (or uint32) words expected")
+    return _flat(valid, "valid", valid.dtype, dev, n * ((classes + 31) // 32))
+
+
+def _matrix_of(t, name):
+    """Rows and columns of a tensor that must be a matrix."""
+    return t.shape if t.dim() == 2 else _bad(f"{name} is not a matrix")
+
+
+def _score(score):
+    if score not in SCORES:
+        _bad(f"score is {score!r}: 'softmax' or 'sigmoid' expected")
+    return SCORES[score]
+
+
+def im_router_forward(z, expert, weight, bias=None, valid=None, score="softmax", renorm=True, scale=1.0, n_sets=1,
+                      top_sets=None, set_best=1, stream=None):
+    """Choice of experts [n, top_k] (int32; -1: none left) and their weights (float32)
+    from logits z [n, experts], whose rows may be strided. score: "softmax" or "sigmoid";
+    the choice goes by score + bias (float32 [experts]) within the top_sets best of
+    n_sets equal sets, valued by their set_best (1 or 2) best; weights are scale times the
+    scores, divided by their sum with renorm. valid: as for im_head_forward."""
+    kind, dev, dt = _kind(z, "z"), z.device, z.dtype
+    n, E = _matrix_of(z, "z")
+    ld = _matrix(z, "z", dt, dev, n, E)
+    k = _matrix_of(expert, "expert")[1]
+    f32, i32 = _KINDS["f32"], _KINDS["i32"]
+    L = _learn or load_learn()
+    d = ImRouterDesc(n, E, k, n_sets, n_sets if top_sets is None else top_sets, set_best, kind, _score(score),
+                     1 if renorm else 0, scale, ld, 0)
+    with _On(dev.index):
+        _done(L.im_router_forward(ctypes.byref(d), z.data_ptr(), _flat(bias, "bias", f32, dev, E),
+                                  _mask(valid, n, E, dev), _flat(expert, "expert", i32, dev, n * k),
+                                  _flat(weight, "weight", f32, dev, n * k), _stream(stream)))
+
+
+def im_router_backward(z, expert, dweight, dz, valid=None, score="softmax", renorm=True, scale=1.0, error=None,
+                       stream=None):
+    """Gradient dz [n, experts] of the logits from dweight (float32 [n, top_k]), for the
+    experts that im_router_forward chose. Rows of z and dz may be strided."""
+    kind, dev, dt = _kind(z, "z"), z.device, z.dtype
+    n, E = _matrix_of(z, "z")
+    ld, ld_dz = _matrix(z, "z", dt, dev, n, E), _matrix(dz, "dz", dt, dev, n, E)
+    k = _matrix_of(expert, "expert")[1]
+    f32, i32 = _KINDS["f32"], _KINDS["i32"]
+    L = _learn or load_learn()
+    d = ImRouterDesc(n, E, k, 1, 1, 1, kind, _score(score), 1 if renorm else 0, scale, ld, ld_dz)
+    with _On(dev.index):
+        _done(L.im_router_backward(ctypes.byref(d), z.data_ptr(), _mask(valid, n, E, dev),
+                                   _flat(expert, "expert", i32, dev, n * k), _flat(dweight, "dweight", f32, dev, n * k),
+                                   dz.data_ptr(), _flat(error, "error", i32, dev, 1), _stream(stream)))
+
+
+def im_dispatch_workspace(n_rows, top_k, n_experts, device=None):
+    """Bytes of workspace of im_dispatch_plan; as im_linear_workspace."""
+    L = _learn or load_learn()
+    d = ImDispatchDesc(n_rows, top_k, n_experts, 0, 1, 0, 1, 1, 1)
+    return _size_of(lambda desc, backward, out: L.im_dispatch_workspace(desc, out), d, False, device)
+
+
+def im_dispatch_plan(expert, offsets, slot, workspace=None, error=None, stream=None):
+    """Places of the pairs of expert (int32 [n, top_k], -1: none) ordered by expert: slot
+    like expert, and offsets int32 [experts + 1], the groups of the layers that follow."""
+    if expert.device.type != "cuda":
+        _bad(f"expert is on {expert.device}, a GPU is expected")
+    if not _KINDS:
+        _kinds()
+    dev, i32 = expert.device, _KINDS["i32"]
+    n, k = _matrix_of(expert, "expert")
+    E = offsets.numel() - 1
+    L = _learn or load_learn()
+    d = ImDispatchDesc(n, k, E, 0, 1, 0, 1, 1, 1)
+    with _On(dev.index):
+        ws, at, size = _workspace(lambda desc, backward, out: L.im_dispatch_workspace(desc, out), d,
+                                  (4, dev.index, n, k, E), 0, workspace, dev, stream)
+        _done(L.im_dispatch_plan(ctypes.byref(d), _flat(expert, "expert", i32, dev, n * k),
+                                 _flat(offsets, "offsets", i32, dev, E + 1), _flat(slot, "slot", i32, dev, n * k), at,
+                                 size, _flat(error, "error", i32, dev, 1), _stream(stream)))
+
+
+def _exchange(rows, rows_name, slots, slots_name, slot, dslots=None, codes=False):
+    """Description of an exchange between rows [n, dim] and slots' rows [n_slots, dim]."""
+    if codes and str(rows.dtype) == "torch.int8" and rows.device.type == "cuda":
+        kind = IM_CODES
+    else:
+        kind = _kind(rows, rows_name)
+    dev, dt = rows.device, rows.dtype
+    n, dim = _matrix_of(rows, rows_name)
+    ld = _matrix(rows, rows_name, dt, dev, n, dim)
+    if slots is None:
+        slots, slots_name = dslots, "dys"
+    m, ld_slot = 0, dim
+    if slots is not None:
+        m = _matrix_of(slots, slots_name)[0]
+        ld_slot = _matrix(slots, slots_name, dt, dev, m, dim)
+    ld_dslot = dim if dslots is None else _matrix(dslots, "dys", dt, dev, m, dim)
+    k = _matrix_of(slot, "slot")[1]
+    if not _KINDS:
+        _kinds()
+    return ImDispatchDesc(n, k, 1, m, dim, kind, ld, ld_slot, ld_dslot), dev, _flat(slot, "slot", _KINDS["i32"], dev, n * k)
+
+
+def im_dispatch_forward(x, slot, xs, error=None, stream=None):
+    """xs[slot[i, c]] = x[i]: rows to their places (float32, bfloat16, or the int8 codes of
+    packed rows; rows of xs that no slot names stay as they are). Rows may be strided."""
+    d, dev, ps = _exchange(x, "x", xs, "xs", slot, codes=True)
+    with _On(dev.index):
+        _done((_learn or load_learn()).im_dispatch_forward(ctypes.byref(d), x.data_ptr(), ps, xs.data_ptr(),
+                                                           _flat(error, "error", _KINDS["i32"], dev, 1), _stream(stream)))
+
+
+def im_dispatch_backward(dxs, slot, dx, error=None, stream=None):
+    """dx[i] = sum of dxs[slot[i, c]] over c."""
+    d, dev, ps = _exchange(dx, "dx", dxs, "dxs", slot)
+    with _On(dev.index):
+        _done((_learn or load_learn()).im_dispatch_backward(ctypes.byref(d), dxs.data_ptr(), ps, dx.data_ptr(),
+                                                            _flat(error, "error", _KINDS["i32"], dev, 1), _stream(stream)))
+
+
+def im_combine_forward(ys, slot, weight, y, error=None, stream=None):
+    """y[i] = sum of weight[i, c] ys[slot[i, c]] over c (weight float32 like slot)."""
+    d, dev, ps = _exchange(y, "y", ys, "ys", slot)
+    with _On(dev.index):
+        _done((_learn or load_learn()).im_combine_forward(
+            ctypes.byref(d), ys.data_ptr(), ps, _flat(weight, "weight", _KINDS["f32"], dev, slot.numel()), y.data_ptr(),
+            _flat(error, "error", _KINDS["i32"], dev, 1), _stream(stream)))
+
+
+def im_combine_backward(dy, ys, slot, weight, dys=None, dweight=None, error=None, stream=None):
+    """Gradients of im_combine_forward: dys[slot[i, c]] = weight[i, c] dy[i] and dweight
+    (float32 like slot); None skips one."""
+    d, dev, ps = _exchange(dy, "dy", ys, "ys", slot, dys)
+    f32 = _KINDS["f32"]
+    with _On(dev.index):
+        _done((_learn or load_learn()).im_combine_backward(
+            ctypes.byref(d), dy.data_ptr(), None if ys is None else ys.data_ptr(), ps,
+            _flat(weight, "weight", f32, dev, slot.numel()), None if dys is None else dys.data_ptr(),
+            _flat(dweight, "dweight", f32, dev, slot.numel()), _flat(error, "error", _KINDS["i32"], dev, 1),
+            _stream(stream)))
+
+
+def _rows(x, codes, scale, keep):
+    kind, dev = _kind(x, "x"), x.device
+    n, dim = _matrix_of(x, "x")
+    d = ImRowsDesc(n, dim, kind, 1 if keep else 0, _matrix(x, "x", x.dtype, dev, n, dim),
+                   _matrix(codes, "codes", _KINDS["i8"], dev, n, dim))
+    return d, dev, _flat(scale, "scale", _KINDS["f32"], dev, n)
+
+
+def im_rows_pack(x, codes, scale, keep=False, stream=None):
+    """Rows in 8 bits: codes int8 [n, dim] and scale float32 [n] of x [n, dim] (float32 or
+    bfloat16), x = scale code up to half a scale. keep: what is not zero gets a code
+    that is not. Rows of x and codes may be strided."""
+    d, dev, ps = _rows(x, codes, scale, keep)
+    with _On(dev.index):
+        _done((_learn or load_learn()).im_rows_pack(ctypes.byref(d), x.data_ptr(), codes.data_ptr(), ps, _stream(stream)))
+
+
+def im_rows_unpack(codes, scale, x, stream=None):
+    """x = scale code in float32, rounded to its type."""
+    d, dev, ps = _rows(x, codes, scale, False)
+    with _On(dev.index):
+        _done((_learn or load_learn()).im_rows_unpack(ctypes.byref(d), codes.data_ptr(), ps, x.data_ptr(), _stream(stream)))
+
+
+def im_linear_workspace_packed(n_rows, in_dim, out_dim, dtype, n_groups=1, backward=False, device=None):
+    """Bytes of workspace of im_linear_forward_packed, or im_linear_backward_packed; as im_linear_workspace."""
+    d = ImLinearDesc(n_groups, n_rows, in_dim, out_dim, _kind_of(dtype), 0, 0, 0, in_dim, out_dim, in_dim)
+    return _size_of((_learn or load_learn()).im_linear_workspace_packed, d, backward, device)
+
+
+def im_linear_forward_packed(x, x_scale, W, W_scale, b, y, offsets=None, relu=False, workspace=None, error=None,
+                             stream=None):
+    """y = act(x_scale W_scale (x W_g^T) + b_g) from packed rows x (int8 [n, in], x_scale
+    float32 [n]) and packed weights W (int8 [groups, out, in] or [out, in], W_scale float32
+    [groups, out]); y float32 or bfloat16 [n, out]. Rows of x and y may be strided."""
+    kind, dev, dt = _kind(y, "y"), y.device, y.dtype
+    f32, i32, i8 = _KINDS["f32"], _KINDS["i32"], _KINDS["i8"]
+    n, k = _matrix_of(x, "x")
+    ld_x = _matrix(x, "x", i8, dev, n, k)
+    G, m = _weights(W, i8, dev, k)
+    ld_y = _matrix(y, "y", dt, dev, n, m)
+    L = _learn or load_learn()
+    d = ImLinearDesc(G, n, k, m, kind, 1 if relu else 0, 0, 0, ld_x, ld_y, 0)
+    with _On(dev.index):
+        ws, at, size = _workspace(L.im_linear_workspace_packed, d, (5, dev.index, G, n, k, m, kind), 0, workspace, dev, stream)
+        _done(L.im_linear_forward_packed(ctypes.byref(d), _offsets(offsets, G, dev), x.data_ptr(),
+                                         _flat(x_scale, "x_scale", f32, dev, n), W.data_ptr(),
+                                         _flat(W_scale, "W_scale", f32, dev, G * m), _flat(b, "b", f32, dev, G * m),
+                                         y.data_ptr(), at, size, _flat(error, "error", i32, dev, 1), _stream(stream)))
+
+
+def im_linear_backward_packed(dy, x, x_scale, W, dx=None, dW=None, db=None, offsets=None, relu_in=False,
+                              workspace=None, error=None, stream=None):
+    """Gradients of a layer as im_linear_backward's, with its input x kept as packed rows
+    (int8 [n, in], x_scale float32 [n]). relu_in: dx is zero where x's code is not above 0."""
+    kind, dev, dt = _kind(dy, "dy"), dy.device, dy.dtype
+    f32, i32 = _KINDS["f32"], _KINDS["i32"]
+    n, m = _matrix_of(dy, "dy")
+    k = _matrix_of(x, "x")[1]
+    ld_y = _matrix(dy, "dy", dt, dev, n, m)
+    ld_x = _matrix(x, "x", _KINDS["i8"], dev, n, k)
+    G, rows = _weights(W, dt, dev, k)
+    if rows != m:
+        _bad(f"W has {rows} outputs, dy {m}")
+    ld_dx = k if dx is None else _matrix(dx, "dx", dt, dev, n, k)
+    L = _learn or load_learn()
+    d = ImLinearDesc(G, n, k, m, kind, 0, 1 if relu_in else 0, 0, ld_x, ld_y, ld_dx)
+    with _On(dev.index):
+        ws, at, size = _workspace(L.im_linear_workspace_packed, d, (6, dev.index, G, n, k, m, kind), 1, workspace, dev, stream)
+        _done(L.im_linear_backward_packed(ctypes.byref(d), _offsets(offsets, G, dev), dy.data_ptr(), x.data_ptr(),
+                                          _flat(x_scale, "x_scale", f32, dev, n), W.data_ptr(),
+                                          None if dx is None else dx.data_ptr(), _flat(dW, "dW", dt, dev, G * m * k),
+                                          _flat(db, "db", f32, dev, G * m), at, size,
+                                          _flat(error, "error", i32, dev, 1), _stream(stream)))
 
 
 # Plans whose AdamW was dropped. To free one synchronises the device, which would spoil a graph
