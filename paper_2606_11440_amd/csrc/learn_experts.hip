@@ -36,6 +36,7 @@ RouterArgs router_args(const im_router_desc& d, const void* z, const uint32_t* v
   a.ld_z = d.ld_z;
   a.valid = valid;
   a.words = (d.n_experts + 31) / 32;
+  a.cus = compute_units();
   return a;
 }
 

@@ -139,6 +139,7 @@ struct RouterArgs {
   void* dz;
   int64_t ld_dz;
   int32_t* error;
+  int32_t cus;
 };
 hipError_t launch_router_forward(const RouterArgs& a, int dtype, int score, hipStream_t s);
 hipError_t launch_router_backward(const RouterArgs& a, int dtype, int score, hipStream_t s);

@@ -211,6 +211,7 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void packed_kernel(const RowArgs 
   using Q = RowTile<T, S::BN, S::NT, S::D, S::SB>;
   using Product = Sum<T, S, P, Q, false>;
   __shared__ __attribute__((aligned(16))) char lds[2 * Product::kBuf];
+  __shared__ __attribute__((aligned(16))) float sides[PARTIAL ? 4 : S::BM + 2 * S::BN];   // scales of rows, of columns, bias
   __shared__ Groups groups;
   groups.init(a.offsets, a.G, a.n, S::BM);
   __syncthreads();
@@ -226,6 +227,8 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void packed_kernel(const RowArgs 
   x.lds = lds;
   x.steps = (a.K + P::kStage - 1) / P::kStage;
   int rt, ct, g, lo, hi, split = 0;
+  static_assert(S::NT >= S::BM && S::NT >= S::BN, "a thread a row, a thread a column");
+  float side[3] = {0.f, 0.f, 0.f};   // the thread's row's and column's
   auto enter = [&](int t) {   // takes tile t: its first loads are on their way
     const int tid = fresh_thread();
     int k0 = 0, K = a.K;
@@ -241,6 +244,12 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void packed_kernel(const RowArgs 
     x.p.init(static_cast<const T*>(a.A) + k0, a.lda, lo, hi - 1, K, tid);
     x.q.init(static_cast<const T*>(a.B) + g * a.b_group + k0, a.ldb, ct * S::BN, a.N - 1, K, tid);
     x.begin();
+    if constexpr (!PARTIAL) {
+      const int row = lo + tid < hi ? lo + tid : hi - 1, col = ct * S::BN + tid < a.N ? ct * S::BN + tid : a.N - 1;
+      side[0] = scales.x[row];
+      side[1] = scales.W[(int64_t)g * a.N + col];
+      side[2] = a.bias ? a.bias[(int64_t)g * a.N + col] : 0.f;
+    }
   };
   enter(tile);
   x.first_stage();
@@ -249,7 +258,7 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void packed_kernel(const RowArgs 
     auto& acc = x.acc;
     const int tid = fresh_thread(), lane = tid % 64, wave = tid / 64, g4 = (lane / 16) * 4;
     const int wm = wave / S::WN, wn = wave % S::WN, m_at = wm * S::MI * 16 + lane % 16;
-    const int at_lo = lo, at_hi = hi, at_g = g, at_split = split, n_first = ct * S::BN;
+    const int at_lo = lo, at_hi = hi, at_split = split, n_first = ct * S::BN;
     tile += gridDim.x;
     const bool more = tile < total;
     auto next = [&] {
@@ -275,31 +284,28 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void packed_kernel(const RowArgs 
       });
       last(more);
     } else {
-      const int n_at = n_first + wn * S::NJ * 16 + g4;
-      const float* bias = a.bias ? a.bias + at_g * a.bias_group : nullptr;
-      const float* sw = scales.W + at_g * (int64_t)a.N;
-      f32x4 plus[S::NJ], times[S::NJ];
+      if (tid < S::BM) sides[tid] = side[0];
+      if (tid < S::BN) {
+        sides[S::BM + tid] = side[1];
+        sides[S::BM + S::BN + tid] = side[2];
+      }
+      __syncthreads();
+      const float least = a.relu ? 0.f : -INFINITY;
       float sx[S::MI];
 #pragma unroll
+      for (int i = 0; i < S::MI; ++i) sx[i] = sides[m_at + i * 16];
+      f32x4 out[S::MI][S::NJ];   // in the sums' place
+#pragma unroll
       for (int j = 0; j < S::NJ; ++j) {
-        plus[j] = times[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (n_at + j * 16 < a.N) {
-          times[j] = load4(sw + n_at + j * 16, a.N - n_at - j * 16);
-          if (bias) plus[j] = load4(bias + n_at + j * 16, a.N - n_at - j * 16);
-        }
-      }
+        const int c = (wn * S::NJ + j) * 16 + g4;
+        const f32x4 times = *reinterpret_cast<const f32x4*>(sides + S::BM + c);
+        const f32x4 plus = *reinterpret_cast<const f32x4*>(sides + S::BM + S::BN + c);
 #pragma unroll
-      for (int i = 0; i < S::MI; ++i) {
-        const int64_t row = (int64_t)at_lo + m_at + i * 16;
-        sx[i] = scales.x[row < at_hi ? row : at_hi - 1];
-      }
-      const float least = a.relu ? 0.f : -INFINITY;
-      auto value = [&](int i, int j) {
-        f32x4 v;
+        for (int i = 0; i < S::MI; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = finish(acc[i][j][r], sx[i], times[j][r], plus[j][r], least);
-        return v;
-      };
+          for (int r = 0; r < 4; ++r) out[i][j][r] = finish(acc[i][j][r], sx[i], times[r], plus[r], least);
+      }
+      auto value = [&](int i, int j) { return out[i][j]; };
       using O = Out<U, S, (int)sizeof(lds)>;
       char* const C = reinterpret_cast<char*>(static_cast<U*>(a.C) + (int64_t)at_lo * a.ldc + n_first);
       auto place = [&](int m, int c) { return ((uint32_t)m * (uint32_t)a.ldc + (uint32_t)c) * (uint32_t)sizeof(U); };
