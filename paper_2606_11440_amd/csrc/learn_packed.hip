@@ -64,6 +64,19 @@ __device__ __forceinline__ uint32_t most_bits(u32x4 v, uint32_t most) {
   return most;
 }
 
+// Largest over L neighbouring lanes (most_bits' integers: no sign).
+template <int L>
+__device__ __forceinline__ uint32_t most_across(uint32_t x) {
+  int32_t v = (int32_t)x;
+  if constexpr (L > 1) v = max(v, dpp<0xB1>(v));     // quad_perm [1,0,3,2]
+  if constexpr (L > 2) v = max(v, dpp<0x4E>(v));     // quad_perm [2,3,0,1]
+  if constexpr (L > 4) v = max(v, dpp<0x141>(v));    // half-row mirror
+  if constexpr (L > 8) v = max(v, dpp<0x140>(v));    // row mirror
+  if constexpr (L > 16) v = max(v, xshfl<16>(v));
+  if constexpr (L > 32) v = max(v, xshfl<32>(v));
+  return (uint32_t)v;
+}
+
 struct Scale {
   float scale, inverse;   // not finite: NaN and 0
   __device__ __forceinline__ explicit Scale(uint32_t most) {
@@ -98,36 +111,40 @@ __device__ __forceinline__ void put_codes(int8_t* row, int u, int dim, u32x4 v, 
   }
 }
 
-// L lanes a row, N units a lane, kept in registers between the largest magnitude and the codes.
-template <typename T, int L, int N>
+// L lanes a row, N units a lane and R rows at once, kept in registers between the largest magnitude and
+// the codes.
+template <typename T, int L, int N, int R>
 __global__ __launch_bounds__(256) void pack_kernel(const PackArgs a) {
-  constexpr int kRows = 256 / L;
+  constexpr int kRows = 256 / L;   // of a block, R times
   const int l = (int)threadIdx.x % L, units = (a.dim + kVec<T> - 1) / kVec<T>;
-  for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.n; first += (int64_t)gridDim.x * kRows) {
-    const int64_t at = first + (int)threadIdx.x / L, row = at < a.n ? at : a.n - 1;
-    const T* from = static_cast<const T*>(a.x) + row * a.ld_x;
-    u32x4 v[N];
+  for (int64_t first = (int64_t)blockIdx.x * (kRows * R); first < a.n; first += (int64_t)gridDim.x * (kRows * R)) {
+    const int64_t at = first + (int)threadIdx.x / L;
+    u32x4 v[R][N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int u = l + i * L;
-      v[i] = u < units ? unit_load<T>(from, u, a.dim) : u32x4{0, 0, 0, 0};
+    for (int k = 0; k < R; ++k) {
+      const int64_t row = at + k * kRows < a.n ? at + k * kRows : a.n - 1;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int u = l + i * L;
+        v[k][i] = unit_load<T>(static_cast<const T*>(a.x) + row * a.ld_x, u < units ? u : units - 1, a.dim);
+      }
     }
-    uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) most = most_bits<T>(v[i], most);
+    for (int k = 0; k < R; ++k) {
+      uint32_t most = 0;
 #pragma unroll
-    for (int d = 1; d < L; d *= 2) {
-      const uint32_t o = (uint32_t)__shfl_xor((int)most, d);
-      most = o > most ? o : most;
+      for (int i = 0; i < N; ++i) most = most_bits<T>(v[k][i], most);
+      most = most_across<L>(most);
+      const int64_t row = at + k * kRows;
+      if (row >= a.n) continue;   // the last block's other lanes
+      const Scale s(most);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int u = l + i * L;
+        if (u < units) put_codes<T>(a.codes + row * a.ld_codes, u, a.dim, v[k][i], s, a.keep != 0);
+      }
+      if (l == 0) a.scale[row] = s.scale;
     }
-    if (at >= a.n) continue;   // the last block's other lanes
-    const Scale s(most);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int u = l + i * L;
-      if (u < units) put_codes<T>(a.codes + row * a.ld_codes, u, a.dim, v[i], s, a.keep != 0);
-    }
-    if (l == 0) a.scale[row] = s.scale;
   }
 }
 
@@ -200,8 +217,7 @@ __device__ __forceinline__ f32x4 load4(const float* p, int left) {
 
 // y = act(sx sw sum + b) of one result.
 __device__ __forceinline__ float finish(int sum, float sx, float sw, float b, float least) {
-  const float v = fmaf((float)sum * sx, sw, b);
-  return v < least ? least : v;   // NaN stays
+  return __builtin_elementwise_maximum(fmaf((float)sum * sx, sw, b), least);   // NaN stays
 }
 
 template <typename U, class S, bool PARTIAL>
@@ -386,27 +402,27 @@ hipError_t launch_type(const RowArgs& a, const PackedScales& p, int shape, hipSt
   }
 }
 
-template <typename T, int L>
+template <typename T, int L, int N, int R>
 hipError_t pack_rows(const PackArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((pack_kernel<T, L, 1>), dim3(blocks_of(a.n, 256 / L)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((pack_kernel<T, L, N, R>), dim3(blocks_of(a.n, 256 / L * R)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
-template <typename T, int N>
-hipError_t pack_wide(const PackArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((pack_kernel<T, 64, N>), dim3(blocks_of(a.n, 4)), dim3(256), 0, s, a);
-  return hipGetLastError();
+// R rows at once where there are enough to fill the card so; single ones otherwise.
+template <typename T, int L, int N, int R>
+hipError_t pack_some(const PackArgs& a, hipStream_t s) {
+  return a.n >= 4096 * 64 / L * R ? pack_rows<T, L, N, R>(a, s) : pack_rows<T, L, N, 1>(a, s);
 }
 template <typename T>
 hipError_t pack(const PackArgs& a, hipStream_t s) {
   const int units = (a.dim + kVec<T> - 1) / kVec<T>;
-  if (units <= 4) return pack_rows<T, 4>(a, s);
-  if (units <= 8) return pack_rows<T, 8>(a, s);
-  if (units <= 16) return pack_rows<T, 16>(a, s);
-  if (units <= 32) return pack_rows<T, 32>(a, s);
-  if (units <= 64) return pack_rows<T, 64>(a, s);
-  if (units <= 128) return pack_wide<T, 2>(a, s);
-  if (units <= 256) return pack_wide<T, 4>(a, s);
-  if (units <= 512) return pack_wide<T, 8>(a, s);
+  if (units <= 4) return pack_some<T, 4, 1, 4>(a, s);
+  if (units <= 8) return pack_some<T, 8, 1, 4>(a, s);
+  if (units <= 16) return pack_some<T, 16, 1, 4>(a, s);
+  if (units <= 32) return pack_some<T, 32, 1, 4>(a, s);
+  if (units <= 64) return pack_some<T, 64, 1, 4>(a, s);
+  if (units <= 128) return pack_some<T, 64, 2, 2>(a, s);
+  if (units <= 256) return pack_rows<T, 64, 4, 1>(a, s);
+  if (units <= 512) return pack_rows<T, 64, 8, 1>(a, s);
   hipLaunchKernelGGL(pack_long_kernel<T>, dim3(blocks_of(a.n, 1)), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
