@@ -216,11 +216,13 @@ __device__ __forceinline__ f32x4 load4(const float* p, int left) {
 }
 
 // y = act(sx sw sum + b) of one result.
-__device__ __forceinline__ float finish(int sum, float sx, float sw, float b, float least) {
-  return __builtin_elementwise_maximum(fmaf((float)sum * sx, sw, b), least);   // NaN stays
+template <bool RELU>
+__device__ __forceinline__ float finish(int sum, float sx, float sw, float b) {
+  const float v = fmaf((float)sum * sx, sw, b);
+  return RELU ? __builtin_elementwise_maximum(v, 0.f) : v;   // NaN stays
 }
 
-template <typename U, class S, bool PARTIAL>
+template <typename U, class S, bool PARTIAL, bool RELU>
 __global__ __launch_bounds__(S::NT, S::kWaves) void packed_kernel(const RowArgs a, const PackedScales scales) {
   using T = int8_t;
   using P = RowTile<T, S::BM, S::NT, S::D, S::SB>;
@@ -306,7 +308,6 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void packed_kernel(const RowArgs 
         sides[S::BM + S::BN + tid] = side[2];
       }
       __syncthreads();
-      const float least = a.relu ? 0.f : -INFINITY;
       float sx[S::MI];
 #pragma unroll
       for (int i = 0; i < S::MI; ++i) sx[i] = sides[m_at + i * 16];
@@ -319,7 +320,7 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void packed_kernel(const RowArgs 
 #pragma unroll
         for (int i = 0; i < S::MI; ++i)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) out[i][j][r] = finish(acc[i][j][r], sx[i], times[r], plus[r], least);
+          for (int r = 0; r < 4; ++r) out[i][j][r] = finish<RELU>(acc[i][j][r], sx[i], times[r], plus[r]);
       }
       auto value = [&](int i, int j) { return out[i][j]; };
       using O = Out<U, S, (int)sizeof(lds)>;
@@ -340,6 +341,214 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void packed_kernel(const RowArgs 
       }
     }
     if (!more) break;
+  }
+}
+
+// The same product for large tiles of rows that are whole 16-byte units at 16-byte addresses: the
+// operands go from memory to LDS without registers (global_load_lds_dwordx4), which leaves room for the
+// fragments of a stage while the next one's are read. Three buffers of 64 bytes of k: stage t is multiplied
+// from registers, t + 1 is read from LDS, t + 2 is on its way, and t + 3 is asked for once every wave has
+// t in registers (one barrier a stage). Two blocks of 256 x 128 share a CU, so that one's products run
+// beside the other's results and first loads; a block's results leave through the third buffer while the first
+// two take the next tile's stages.
+//
+// The loads are written in assembly, and so are the waits for them: the compiler would have every read of
+// LDS wait for all of them. They write no register, and a wave's loads and stores end in their order.
+struct Deep {
+  static constexpr int kThreads = 256, kRows = 256, kCols = 128, kBytes = 64, kBuffers = 3;
+  static constexpr int kRowBytes = kRows * kBytes, kBuffer = kRowBytes + kCols * kBytes;
+  static constexpr int kLoads = kBuffer / 16 / kThreads;   // of a thread, a stage
+};
+
+__device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, const char* base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
+template <int LEFT>
+__device__ __forceinline__ void wait_loads() {   // until that many are on their way at most
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+}
+__device__ __forceinline__ void barrier_behind_lds() {   // a barrier behind the wave's own LDS reads and writes
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  return reinterpret_cast<const char*>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
+                                       (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v));
+}
+
+template <typename U, bool RELU>
+__global__ __launch_bounds__(Deep::kThreads, 2) void packed_deep_kernel(const RowArgs a, const PackedScales scales) {
+  using S = Shape<2, 2, 8, 4, 1, Deep::kBytes>;
+  using Tile = RowTile<int8_t, Deep::kRows, Deep::kThreads, 1, Deep::kBytes>;
+  static_assert(S::BM == Deep::kRows && S::BN == Deep::kCols && S::NT == Deep::kThreads, "the tile's");
+  __shared__ __attribute__((aligned(1024))) char lds[Deep::kBuffers * Deep::kBuffer];
+  __shared__ __attribute__((aligned(16))) float sides[Deep::kRows + 2 * Deep::kCols];   // scales of rows, of columns, bias
+  __shared__ Groups groups;
+  groups.init(a.offsets, a.G, a.n, Deep::kRows);
+  __syncthreads();
+  if (groups.total < 0) {
+    if (blockIdx.x == 0 && threadIdx.x == 0 && a.error) atomicOr(a.error, IM_ERR_COUNT);
+    return;
+  }
+  const int row_tiles = groups.total, total = row_tiles * a.col_tiles;
+  int tile = blockIdx.x;
+  if (tile >= total) return;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+  const uint32_t place0 = __builtin_amdgcn_readfirstlane(
+      (int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds) + (uint32_t)wave * 1024u;
+  const int steps = (a.K + Deep::kBytes - 1) / Deep::kBytes, left = a.K - (steps - 1) * Deep::kBytes;   // bytes of the last stage
+
+  // the thread's units of a stage: rows tid / 4 + 64 i, four of A and two of B
+  uint32_t off[Deep::kLoads];
+  const char *A, *B;
+  int rt, ct, g, lo, hi;
+  float side[3];
+  auto logical = [](int tid) { return (tid % 4) ^ Tile::key(tid / 4); };   // the unit that lies at the thread's place
+  auto ask = [&](int t) {   // loads of stage t
+    const uint32_t to = place0 + (uint32_t)(t % Deep::kBuffers) * Deep::kBuffer;
+    const int64_t k = (int64_t)t * Deep::kBytes;
+    uint32_t back = 0;   // units past the end of k are read from its last one, and multiplied by zero
+    if (left < Deep::kBytes && t == steps - 1) {
+      const int u = logical(fresh_thread()) * 16;
+      back = u + 16 > left ? (uint32_t)(u + 16 - left) : 0u;
+    }
+    const char *pa = uniform(A + k), *pb = uniform(B + k);
+#pragma unroll
+    for (int i = 0; i < Deep::kLoads; ++i) load_to_lds(to + i * Deep::kThreads * 16, off[i] - back, i < 4 ? pa : pb);
+  };
+  auto enter = [&](int t) {   // takes tile t: its first loads are on their way
+    const int tid = fresh_thread();
+    tile_of(t, row_tiles, a.col_tiles, rt, ct);
+    groups.find(a.offsets, a.G, a.n, Deep::kRows, rt, g, lo, hi);
+    A = static_cast<const char*>(a.A) + (int64_t)lo * a.lda;
+    B = static_cast<const char*>(a.B) + (int64_t)g * a.b_group + (int64_t)ct * Deep::kCols * a.ldb;
+    const int rows = hi - lo, cols = a.N - ct * Deep::kCols, u = logical(tid) * 16;
+#pragma unroll
+    for (int i = 0; i < Deep::kLoads; ++i) {
+      const int r = tid / 4 + (i < 4 ? i : i - 4) * 64, most = i < 4 ? rows : cols;
+      off[i] = (uint32_t)(r < most ? r : most - 1) * (uint32_t)(i < 4 ? a.lda : a.ldb) + u;
+    }
+    ask(0);
+    if (steps > 1) ask(1);
+    const int row = lo + tid < hi ? lo + tid : hi - 1;
+    const int col = ct * Deep::kCols + tid < a.N ? ct * Deep::kCols + tid : a.N - 1;
+    side[0] = scales.x[row];
+    side[1] = scales.W[(int64_t)g * a.N + col];
+    side[2] = a.bias ? a.bias[(int64_t)g * a.N + col] : 0.f;
+  };
+
+  enter(tile);
+  wait_loads<0>();
+  barrier_behind_lds();
+  if (steps > 2) ask(2);
+  while (true) {
+    i32x4 acc[S::MI][S::NJ];
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+    const int lane = fresh_thread() % 64, m0 = (wave / S::WN) * S::MI * 16, n0 = (wave % S::WN) * S::NJ * 16;
+    u32x4 x[S::MI], w[S::NJ];
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j) w[j] = Tile::frag(lds + Deep::kRowBytes, n0 + j * 16, 0, lane);
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i) x[i] = Tile::frag(lds, m0 + i * 16, 0, lane);
+    int buffer = 0;
+    for (int t = 0; t < steps; ++t) {
+      if (t > 0 && t + 1 < steps) {   // stage t + 1 is here (the first two are)
+        if (t + 2 < steps) wait_loads<Deep::kLoads>();
+        else wait_loads<0>();
+      }
+      barrier_behind_lds();
+      if (t + Deep::kBuffers < steps) ask(t + Deep::kBuffers);
+      buffer = buffer + 1 == Deep::kBuffers ? 0 : buffer + 1;
+      const char* at = lds + buffer * Deep::kBuffer;   // of no stage behind the last one: read, not used
+      if (t == steps - 1 && (lane / 16) * 16 >= left) {   // the lane's units lie past the end of k
+#pragma unroll
+        for (int j = 0; j < S::NJ; ++j) w[j] = u32x4{0, 0, 0, 0};
+      }
+      u32x4 next[S::NJ];
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) next[j] = Tile::frag(at + Deep::kRowBytes, n0 + j * 16, 0, lane);
+#pragma unroll
+      for (int i = 0; i < S::MI; ++i) {
+#pragma unroll
+        for (int j = 0; j < S::NJ; ++j) acc[i][j] = mma<int8_t>(w[j], x[i], acc[i][j]);
+        x[i] = Tile::frag(at, m0 + i * 16, 0, lane);
+        __builtin_amdgcn_sched_barrier(0);   // the read goes beside the products that follow
+      }
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) w[j] = next[j];
+    }
+    barrier_behind_lds();   // every wave is through with the buffers
+
+    const int tid = fresh_thread(), at_lo = lo, at_hi = hi, n_first = ct * Deep::kCols, g4 = (tid % 64 / 16) * 4;
+    sides[tid] = side[0];
+    if (tid < Deep::kCols) {
+      sides[Deep::kRows + tid] = side[1];
+      sides[Deep::kRows + Deep::kCols + tid] = side[2];
+    }
+    tile += gridDim.x;
+    const bool more = tile < total, full = at_hi - at_lo == Deep::kRows && n_first + Deep::kCols <= a.N;
+    if (more) enter(tile);
+    barrier_behind_lds();
+    // rows of all the tile's columns, 16 KB of them at a time
+    constexpr int kPitch = Deep::kCols * (int)sizeof(U), kUnits = kPitch / 16, kI = 32768 / (32 * kPitch) / 2;
+    static_assert(32 * kI * kPitch <= Deep::kBuffer && S::MI % kI == 0, "they fit the buffer");
+    char* const outs = lds + 2 * Deep::kBuffer;
+    char* const C = reinterpret_cast<char*>(static_cast<U*>(a.C) + (int64_t)at_lo * a.ldc + n_first);
+#pragma unroll
+    for (int i0 = 0; i0 < S::MI; i0 += kI) {
+#pragma unroll
+      for (int i = 0; i < kI; ++i) {
+        const float sx = sides[m0 + (i0 + i) * 16 + tid % 16];
+        const int r = ((wave / S::WN) * kI + i) * 16 + tid % 16;
+#pragma unroll
+        for (int j = 0; j < S::NJ; ++j) {
+          const int c = n0 + j * 16 + g4;
+          const f32x4 times = *reinterpret_cast<const f32x4*>(sides + Deep::kRows + c);
+          const f32x4 plus = *reinterpret_cast<const f32x4*>(sides + Deep::kRows + Deep::kCols + c);
+          f32x4 v;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) v[q] = finish<RELU>(acc[i0 + i][j][q], sx, times[q], plus[q]);
+          const int byte = c * (int)sizeof(U);
+          char* const to = outs + r * kPitch + (((byte / 16) ^ (r % 16)) << 4) + byte % 16;
+          if constexpr (sizeof(U) == 2) {
+            bf16x4 o;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) o[q] = (__bf16)v[q];
+            *reinterpret_cast<bf16x4*>(to) = o;
+          } else {
+            *reinterpret_cast<f32x4*>(to) = v;
+          }
+        }
+      }
+      barrier_behind_lds();
+#pragma unroll
+      for (int k = 0; k < 32 * kI * kUnits / Deep::kThreads; ++k) {
+        const int row = tid / kUnits + k * (Deep::kThreads / kUnits), u = tid % kUnits;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(outs + row * kPitch + ((u ^ (row % 16)) << 4));
+        const int m = (row / (16 * kI)) * S::MI * 16 + i0 * 16 + row % (16 * kI), c = u * kVec<U>;
+        char* const to = C + ((uint32_t)m * (uint32_t)a.ldc + (uint32_t)c) * (uint32_t)sizeof(U);
+        if (full) {
+          *reinterpret_cast<u32x4_any*>(to) = v;
+        } else {
+          const int some = a.N - n_first - c;
+          if (at_lo + m < at_hi && some > 0) {
+            if (some >= kVec<U>) *reinterpret_cast<u32x4_any*>(to) = v;
+            else store_few(reinterpret_cast<U*>(to), v, some);
+          }
+        }
+      }
+      barrier_behind_lds();   // the next rows take the LDS
+    }
+    if (!more) break;
+    if (steps > 2) ask(2);
+    // the first two stages were asked for before the stores (16 of a full tile, in fp32 32) and the third stage
+    constexpr int kStores = S::MI * 32 * kUnits / Deep::kThreads;
+    if (full && steps > 2) wait_loads<Deep::kLoads + kStores>();
+    else wait_loads<0>();
+    barrier_behind_lds();
   }
 }
 
@@ -368,10 +577,12 @@ __global__ __launch_bounds__(256) void join_packed_kernel(const RowArgs a, const
   }
   const f32x4 times = load4(scales.W + (int64_t)g * a.N + n, left);
   const f32x4 plus = a.bias ? load4(a.bias + g * a.bias_group + n, left) : f32x4{0.f, 0.f, 0.f, 0.f};
-  const float sx = scales.x[row], least = a.relu ? 0.f : -INFINITY;
+  const float sx = scales.x[row];
 #pragma unroll
   for (int r = 0; r < 4; ++r)
-    if (r < left) static_cast<U*>(a.C)[row * a.ldc + n + r] = (U)finish(sum[r], sx, times[r], plus[r], least);
+    if (r < left)
+      static_cast<U*>(a.C)[row * a.ldc + n + r] = (U)(a.relu ? finish<true>(sum[r], sx, times[r], plus[r])
+                                                             : finish<false>(sum[r], sx, times[r], plus[r]));
 }
 
 using Large = Shape<2, 4, 8, 4, 1, 128>;    // 256 x 256, 512 threads
@@ -382,7 +593,18 @@ using Small = Shape<2, 2, 2, 2, 2, 128>;    // 64 x 64
 template <typename U, class S, bool PARTIAL>
 hipError_t launch(const RowArgs& a, const PackedScales& p, hipStream_t s) {
   const int tiles = a.row_tiles * a.col_tiles * (PARTIAL ? a.splits : 1), most = a.cus * S::kBlocks;
-  hipLaunchKernelGGL((packed_kernel<U, S, PARTIAL>), dim3((unsigned)(tiles < most ? tiles : most)), dim3(S::NT), 0, s, a, p);
+  const dim3 grid((unsigned)(tiles < most ? tiles : most)), block(S::NT);
+  if (PARTIAL || !a.relu) hipLaunchKernelGGL((packed_kernel<U, S, PARTIAL, false>), grid, block, 0, s, a, p);
+  else hipLaunchKernelGGL((packed_kernel<U, S, PARTIAL, true>), grid, block, 0, s, a, p);
+  return hipGetLastError();
+}
+template <typename U>
+hipError_t launch_deep(RowArgs a, const PackedScales& p, hipStream_t s) {
+  a.col_tiles = (a.N + Deep::kCols - 1) / Deep::kCols;
+  const int tiles = a.row_tiles * a.col_tiles, most = 2 * a.cus;
+  const dim3 grid((unsigned)(tiles < most ? tiles : most)), block(Deep::kThreads);
+  if (a.relu) hipLaunchKernelGGL((packed_deep_kernel<U, true>), grid, block, 0, s, a, p);
+  else hipLaunchKernelGGL((packed_deep_kernel<U, false>), grid, block, 0, s, a, p);
   return hipGetLastError();
 }
 template <typename U>
@@ -394,6 +616,9 @@ hipError_t launch_type(const RowArgs& a, const PackedScales& p, int shape, hipSt
     hipLaunchKernelGGL(join_packed_kernel<U>, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, a, p);
     return hipGetLastError();
   }
+  const uint64_t all = reinterpret_cast<uintptr_t>(a.A) | reinterpret_cast<uintptr_t>(a.B) | (uint64_t)a.lda |
+                       (uint64_t)a.ldb | (uint64_t)a.K;
+  if (shape == 0 && all % 16 == 0) return launch_deep<U>(a, p, s);
   switch (shape) {
     case 0: return launch<U, Large, false>(a, p, s);
     case 1: return launch<U, Middle, false>(a, p, s);

@@ -174,6 +174,25 @@ def test_strides(dtype, pad):
         check_backward(c, relu_in=True, pad=pad)
 
 
+# large tiles of rows that are whole units of 16 bytes: from one stage of 64 bytes to many, ends inside one
+LARGE = [(30000, 16, 777, None), (5000, 48, 5000, None), (70000, 64, 512, [33000, 36990]), (20000, 272, 1030, [7000, 0, 12999]),
+         (40000, 528, 520, [1, 39999]), (9000, 1040, 2056, [100, 8000, 3, 800]), (30000, 320, 640, [300] * 100),
+         (4096, 4096, 2048, None)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,k,m,sizes", LARGE)
+def test_large_tiles(n, k, m, sizes, dtype):
+    note(f"[packed large] n={n} k={k} m={m} groups={sizes and len(sizes)} {dtype}")
+    c = make(n, k, m, sizes, dtype, seed=k)
+    check_forward(c, relu=True)
+    check_forward(c, relu=False, b=False, pad=3)
+    wide = make(n, k, m, sizes, dtype, seed=k, pad=32)   # rows of 16-byte units within wider ones
+    wide["q"] = c["q"].new_empty(n, k + 32)[:, :k].copy_(c["q"])
+    wide["s"] = c["s"]
+    check_forward(wide, relu=True)
+
+
 @pytest.mark.parametrize("some", [("dx",), ("dW",), ("db",), ("dW", "db")])
 def test_some_gradients(some):
     note(f"[packed: some gradients] {some}")
