@@ -619,6 +619,7 @@ __global__ __launch_bounds__(256) void router_kernel(const RouterArgs a, int sco
 // C choices a lane.
 template <typename T, int L, int V, int C>
 __global__ __launch_bounds__(256) void router_backward_kernel(const RouterArgs a, int score) {
+  __shared__ __attribute__((aligned(16))) float lds[4][64 * V];
   const int l = (int)threadIdx.x % L;
   constexpr int kRows = 256 / L;
   for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.n; first += (int64_t)gridDim.x * kRows) {
@@ -687,18 +688,47 @@ __global__ __launch_bounds__(256) void router_backward_kernel(const RouterArgs a
     const float each = dense ? -dot / total : 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) q[v] *= each;
-    for (int c = 0; c < a.k; ++c) {
-      int ec = e[0];
-      float dc = d[0];
+    // The choices' parts are added in LDS: a row's listed experts are as a rule no two the same, which
+    // each place's last writer tells. Where they are, they are added in their order, one by one.
+    float* const mine = lds[threadIdx.x / 64] + ((int)threadIdx.x % 64) / L * (L * V);
+    lds_order();
 #pragma unroll
-      for (int t = 1; t < C; ++t) {
-        ec = c / L == t ? e[t] : ec;
-        dc = c / L == t ? d[t] : dc;
+    for (int t = 0; t < C; ++t)
+      if (e[t] >= 0) mine[e[t]] = __builtin_bit_cast(float, t * L + l);
+    lds_order();
+    bool twice = false;
+#pragma unroll
+    for (int t = 0; t < C; ++t) twice |= e[t] >= 0 && __builtin_bit_cast(int, mine[e[t]]) != t * L + l;
+    lds_order();
+    if (ballot(twice) != 0) {
+      for (int c = 0; c < a.k; ++c) {
+        int ec = e[0];
+        float dc = d[0];
+#pragma unroll
+        for (int t = 1; t < C; ++t) {
+          ec = c / L == t ? e[t] : ec;
+          dc = c / L == t ? d[t] : dc;
+        }
+        const int i = __shfl(ec, c % L, L);
+        const float x = __shfl(dc, c % L, L);
+#pragma unroll
+        for (int v = 0; v < V; ++v) q[v] += i - 4 * l == place<L>(v) ? x : 0.f;
       }
-      const int i = __shfl(ec, c % L, L);
-      const float x = __shfl(dc, c % L, L);
+    } else {
 #pragma unroll
-      for (int v = 0; v < V; ++v) q[v] += i - 4 * l == place<L>(v) ? x : 0.f;
+      for (int v = 0; v < V; v += 4)
+        *reinterpret_cast<f32x4*>(mine + place<L>(v) + 4 * l) = f32x4{q[v], q[v + 1], q[v + 2], q[v + 3]};
+      lds_order();
+#pragma unroll
+      for (int t = 0; t < C; ++t)
+        if (e[t] >= 0) mine[e[t]] += d[t];
+      lds_order();
+#pragma unroll
+      for (int v = 0; v < V; v += 4) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(mine + place<L>(v) + 4 * l);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[v + i] = x[i];
+      }
     }
     if (!in) continue;
     T* const to = static_cast<T*>(a.dz) + row * a.ld_dz;

@@ -142,11 +142,31 @@ class _On:
             torch.cuda.set_device(self.was)
 
 
+_device = None   # torch's accessor of the current device's number
+
+
+def _run(index, call, *args):
+    """A call of the library on device `index`, with torch's current stream of it where the last
+    argument is None."""
+    global _device
+    if _device is None:
+        import torch
+        torch.cuda.init()
+        _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    if _device() == index:
+        status = call(*args[:-1], _stream(args[-1]))
+    else:
+        with _On(index):
+            status = call(*args[:-1], _stream(args[-1]))
+    if status != IM_OK:
+        raise IMError(status, im_learn_last_error())
+
+
 def _matrix(t, name, dtype, device, rows, cols):
     """Row stride of a [rows, cols] tensor whose columns are contiguous."""
     if t.dtype is not dtype or t.device != device:
         _bad(f"{name} is {t.dtype} on {t.device}, {dtype} on {device} expected")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if t.shape != (rows, cols):
         _bad(f"{name} has shape {tuple(t.shape)}, ({rows}, {cols}) expected")
     ld, inner = t.stride()
     if inner != 1 and cols > 1:
@@ -215,7 +235,8 @@ def _workspace(query, desc, key, backward, workspace, device, stream):
     need = _SIZES.get(key)
     if need is None:
         out = _I64(0)
-        _done(query(ctypes.byref(desc), backward, ctypes.byref(out)))
+        with _On(device.index):
+            _done(query(ctypes.byref(desc), backward, ctypes.byref(out)))
         if len(_SIZES) >= 4096:
             _SIZES.clear()
         need = _SIZES[key] = out.value
@@ -406,10 +427,9 @@ def im_router_forward(z, expert, weight, bias=None, valid=None, score="softmax",
     L = _learn or load_learn()
     d = ImRouterDesc(n, E, k, n_sets, n_sets if top_sets is None else top_sets, set_best, kind, _score(score),
                      1 if renorm else 0, scale, ld, 0)
-    with _On(dev.index):
-        _done(L.im_router_forward(ctypes.byref(d), z.data_ptr(), _flat(bias, "bias", f32, dev, E),
-                                  _mask(valid, n, E, dev), _flat(expert, "expert", i32, dev, n * k),
-                                  _flat(weight, "weight", f32, dev, n * k), _stream(stream)))
+    _run(dev.index, L.im_router_forward, ctypes.byref(d), z.data_ptr(), _flat(bias, "bias", f32, dev, E),
+         _mask(valid, n, E, dev), _flat(expert, "expert", i32, dev, n * k),
+         _flat(weight, "weight", f32, dev, n * k), stream)
 
 
 def im_router_backward(z, expert, dweight, dz, valid=None, score="softmax", renorm=True, scale=1.0, error=None,
@@ -423,17 +443,19 @@ def im_router_backward(z, expert, dweight, dz, valid=None, score="softmax", reno
     f32, i32 = _KINDS["f32"], _KINDS["i32"]
     L = _learn or load_learn()
     d = ImRouterDesc(n, E, k, 1, 1, 1, kind, _score(score), 1 if renorm else 0, scale, ld, ld_dz)
-    with _On(dev.index):
-        _done(L.im_router_backward(ctypes.byref(d), z.data_ptr(), _mask(valid, n, E, dev),
-                                   _flat(expert, "expert", i32, dev, n * k), _flat(dweight, "dweight", f32, dev, n * k),
-                                   dz.data_ptr(), _flat(error, "error", i32, dev, 1), _stream(stream)))
+    _run(dev.index, L.im_router_backward, ctypes.byref(d), z.data_ptr(), _mask(valid, n, E, dev),
+         _flat(expert, "expert", i32, dev, n * k), _flat(dweight, "dweight", f32, dev, n * k),
+         dz.data_ptr(), _flat(error, "error", i32, dev, 1), stream)
+
+
+def _dispatch_size(desc, backward, out):
+    return (_learn or load_learn()).im_dispatch_workspace(desc, out)
 
 
 def im_dispatch_workspace(n_rows, top_k, n_experts, device=None):
     """Bytes of workspace of im_dispatch_plan; as im_linear_workspace."""
-    L = _learn or load_learn()
     d = ImDispatchDesc(n_rows, top_k, n_experts, 0, 1, 0, 1, 1, 1)
-    return _size_of(lambda desc, backward, out: L.im_dispatch_workspace(desc, out), d, False, device)
+    return _size_of(_dispatch_size, d, False, device)
 
 
 def im_dispatch_plan(expert, offsets, slot, workspace=None, error=None, stream=None):
@@ -448,12 +470,11 @@ def im_dispatch_plan(expert, offsets, slot, workspace=None, error=None, stream=N
     E = offsets.numel() - 1
     L = _learn or load_learn()
     d = ImDispatchDesc(n, k, E, 0, 1, 0, 1, 1, 1)
-    with _On(dev.index):
-        ws, at, size = _workspace(lambda desc, backward, out: L.im_dispatch_workspace(desc, out), d,
+    ws, at, size = _workspace(lambda desc, backward, out: L.im_dispatch_workspace(desc, out), d,
                                   (4, dev.index, n, k, E), 0, workspace, dev, stream)
-        _done(L.im_dispatch_plan(ctypes.byref(d), _flat(expert, "expert", i32, dev, n * k),
-                                 _flat(offsets, "offsets", i32, dev, E + 1), _flat(slot, "slot", i32, dev, n * k), at,
-                                 size, _flat(error, "error", i32, dev, 1), _stream(stream)))
+    _run(dev.index, L.im_dispatch_plan, ctypes.byref(d), _flat(expert, "expert", i32, dev, n * k),
+         _flat(offsets, "offsets", i32, dev, E + 1), _flat(slot, "slot", i32, dev, n * k), at,
+         size, _flat(error, "error", i32, dev, 1), stream)
 
 
 def _exchange(rows, rows_name, slots, slots_name, slot, dslots=None, codes=False):
@@ -482,26 +503,22 @@ def im_dispatch_forward(x, slot, xs, error=None, stream=None):
     """xs[slot[i, c]] = x[i]: rows to their places (float32, bfloat16, or the int8 codes of
     packed rows; rows of xs that no slot names stay as they are). Rows may be strided."""
     d, dev, ps = _exchange(x, "x", xs, "xs", slot, codes=True)
-    with _On(dev.index):
-        _done((_learn or load_learn()).im_dispatch_forward(ctypes.byref(d), x.data_ptr(), ps, xs.data_ptr(),
-                                                           _flat(error, "error", _KINDS["i32"], dev, 1), _stream(stream)))
+    _run(dev.index, (_learn or load_learn()).im_dispatch_forward, ctypes.byref(d), x.data_ptr(), ps, xs.data_ptr(),
+         _flat(error, "error", _KINDS["i32"], dev, 1), stream)
 
 
 def im_dispatch_backward(dxs, slot, dx, error=None, stream=None):
     """dx[i] = sum of dxs[slot[i, c]] over c."""
     d, dev, ps = _exchange(dx, "dx", dxs, "dxs", slot)
-    with _On(dev.index):
-        _done((_learn or load_learn()).im_dispatch_backward(ctypes.byref(d), dxs.data_ptr(), ps, dx.data_ptr(),
-                                                            _flat(error, "error", _KINDS["i32"], dev, 1), _stream(stream)))
+    _run(dev.index, (_learn or load_learn()).im_dispatch_backward, ctypes.byref(d), dxs.data_ptr(), ps, dx.data_ptr(),
+         _flat(error, "error", _KINDS["i32"], dev, 1), stream)
 
 
 def im_combine_forward(ys, slot, weight, y, error=None, stream=None):
     """y[i] = sum of weight[i, c] ys[slot[i, c]] over c (weight float32 like slot)."""
     d, dev, ps = _exchange(y, "y", ys, "ys", slot)
-    with _On(dev.index):
-        _done((_learn or load_learn()).im_combine_forward(
-            ctypes.byref(d), ys.data_ptr(), ps, _flat(weight, "weight", _KINDS["f32"], dev, slot.numel()), y.data_ptr(),
-            _flat(error, "error", _KINDS["i32"], dev, 1), _stream(stream)))
+    _run(dev.index, (_learn or load_learn()).im_combine_forward, ctypes.byref(d), ys.data_ptr(), ps, _flat(weight, "weight", _KINDS["f32"], dev, slot.numel()), y.data_ptr(),
+         _flat(error, "error", _KINDS["i32"], dev, 1), stream)
 
 
 def im_combine_backward(dy, ys, slot, weight, dys=None, dweight=None, error=None, stream=None):
@@ -509,12 +526,9 @@ def im_combine_backward(dy, ys, slot, weight, dys=None, dweight=None, error=None
     (float32 like slot); None skips one."""
     d, dev, ps = _exchange(dy, "dy", ys, "ys", slot, dys)
     f32 = _KINDS["f32"]
-    with _On(dev.index):
-        _done((_learn or load_learn()).im_combine_backward(
-            ctypes.byref(d), dy.data_ptr(), None if ys is None else ys.data_ptr(), ps,
-            _flat(weight, "weight", f32, dev, slot.numel()), None if dys is None else dys.data_ptr(),
-            _flat(dweight, "dweight", f32, dev, slot.numel()), _flat(error, "error", _KINDS["i32"], dev, 1),
-            _stream(stream)))
+    _run(dev.index, (_learn or load_learn()).im_combine_backward, ctypes.byref(d), dy.data_ptr(), None if ys is None else ys.data_ptr(), ps,
+         _flat(weight, "weight", f32, dev, slot.numel()), None if dys is None else dys.data_ptr(),
+         _flat(dweight, "dweight", f32, dev, slot.numel()), _flat(error, "error", _KINDS["i32"], dev, 1), stream)
 
 
 def _rows(x, codes, scale, keep):
@@ -530,15 +544,13 @@ def im_rows_pack(x, codes, scale, keep=False, stream=None):
     bfloat16), x = scale code up to half a scale. keep: what is not zero gets a code
     that is not. Rows of x and codes may be strided."""
     d, dev, ps = _rows(x, codes, scale, keep)
-    with _On(dev.index):
-        _done((_learn or load_learn()).im_rows_pack(ctypes.byref(d), x.data_ptr(), codes.data_ptr(), ps, _stream(stream)))
+    _run(dev.index, (_learn or load_learn()).im_rows_pack, ctypes.byref(d), x.data_ptr(), codes.data_ptr(), ps, stream)
 
 
 def im_rows_unpack(codes, scale, x, stream=None):
     """x = scale code in float32, rounded to its type."""
     d, dev, ps = _rows(x, codes, scale, False)
-    with _On(dev.index):
-        _done((_learn or load_learn()).im_rows_unpack(ctypes.byref(d), codes.data_ptr(), ps, x.data_ptr(), _stream(stream)))
+    _run(dev.index, (_learn or load_learn()).im_rows_unpack, ctypes.byref(d), codes.data_ptr(), ps, x.data_ptr(), stream)
 
 
 def im_linear_workspace_packed(n_rows, in_dim, out_dim, dtype, n_groups=1, backward=False, device=None):
@@ -560,12 +572,11 @@ def im_linear_forward_packed(x, x_scale, W, W_scale, b, y, offsets=None, relu=Fa
     ld_y = _matrix(y, "y", dt, dev, n, m)
     L = _learn or load_learn()
     d = ImLinearDesc(G, n, k, m, kind, 1 if relu else 0, 0, 0, ld_x, ld_y, 0)
-    with _On(dev.index):
-        ws, at, size = _workspace(L.im_linear_workspace_packed, d, (5, dev.index, G, n, k, m, kind), 0, workspace, dev, stream)
-        _done(L.im_linear_forward_packed(ctypes.byref(d), _offsets(offsets, G, dev), x.data_ptr(),
-                                         _flat(x_scale, "x_scale", f32, dev, n), W.data_ptr(),
-                                         _flat(W_scale, "W_scale", f32, dev, G * m), _flat(b, "b", f32, dev, G * m),
-                                         y.data_ptr(), at, size, _flat(error, "error", i32, dev, 1), _stream(stream)))
+    ws, at, size = _workspace(L.im_linear_workspace_packed, d, (5, dev.index, G, n, k, m, kind), 0, workspace, dev, stream)
+    _run(dev.index, L.im_linear_forward_packed, ctypes.byref(d), _offsets(offsets, G, dev), x.data_ptr(),
+         _flat(x_scale, "x_scale", f32, dev, n), W.data_ptr(),
+         _flat(W_scale, "W_scale", f32, dev, G * m), _flat(b, "b", f32, dev, G * m),
+         y.data_ptr(), at, size, _flat(error, "error", i32, dev, 1), stream)
 
 
 def im_linear_backward_packed(dy, x, x_scale, W, dx=None, dW=None, db=None, offsets=None, relu_in=False,
@@ -584,13 +595,12 @@ def im_linear_backward_packed(dy, x, x_scale, W, dx=None, dW=None, db=None, offs
     ld_dx = k if dx is None else _matrix(dx, "dx", dt, dev, n, k)
     L = _learn or load_learn()
     d = ImLinearDesc(G, n, k, m, kind, 0, 1 if relu_in else 0, 0, ld_x, ld_y, ld_dx)
-    with _On(dev.index):
-        ws, at, size = _workspace(L.im_linear_workspace_packed, d, (6, dev.index, G, n, k, m, kind), 1, workspace, dev, stream)
-        _done(L.im_linear_backward_packed(ctypes.byref(d), _offsets(offsets, G, dev), dy.data_ptr(), x.data_ptr(),
-                                          _flat(x_scale, "x_scale", f32, dev, n), W.data_ptr(),
-                                          None if dx is None else dx.data_ptr(), _flat(dW, "dW", dt, dev, G * m * k),
-                                          _flat(db, "db", f32, dev, G * m), at, size,
-                                          _flat(error, "error", i32, dev, 1), _stream(stream)))
+    ws, at, size = _workspace(L.im_linear_workspace_packed, d, (6, dev.index, G, n, k, m, kind), 1, workspace, dev, stream)
+    _run(dev.index, L.im_linear_backward_packed, ctypes.byref(d), _offsets(offsets, G, dev), dy.data_ptr(), x.data_ptr(),
+         _flat(x_scale, "x_scale", f32, dev, n), W.data_ptr(),
+         None if dx is None else dx.data_ptr(), _flat(dW, "dW", dt, dev, G * m * k),
+         _flat(db, "db", f32, dev, G * m), at, size,
+         _flat(error, "error", i32, dev, 1), stream)
 
 
 # Plans whose AdamW was dropped. To free one synchronises the device, which would spoil a graph
