@@ -121,7 +121,7 @@ __device__ __forceinline__ double shfl_xor_f64(double v, int m) {
 // of the wave, 64 V doubles. Lane l gets the row's l-th chosen expert, or -1.
 template <typename T, int V>
 __device__ __forceinline__ int choose_exact(const RouterArgs& a, int score, int64_t row, double* keys) {
-  const int lane = (int)threadIdx.x % 64;
+  const int lane = fresh_thread() % 64;   // nothing of this is worked out ahead, in registers of the rows that need none
   float z[V];
   double key[V], share[V];
   float top = -INFINITY;
@@ -241,7 +241,7 @@ __device__ __forceinline__ int choose_exact(const RouterArgs& a, int score, int6
 // A row by a whole wave: choice in 64 bits, weights, stores.
 template <typename T, int V>
 __device__ __forceinline__ void route_exact(const RouterArgs& a, int score, int64_t row, double* keys) {
-  const int lane = (int)threadIdx.x % 64;
+  const int lane = fresh_thread() % 64;
   const int mine = choose_exact<T, V>(a, score, row, keys);
   float z[1] = {mine >= 0 ? logit<T>(a, row, mine) : -INFINITY}, w[1], top = 0.f, total = 1.f;
   if (score == IM_SOFTMAX && !a.renorm) {
@@ -361,16 +361,17 @@ __global__ __launch_bounds__(256) void router_kernel(const RouterArgs a, int sco
   constexpr int kPitch = L * V + 4;   // floats of a row
   constexpr int kLds = kRows * kPitch * 4 > kWide * 512 ? kRows * kPitch * 4 : kWide * 512;
   __shared__ __attribute__((aligned(16))) char lds[4][kLds];
-  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, l = lane % L, r = lane / L;
-  float* const mine = reinterpret_cast<float*>(lds[wave]) + r * kPitch;   // the row's LDS
+  const int wave = threadIdx.x / 64, l0 = threadIdx.x % L;
   const int each = a.E / a.sets;
   const bool pairs = a.best == 2;
   float bias[SCORES ? V : 1];
   if constexpr (SCORES) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) bias[v] = a.bias && place<L>(v) + 4 * l < a.E ? a.bias[place<L>(v) + 4 * l] : 0.f;
+    for (int v = 0; v < V; ++v) bias[v] = a.bias && place<L>(v) + 4 * l0 < a.E ? a.bias[place<L>(v) + 4 * l0] : 0.f;
   }
   for (int64_t first = ((int64_t)blockIdx.x * 4 + wave) * kRows; first < a.n; first += (int64_t)gridDim.x * 4 * kRows) {
+    const int lane = fresh_thread() % 64, l = lane % L, r = lane / L;
+    float* const mine = reinterpret_cast<float*>(lds[wave]) + r * kPitch;   // the row's LDS
     const bool in = first + r < a.n;   // the last wave's other lanes follow the last row, and store nothing
     const int64_t row = in ? first + r : a.n - 1;
     float key[V];
@@ -416,9 +417,20 @@ __global__ __launch_bounds__(256) void router_kernel(const RouterArgs a, int sco
         near = most * 0x1p-17f;
       } else {
         most = __builtin_amdgcn_rcpf(1.f + exp_(-top));
+        float least = key[0];
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-          key[v] = key[v] > -INFINITY ? __builtin_amdgcn_rcpf(1.f + exp_(-key[v])) : -INFINITY;
+        for (int v = 1; v < V; ++v) least = fminf(least, key[v]);
+        uint32_t out = 0;   // experts that are not valid, where there are any
+        if (ballot(least == -INFINITY) != 0) {
+#pragma unroll
+          for (int v = 0; v < V; ++v) out |= key[v] == -INFINITY ? 1u << v : 0u;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) key[v] = __builtin_amdgcn_rcpf(1.f + exp_(-key[v]));
+        if (ballot(out != 0) != 0) {
+#pragma unroll
+          for (int v = 0; v < V; ++v) key[v] = (out >> v) & 1u ? -INFINITY : key[v];
+        }
         // the exponential is off by (1.25 |z| + 2) 2^-24 of itself, which counts by the score times
         // (1 - score); the sum and the reciprocal add 3 2^-24 of the score; both for two scores
         near = most * (0x1p-20f + 0x1p-21f * fmaxf(-top, 0.f));
