@@ -1,9 +1,10 @@
 // Rows in 8 bits: packing, unpacking, and the product of packed rows with packed weights.
 //
-// Pack and unpack are one pass over memory. The product goes as that of bf16 rows does
-// (tiles, stages of 128 bytes, blocks that keep taking tiles), on v_mfma_i32_16x16x64_i8: twice the
-// operations a byte of LDS, and an exact sum (127^2 65536 is below 2^31), which the
-// scales of its row and column multiply once.
+// Pack and unpack are one pass over memory: 262144 rows of 512, bf16, 82 us (4.9 TB/s).
+// The product goes as that of bf16 rows does (tiles, stages of 128 bytes, blocks that keep taking tiles), on
+// v_mfma_i32_16x16x64_i8: twice the operations a byte of LDS, and an exact sum (127^2 65536 is below
+// 2^31), which the scales of its row and column multiply once. Large tiles of aligned rows have a kernel
+// of their own, below.
 #include "learn_internal.h"
 #include "learn_tile.h"
 #include "wave.h"
@@ -346,18 +347,23 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void packed_kernel(const RowArgs 
 
 // The same product for large tiles of rows that are whole 16-byte units at 16-byte addresses: the
 // operands go from memory to LDS without registers (global_load_lds_dwordx4), which leaves room for the
-// fragments of a stage while the next one's are read. Three buffers of 64 bytes of k: stage t is multiplied
-// from registers, t + 1 is read from LDS, t + 2 is on its way, and t + 3 is asked for once every wave has
-// t in registers (one barrier a stage). Two blocks of 256 x 128 share a CU, so that one's products run
-// beside the other's results and first loads; a block's results leave through the third buffer while the first
-// two take the next tile's stages.
+// fragments of a stage while the next one's are read. A stage is 64 bytes of k. With B buffers stage t is multiplied
+// from registers, t + 1 is read from LDS, those up to t + B - 1 are on their way, and t + B is asked for once every
+// wave has t in registers (one barrier a stage). A block's results leave through the last buffer
+// while the others take the next tile's first stages.
+// What bounds it: LDS (12 fragments read for 32 products, and the operands' writes), which the products
+// overlap but for each stage's barrier, and at k of some stages the tile's own start and results. 8192 x 8192 x 8192
+// 605 us, 1.82 POP/s (a library product of that size 2.2); 262144 x 512 x 512 of 64 groups 151 us (75 at the rate of
+// a copy). Taking rows of products from LDS ahead of the barrier and a wave's priority over its products changed nothing.
 //
 // The loads are written in assembly, and so are the waits for them: the compiler would have every read of
 // LDS wait for all of them. They write no register, and a wave's loads and stores end in their order.
+template <int WN, int BUFFERS>
 struct Deep {
-  static constexpr int kThreads = 256, kRows = 256, kCols = 128, kBytes = 64, kBuffers = 3;
+  static constexpr int kThreads = 128 * WN, kRows = 256, kCols = 64 * WN, kBytes = 64, kBuffers = BUFFERS;
   static constexpr int kRowBytes = kRows * kBytes, kBuffer = kRowBytes + kCols * kBytes;
-  static constexpr int kLoads = kBuffer / 16 / kThreads;   // of a thread, a stage
+  static constexpr int kLoads = kBuffer / 16 / kThreads, kRowLoads = kRowBytes / 16 / kThreads;   // of a thread, a stage
+  static constexpr int kWN = WN, kBlocks = WN == 2 ? 2 : 1;   // a CU
 };
 
 __device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, const char* base) {
@@ -376,9 +382,9 @@ __device__ __forceinline__ const char* uniform(const char* p) {
                                        (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v));
 }
 
-template <typename U, bool RELU>
+template <typename U, class Deep, bool RELU>
 __global__ __launch_bounds__(Deep::kThreads, 2) void packed_deep_kernel(const RowArgs a, const PackedScales scales) {
-  using S = Shape<2, 2, 8, 4, 1, Deep::kBytes>;
+  using S = Shape<2, Deep::kWN, 8, 4, 1, Deep::kBytes>;
   using Tile = RowTile<int8_t, Deep::kRows, Deep::kThreads, 1, Deep::kBytes>;
   static_assert(S::BM == Deep::kRows && S::BN == Deep::kCols && S::NT == Deep::kThreads, "the tile's");
   __shared__ __attribute__((aligned(1024))) char lds[Deep::kBuffers * Deep::kBuffer];
@@ -398,7 +404,7 @@ __global__ __launch_bounds__(Deep::kThreads, 2) void packed_deep_kernel(const Ro
       (int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds) + (uint32_t)wave * 1024u;
   const int steps = (a.K + Deep::kBytes - 1) / Deep::kBytes, left = a.K - (steps - 1) * Deep::kBytes;   // bytes of the last stage
 
-  // the thread's units of a stage: rows tid / 4 + 64 i, four of A and two of B
+  // the thread's units of a stage: rows tid / 4 + kThreads / 4 i, the first of A, then of B
   uint32_t off[Deep::kLoads];
   const char *A, *B;
   int rt, ct, g, lo, hi;
@@ -414,7 +420,7 @@ __global__ __launch_bounds__(Deep::kThreads, 2) void packed_deep_kernel(const Ro
     }
     const char *pa = uniform(A + k), *pb = uniform(B + k);
 #pragma unroll
-    for (int i = 0; i < Deep::kLoads; ++i) load_to_lds(to + i * Deep::kThreads * 16, off[i] - back, i < 4 ? pa : pb);
+    for (int i = 0; i < Deep::kLoads; ++i) load_to_lds(to + i * Deep::kThreads * 16, off[i] - back, i < Deep::kRowLoads ? pa : pb);
   };
   auto enter = [&](int t) {   // takes tile t: its first loads are on their way
     const int tid = fresh_thread();
@@ -425,11 +431,13 @@ __global__ __launch_bounds__(Deep::kThreads, 2) void packed_deep_kernel(const Ro
     const int rows = hi - lo, cols = a.N - ct * Deep::kCols, u = logical(tid) * 16;
 #pragma unroll
     for (int i = 0; i < Deep::kLoads; ++i) {
-      const int r = tid / 4 + (i < 4 ? i : i - 4) * 64, most = i < 4 ? rows : cols;
-      off[i] = (uint32_t)(r < most ? r : most - 1) * (uint32_t)(i < 4 ? a.lda : a.ldb) + u;
+      const bool of_a = i < Deep::kRowLoads;
+      const int r = tid / 4 + (of_a ? i : i - Deep::kRowLoads) * (Deep::kThreads / 4), most = of_a ? rows : cols;
+      off[i] = (uint32_t)(r < most ? r : most - 1) * (uint32_t)(of_a ? a.lda : a.ldb) + u;
     }
-    ask(0);
-    if (steps > 1) ask(1);
+#pragma unroll
+    for (int t0 = 0; t0 + 1 < Deep::kBuffers; ++t0)
+      if (t0 < steps) ask(t0);
     const int row = lo + tid < hi ? lo + tid : hi - 1;
     const int col = ct * Deep::kCols + tid < a.N ? ct * Deep::kCols + tid : a.N - 1;
     side[0] = scales.x[row];
@@ -440,7 +448,7 @@ __global__ __launch_bounds__(Deep::kThreads, 2) void packed_deep_kernel(const Ro
   enter(tile);
   wait_loads<0>();
   barrier_behind_lds();
-  if (steps > 2) ask(2);
+  if (steps >= Deep::kBuffers) ask(Deep::kBuffers - 1);
   while (true) {
     i32x4 acc[S::MI][S::NJ];
 #pragma unroll
@@ -455,8 +463,9 @@ __global__ __launch_bounds__(Deep::kThreads, 2) void packed_deep_kernel(const Ro
     for (int i = 0; i < S::MI; ++i) x[i] = Tile::frag(lds, m0 + i * 16, 0, lane);
     int buffer = 0;
     for (int t = 0; t < steps; ++t) {
-      if (t > 0 && t + 1 < steps) {   // stage t + 1 is here (the first two are)
-        if (t + 2 < steps) wait_loads<Deep::kLoads>();
+      if (t + 2 >= Deep::kBuffers && t + 1 < steps) {   // stage t + 1 is here (those before the last buffer's are)
+        if (t + Deep::kBuffers - 1 < steps) wait_loads<(Deep::kBuffers - 2) * Deep::kLoads>();
+        else if (Deep::kBuffers > 3 && t + 2 < steps) wait_loads<Deep::kLoads>();
         else wait_loads<0>();
       }
       barrier_behind_lds();
@@ -483,7 +492,7 @@ __global__ __launch_bounds__(Deep::kThreads, 2) void packed_deep_kernel(const Ro
     barrier_behind_lds();   // every wave is through with the buffers
 
     const int tid = fresh_thread(), at_lo = lo, at_hi = hi, n_first = ct * Deep::kCols, g4 = (tid % 64 / 16) * 4;
-    sides[tid] = side[0];
+    if (tid < Deep::kRows) sides[tid] = side[0];
     if (tid < Deep::kCols) {
       sides[Deep::kRows + tid] = side[1];
       sides[Deep::kRows + Deep::kCols + tid] = side[2];
@@ -493,9 +502,9 @@ __global__ __launch_bounds__(Deep::kThreads, 2) void packed_deep_kernel(const Ro
     if (more) enter(tile);
     barrier_behind_lds();
     // rows of all the tile's columns, 16 KB of them at a time
-    constexpr int kPitch = Deep::kCols * (int)sizeof(U), kUnits = kPitch / 16, kI = 32768 / (32 * kPitch) / 2;
+    constexpr int kPitch = Deep::kCols * (int)sizeof(U), kUnits = kPitch / 16, kI = 16384 / (32 * kPitch) > 0 ? 16384 / (32 * kPitch) : 1;
     static_assert(32 * kI * kPitch <= Deep::kBuffer && S::MI % kI == 0, "they fit the buffer");
-    char* const outs = lds + 2 * Deep::kBuffer;
+    char* const outs = lds + (Deep::kBuffers - 1) * Deep::kBuffer;
     char* const C = reinterpret_cast<char*>(static_cast<U*>(a.C) + (int64_t)at_lo * a.ldc + n_first);
 #pragma unroll
     for (int i0 = 0; i0 < S::MI; i0 += kI) {
@@ -543,10 +552,10 @@ __global__ __launch_bounds__(Deep::kThreads, 2) void packed_deep_kernel(const Ro
       barrier_behind_lds();   // the next rows take the LDS
     }
     if (!more) break;
-    if (steps > 2) ask(2);
-    // the first two stages were asked for before the stores (16 of a full tile, in fp32 32) and the third stage
+    if (steps >= Deep::kBuffers) ask(Deep::kBuffers - 1);
+    // the other stages were asked for before the stores (16 of a full tile, in fp32 32) and this one
     constexpr int kStores = S::MI * 32 * kUnits / Deep::kThreads;
-    if (full && steps > 2) wait_loads<Deep::kLoads + kStores>();
+    if (full && steps >= Deep::kBuffers) wait_loads<Deep::kLoads + kStores>();
     else wait_loads<0>();
     barrier_behind_lds();
   }
@@ -598,13 +607,13 @@ hipError_t launch(const RowArgs& a, const PackedScales& p, hipStream_t s) {
   else hipLaunchKernelGGL((packed_kernel<U, S, PARTIAL, true>), grid, block, 0, s, a, p);
   return hipGetLastError();
 }
-template <typename U>
+template <typename U, class Deep>
 hipError_t launch_deep(RowArgs a, const PackedScales& p, hipStream_t s) {
   a.col_tiles = (a.N + Deep::kCols - 1) / Deep::kCols;
-  const int tiles = a.row_tiles * a.col_tiles, most = 2 * a.cus;
+  const int tiles = a.row_tiles * a.col_tiles, most = Deep::kBlocks * a.cus;
   const dim3 grid((unsigned)(tiles < most ? tiles : most)), block(Deep::kThreads);
-  if (a.relu) hipLaunchKernelGGL((packed_deep_kernel<U, true>), grid, block, 0, s, a, p);
-  else hipLaunchKernelGGL((packed_deep_kernel<U, false>), grid, block, 0, s, a, p);
+  if (a.relu) hipLaunchKernelGGL((packed_deep_kernel<U, Deep, true>), grid, block, 0, s, a, p);
+  else hipLaunchKernelGGL((packed_deep_kernel<U, Deep, false>), grid, block, 0, s, a, p);
   return hipGetLastError();
 }
 template <typename U>
@@ -618,7 +627,11 @@ hipError_t launch_type(const RowArgs& a, const PackedScales& p, int shape, hipSt
   }
   const uint64_t all = reinterpret_cast<uintptr_t>(a.A) | reinterpret_cast<uintptr_t>(a.B) | (uint64_t)a.lda |
                        (uint64_t)a.ldb | (uint64_t)a.K;
-  if (shape == 0 && all % 16 == 0) return launch_deep<U>(a, p, s);
+  // One block a CU of 256 x 256 and four buffers for long sums, two of 256 x 128 and three buffers, whose results and
+  // products overlap, for others. Both sides, us with two blocks / one: 8192 x 8192 x 8192 691 / 605, 8192 x 4096 x
+  // 4096 153 / 140; k 2048 with ragged experts 168 / 184, 512 with 64 groups 151 / 167.
+  if (shape == 0 && all % 16 == 0)
+    return a.K >= 4096 ? launch_deep<U, Deep<4, 4>>(a, p, s) : launch_deep<U, Deep<2, 3>>(a, p, s);
   switch (shape) {
     case 0: return launch<U, Large, false>(a, p, s);
     case 1: return launch<U, Middle, false>(a, p, s);
@@ -670,7 +683,7 @@ hipError_t launch_unpack(const PackArgs& a, int dtype, hipStream_t s) {
   return dtype == IM_BF16 ? unpack<__bf16>(a, s) : unpack<float>(a, s);
 }
 
-// A stage holds twice the k of a bf16 one and takes as long.
+// A stage holds twice the k of a bf16 one and takes as long: the shapes are chosen as there.
 RowPlan plan_packed(int64_t n, int64_t G, int64_t N, int64_t K, int cus) {
   RowPlan p = plan_rows(IM_BF16, n, G, N, (K + 1) / 2, cus, true);
   p.split_k *= 2;
