@@ -177,7 +177,7 @@ def test_strides(dtype, pad):
 # large tiles of rows that are whole units of 16 bytes: from one stage of 64 bytes to many, ends inside one
 LARGE = [(30000, 16, 777, None), (5000, 48, 5000, None), (70000, 64, 512, [33000, 36990]), (20000, 272, 1030, [7000, 0, 12999]),
          (40000, 528, 520, [1, 39999]), (9000, 1040, 2056, [100, 8000, 3, 800]), (30000, 320, 640, [300] * 100),
-         (4096, 4096, 2048, None)]
+         (4096, 4096, 2048, None), (8192, 4096, 4096, None), (9000, 4112, 2050, [100, 8000, 899]), (5000, 4224, 4096, [0, 5000])]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
