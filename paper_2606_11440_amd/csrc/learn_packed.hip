@@ -358,16 +358,19 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void packed_kernel(const RowArgs 
 //
 // The loads are written in assembly, and so are the waits for them: the compiler would have every read of
 // LDS wait for all of them. They write no register, and a wave's loads and stores end in their order.
-template <int WN, int BUFFERS>
+template <int WN, int BUFFERS, int BLOCKS>
 struct Deep {
   static constexpr int kThreads = 128 * WN, kRows = 256, kCols = 64 * WN, kBytes = 64, kBuffers = BUFFERS;
   static constexpr int kRowBytes = kRows * kBytes, kBuffer = kRowBytes + kCols * kBytes;
   static constexpr int kLoads = kBuffer / 16 / kThreads, kRowLoads = kRowBytes / 16 / kThreads;   // of a thread, a stage
-  static constexpr int kWN = WN, kBlocks = WN == 2 ? 2 : 1;   // a CU
+  static constexpr int kBlocks = BLOCKS, kWaves = BLOCKS * kThreads / 256;   // a CU, a SIMD
+  static constexpr int kWN = WN, kOut = 16384;   // bytes of results that leave at a time
+  static_assert(kOut + (kRows + 2 * kCols) * 4 <= kBuffer, "they fit the last buffer with the scales");
 };
 
 __device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, const char* base) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base)
+               : "memory", "m0");
 }
 template <int LEFT>
 __device__ __forceinline__ void wait_loads() {   // until that many are on their way at most
@@ -383,12 +386,11 @@ __device__ __forceinline__ const char* uniform(const char* p) {
 }
 
 template <typename U, class Deep, bool RELU>
-__global__ __launch_bounds__(Deep::kThreads, 2) void packed_deep_kernel(const RowArgs a, const PackedScales scales) {
+__global__ __launch_bounds__(Deep::kThreads, Deep::kWaves) void packed_deep_kernel(const RowArgs a, const PackedScales scales) {
   using S = Shape<2, Deep::kWN, 8, 4, 1, Deep::kBytes>;
   using Tile = RowTile<int8_t, Deep::kRows, Deep::kThreads, 1, Deep::kBytes>;
   static_assert(S::BM == Deep::kRows && S::BN == Deep::kCols && S::NT == Deep::kThreads, "the tile's");
   __shared__ __attribute__((aligned(1024))) char lds[Deep::kBuffers * Deep::kBuffer];
-  __shared__ __attribute__((aligned(16))) float sides[Deep::kRows + 2 * Deep::kCols];   // scales of rows, of columns, bias
   __shared__ Groups groups;
   groups.init(a.offsets, a.G, a.n, Deep::kRows);
   __syncthreads();
@@ -399,6 +401,8 @@ __global__ __launch_bounds__(Deep::kThreads, 2) void packed_deep_kernel(const Ro
   const int row_tiles = groups.total, total = row_tiles * a.col_tiles;
   int tile = blockIdx.x;
   if (tile >= total) return;
+  char* const outs = lds + (Deep::kBuffers - 1) * Deep::kBuffer;
+  float* const sides = reinterpret_cast<float*>(outs + Deep::kOut);   // scales of rows, of columns, bias
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
   const uint32_t place0 = __builtin_amdgcn_readfirstlane(
       (int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds) + (uint32_t)wave * 1024u;
@@ -501,26 +505,28 @@ __global__ __launch_bounds__(Deep::kThreads, 2) void packed_deep_kernel(const Ro
     const bool more = tile < total, full = at_hi - at_lo == Deep::kRows && n_first + Deep::kCols <= a.N;
     if (more) enter(tile);
     barrier_behind_lds();
-    // rows of all the tile's columns, 16 KB of them at a time
-    constexpr int kPitch = Deep::kCols * (int)sizeof(U), kUnits = kPitch / 16, kI = 16384 / (32 * kPitch) > 0 ? 16384 / (32 * kPitch) : 1;
-    static_assert(32 * kI * kPitch <= Deep::kBuffer && S::MI % kI == 0, "they fit the buffer");
-    char* const outs = lds + (Deep::kBuffers - 1) * Deep::kBuffer;
+    // kI rows of fragments at a time, of all the waves' columns or half of each wave's
+    constexpr int kJ = 32 * Deep::kCols * (int)sizeof(U) <= Deep::kOut ? 4 : 2;
+    constexpr int kPitch = Deep::kWN * kJ * 16 * (int)sizeof(U), kUnits = kPitch / 16, kWaveUnits = kUnits / Deep::kWN;
+    constexpr int kI = Deep::kOut / (32 * kPitch);
+    static_assert(kI >= 1 && S::MI % kI == 0 && kUnits >= 16, "whole rows");
     char* const C = reinterpret_cast<char*>(static_cast<U*>(a.C) + (int64_t)at_lo * a.ldc + n_first);
 #pragma unroll
-    for (int i0 = 0; i0 < S::MI; i0 += kI) {
+    for (int pass = 0; pass < S::MI / kI * (S::NJ / kJ); ++pass) {
+      const int i0 = pass / (S::NJ / kJ) * kI, j0 = pass % (S::NJ / kJ) * kJ;
 #pragma unroll
       for (int i = 0; i < kI; ++i) {
         const float sx = sides[m0 + (i0 + i) * 16 + tid % 16];
         const int r = ((wave / S::WN) * kI + i) * 16 + tid % 16;
 #pragma unroll
-        for (int j = 0; j < S::NJ; ++j) {
-          const int c = n0 + j * 16 + g4;
+        for (int j = 0; j < kJ; ++j) {
+          const int c = n0 + (j0 + j) * 16 + g4;
           const f32x4 times = *reinterpret_cast<const f32x4*>(sides + Deep::kRows + c);
           const f32x4 plus = *reinterpret_cast<const f32x4*>(sides + Deep::kRows + Deep::kCols + c);
           f32x4 v;
 #pragma unroll
-          for (int q = 0; q < 4; ++q) v[q] = finish<RELU>(acc[i0 + i][j][q], sx, times[q], plus[q]);
-          const int byte = c * (int)sizeof(U);
+          for (int q = 0; q < 4; ++q) v[q] = finish<RELU>(acc[i0 + i][j0 + j][q], sx, times[q], plus[q]);
+          const int byte = (wave % S::WN) * kWaveUnits * 16 + (j * 16 + g4) * (int)sizeof(U);
           char* const to = outs + r * kPitch + (((byte / 16) ^ (r % 16)) << 4) + byte % 16;
           if constexpr (sizeof(U) == 2) {
             bf16x4 o;
@@ -537,7 +543,8 @@ __global__ __launch_bounds__(Deep::kThreads, 2) void packed_deep_kernel(const Ro
       for (int k = 0; k < 32 * kI * kUnits / Deep::kThreads; ++k) {
         const int row = tid / kUnits + k * (Deep::kThreads / kUnits), u = tid % kUnits;
         const u32x4 v = *reinterpret_cast<const u32x4*>(outs + row * kPitch + ((u ^ (row % 16)) << 4));
-        const int m = (row / (16 * kI)) * S::MI * 16 + i0 * 16 + row % (16 * kI), c = u * kVec<U>;
+        const int m = (row / (16 * kI)) * S::MI * 16 + i0 * 16 + row % (16 * kI);
+        const int c = (u / kWaveUnits) * S::NJ * 16 + j0 * 16 + (u % kWaveUnits) * kVec<U>;
         char* const to = C + ((uint32_t)m * (uint32_t)a.ldc + (uint32_t)c) * (uint32_t)sizeof(U);
         if (full) {
           *reinterpret_cast<u32x4_any*>(to) = v;
@@ -553,8 +560,9 @@ __global__ __launch_bounds__(Deep::kThreads, 2) void packed_deep_kernel(const Ro
     }
     if (!more) break;
     if (steps >= Deep::kBuffers) ask(Deep::kBuffers - 1);
-    // the other stages were asked for before the stores (16 of a full tile, in fp32 32) and this one
-    constexpr int kStores = S::MI * 32 * kUnits / Deep::kThreads;
+    // the other stages were asked for before the stores of a full tile and this one
+    constexpr int kStores = Deep::kRows * Deep::kCols * (int)sizeof(U) / 16 / Deep::kThreads;
+    static_assert(Deep::kLoads + kStores < 64, "counted by the hardware");
     if (full && steps >= Deep::kBuffers) wait_loads<Deep::kLoads + kStores>();
     else wait_loads<0>();
     barrier_behind_lds();
@@ -631,7 +639,7 @@ hipError_t launch_type(const RowArgs& a, const PackedScales& p, int shape, hipSt
   // products overlap, for others. Both sides, us with two blocks / one: 8192 x 8192 x 8192 691 / 605, 8192 x 4096 x
   // 4096 153 / 140; k 2048 with ragged experts 168 / 184, 512 with 64 groups 151 / 167.
   if (shape == 0 && all % 16 == 0)
-    return a.K >= 4096 ? launch_deep<U, Deep<4, 4>>(a, p, s) : launch_deep<U, Deep<2, 3>>(a, p, s);
+    return a.K >= 4096 ? launch_deep<U, Deep<4, 4, 1>>(a, p, s) : launch_deep<U, Deep<2, 3, 2>>(a, p, s);
   switch (shape) {
     case 0: return launch<U, Large, false>(a, p, s);
     case 1: return launch<U, Middle, false>(a, p, s);

@@ -1,5 +1,12 @@
 // Routing to experts: scores of a row's logits, the choice of its best experts, their
 // weights, and the gradient of the logits.
+//
+// A row's experts are spread over few lanes (16 a lane where there are as many), so that most of the
+// work is within lanes and a wave has several rows. What bounds it is the number of operations: 262144 rows of
+// 64 experts in 8 sets, fp32, sigmoid and bias, 45 us (75 MB: 14 us at the rate of a copy), of some 1100
+// instructions for 16 rows; 8 lanes of 8 experts took 61 us, a wave a row in 64 bits throughout 332. The gradient
+// of 100003 rows of 193 experts, bf16, dense softmax: 30 us (85 MB: 16 us); adding the choices' parts
+// to every lane's experts in registers took 39.
 #include "learn_internal.h"
 #include "learn_softmax.h"
 #include "learn_tile.h"
@@ -676,7 +683,8 @@ __global__ __launch_bounds__(256) void router_backward_kernel(const RouterArgs a
       total = 0.f;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        q[v] = exp_near(q[v] - top);
+        // of bf16 logits the gradient is rounded to 2^-8: an exponential off by |z - top| 2^-23 will do
+        q[v] = sizeof(T) == 2 ? exp_(fmaxf(q[v] - top, kLeastE)) : exp_near(q[v] - top);
         total += q[v];
       }
       total = sum_of<L>(total);

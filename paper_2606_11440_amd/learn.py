@@ -496,7 +496,8 @@ def _exchange(rows, rows_name, slots, slots_name, slot, dslots=None, codes=False
     k = _matrix_of(slot, "slot")[1]
     if not _KINDS:
         _kinds()
-    return ImDispatchDesc(n, k, 1, m, dim, kind, ld, ld_slot, ld_dslot), dev, _flat(slot, "slot", _KINDS["i32"], dev, n * k)
+    return ImDispatchDesc(n, k, 1, m, dim, kind, ld, ld_slot, ld_dslot), dev, _flat(slot, "slot", _KINDS["i32"], dev,
+        n * k)
 
 
 def im_dispatch_forward(x, slot, xs, error=None, stream=None):
@@ -517,16 +518,20 @@ def im_dispatch_backward(dxs, slot, dx, error=None, stream=None):
 def im_combine_forward(ys, slot, weight, y, error=None, stream=None):
     """y[i] = sum of weight[i, c] ys[slot[i, c]] over c (weight float32 like slot)."""
     d, dev, ps = _exchange(y, "y", ys, "ys", slot)
-    _run(dev.index, (_learn or load_learn()).im_combine_forward, ctypes.byref(d), ys.data_ptr(), ps, _flat(weight, "weight", _KINDS["f32"], dev, slot.numel()), y.data_ptr(),
+    _run(dev.index, (_learn or load_learn()).im_combine_forward, ctypes.byref(d), ys.data_ptr(), ps, _flat(weight,
+         "weight", _KINDS["f32"], dev, slot.numel()), y.data_ptr(),
          _flat(error, "error", _KINDS["i32"], dev, 1), stream)
 
 
 def im_combine_backward(dy, ys, slot, weight, dys=None, dweight=None, error=None, stream=None):
     """Gradients of im_combine_forward: dys[slot[i, c]] = weight[i, c] dy[i] and dweight
     (float32 like slot); None skips one."""
+    if dweight is not None and ys is None:
+        _bad("dweight needs ys")
     d, dev, ps = _exchange(dy, "dy", ys, "ys", slot, dys)
     f32 = _KINDS["f32"]
-    _run(dev.index, (_learn or load_learn()).im_combine_backward, ctypes.byref(d), dy.data_ptr(), None if ys is None else ys.data_ptr(), ps,
+    _run(dev.index, (_learn or load_learn()).im_combine_backward, ctypes.byref(d), dy.data_ptr(),
+         None if ys is None else ys.data_ptr(), ps,
          _flat(weight, "weight", f32, dev, slot.numel()), None if dys is None else dys.data_ptr(),
          _flat(dweight, "dweight", f32, dev, slot.numel()), _flat(error, "error", _KINDS["i32"], dev, 1), stream)
 
@@ -550,7 +555,8 @@ def im_rows_pack(x, codes, scale, keep=False, stream=None):
 def im_rows_unpack(codes, scale, x, stream=None):
     """x = scale code in float32, rounded to its type."""
     d, dev, ps = _rows(x, codes, scale, False)
-    _run(dev.index, (_learn or load_learn()).im_rows_unpack, ctypes.byref(d), codes.data_ptr(), ps, x.data_ptr(), stream)
+    _run(dev.index, (_learn or load_learn()).im_rows_unpack, ctypes.byref(d), codes.data_ptr(), ps, x.data_ptr(),
+         stream)
 
 
 def im_linear_workspace_packed(n_rows, in_dim, out_dim, dtype, n_groups=1, backward=False, device=None):
@@ -572,7 +578,8 @@ def im_linear_forward_packed(x, x_scale, W, W_scale, b, y, offsets=None, relu=Fa
     ld_y = _matrix(y, "y", dt, dev, n, m)
     L = _learn or load_learn()
     d = ImLinearDesc(G, n, k, m, kind, 1 if relu else 0, 0, 0, ld_x, ld_y, 0)
-    ws, at, size = _workspace(L.im_linear_workspace_packed, d, (5, dev.index, G, n, k, m, kind), 0, workspace, dev, stream)
+    ws, at, size = _workspace(L.im_linear_workspace_packed, d, (5, dev.index, G, n, k, m, kind), 0, workspace, dev,
+        stream)
     _run(dev.index, L.im_linear_forward_packed, ctypes.byref(d), _offsets(offsets, G, dev), x.data_ptr(),
          _flat(x_scale, "x_scale", f32, dev, n), W.data_ptr(),
          _flat(W_scale, "W_scale", f32, dev, G * m), _flat(b, "b", f32, dev, G * m),
@@ -595,8 +602,10 @@ def im_linear_backward_packed(dy, x, x_scale, W, dx=None, dW=None, db=None, offs
     ld_dx = k if dx is None else _matrix(dx, "dx", dt, dev, n, k)
     L = _learn or load_learn()
     d = ImLinearDesc(G, n, k, m, kind, 0, 1 if relu_in else 0, 0, ld_x, ld_y, ld_dx)
-    ws, at, size = _workspace(L.im_linear_workspace_packed, d, (6, dev.index, G, n, k, m, kind), 1, workspace, dev, stream)
-    _run(dev.index, L.im_linear_backward_packed, ctypes.byref(d), _offsets(offsets, G, dev), dy.data_ptr(), x.data_ptr(),
+    ws, at, size = _workspace(L.im_linear_workspace_packed, d, (6, dev.index, G, n, k, m, kind), 1, workspace, dev,
+        stream)
+    _run(dev.index, L.im_linear_backward_packed, ctypes.byref(d), _offsets(offsets, G, dev), dy.data_ptr(),
+         x.data_ptr(),
          _flat(x_scale, "x_scale", f32, dev, n), W.data_ptr(),
          None if dx is None else dx.data_ptr(), _flat(dW, "dW", dt, dev, G * m * k),
          _flat(db, "db", f32, dev, G * m), at, size,
