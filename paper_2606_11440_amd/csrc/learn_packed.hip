@@ -47,25 +47,31 @@ __device__ __forceinline__ u32x4 unit_load(const T* row, int u, int dim) {
   return dim < kVec<T> ? load_few(row, dim) : load16(row + unit_at<T>(u, dim));
 }
 
-// Largest magnitude of a unit, as the bits of a float: they order as magnitudes do, NaN above infinity.
+// Largest magnitude of units, as the bits of a float: they order as magnitudes do, NaN above
+// infinity. bf16: two at a time as 16-bit integers.
 template <typename T>
-__device__ __forceinline__ uint32_t most_bits(u32x4 v, uint32_t most) {
+struct Most {
+  uint32_t v = 0;
+  __device__ __forceinline__ void add(u32x4 x) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t w = v[i];
-    if constexpr (sizeof(T) == 2) {
-      const uint32_t lo = (w << 16) & 0x7fffffffu, hi = w & 0x7fff0000u;
-      most = lo > most ? lo : most;
-      most = hi > most ? hi : most;
-    } else {
-      const uint32_t b = w & 0x7fffffffu;
-      most = b > most ? b : most;
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 2) {
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        const uint32_t w = x[i] & 0x7fff7fffu;
+        v = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, v), __builtin_bit_cast(u16x2, w)));
+      } else {
+        const uint32_t w = x[i] & 0x7fffffffu;
+        v = w > v ? w : v;
+      }
     }
   }
-  return most;
-}
+  __device__ __forceinline__ uint32_t bits() const {
+    if constexpr (sizeof(T) == 2) return max(v << 16, v & 0xffff0000u);
+    else return v;
+  }
+};
 
-// Largest over L neighbouring lanes (most_bits' integers: no sign).
+// Largest over L neighbouring lanes (Most's bits: no sign).
 template <int L>
 __device__ __forceinline__ uint32_t most_across(uint32_t x) {
   int32_t v = (int32_t)x;
@@ -91,30 +97,39 @@ struct Scale {
   }
 };
 
-template <typename T>
-__device__ __forceinline__ void put_codes(int8_t* row, int u, int dim, u32x4 v, const Scale& s, bool keep) {
+// Codes of a unit: x times the inverse, rounded to nearest even by adding 1.5 2^23, whose sum's low byte is
+// the code (at most 127: scale and inverse are off by half a unit each). keep: below 3/4 other numbers than zero
+// count as that.
+template <typename T, bool KEEP>
+__device__ __forceinline__ void put_codes(int8_t* row, int u, int dim, u32x4 v, const Scale& s) {
+#pragma clang fp contract(off)   // the product is rounded before the sum
+  if (s.inverse == 0.f) v = u32x4{0, 0, 0, 0};   // no infinity times 0
   float f[kVec<T>];
   widen<T>(v, f);
-  int8_t q[kVec<T>];
+  uint32_t q[kVec<T>];
 #pragma unroll
   for (int i = 0; i < kVec<T>; ++i) {
-    const float x = s.inverse == 0.f ? 0.f : f[i];   // no infinity times 0
-    int c = (int)rintf(x * s.inverse);               // 127 at most: scale and inverse are off by half a unit each
-    if (keep && c == 0) c = x > 0.f ? 1 : (x < 0.f ? -1 : 0);
-    q[i] = (int8_t)c;
+    float p = f[i] * s.inverse;
+    if (KEEP) p = f[i] == 0.f ? 0.f : copysignf(fmaxf(fabsf(p), 0.75f), f[i]);
+    q[i] = __builtin_bit_cast(uint32_t, p + 12582912.f);
   }
+  uint32_t c[kVec<T> / 4];   // four codes each: their low bytes
+#pragma unroll
+  for (int i = 0; i < kVec<T> / 4; ++i)
+    c[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[4 * i + 3], q[4 * i + 2], 0x0c0c0400u),
+                                 __builtin_amdgcn_perm(q[4 * i + 1], q[4 * i], 0x0c0c0400u), 0x05040100u);
   if (dim < kVec<T>) {
 #pragma unroll
     for (int i = 0; i < kVec<T>; ++i)
-      if (i < dim) row[i] = q[i];
+      if (i < dim) row[i] = (int8_t)(c[i / 4] >> (8 * (i % 4)));
   } else {
-    __builtin_memcpy(row + unit_at<T>(u, dim), q, kVec<T>);
+    __builtin_memcpy(row + unit_at<T>(u, dim), c, kVec<T>);
   }
 }
 
 // L lanes a row, N units a lane and R rows at once, kept in registers between the largest magnitude and
 // the codes.
-template <typename T, int L, int N, int R>
+template <typename T, int L, int N, int R, bool KEEP>
 __global__ __launch_bounds__(256) void pack_kernel(const PackArgs a) {
   constexpr int kRows = 256 / L;   // of a block, R times
   const int l = (int)threadIdx.x % L, units = (a.dim + kVec<T> - 1) / kVec<T>;
@@ -132,17 +147,17 @@ __global__ __launch_bounds__(256) void pack_kernel(const PackArgs a) {
     }
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      uint32_t most = 0;
+      Most<T> seen;
 #pragma unroll
-      for (int i = 0; i < N; ++i) most = most_bits<T>(v[k][i], most);
-      most = most_across<L>(most);
+      for (int i = 0; i < N; ++i) seen.add(v[k][i]);
+      const uint32_t most = most_across<L>(seen.bits());
       const int64_t row = at + k * kRows;
       if (row >= a.n) continue;   // the last block's other lanes
       const Scale s(most);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int u = l + i * L;
-        if (u < units) put_codes<T>(a.codes + row * a.ld_codes, u, a.dim, v[k][i], s, a.keep != 0);
+        if (u < units) put_codes<T, KEEP>(a.codes + row * a.ld_codes, u, a.dim, v[k][i], s);
       }
       if (l == 0) a.scale[row] = s.scale;
     }
@@ -150,20 +165,16 @@ __global__ __launch_bounds__(256) void pack_kernel(const PackArgs a) {
 }
 
 // A block a row, for long rows: they are read again for the codes (from the L2).
-template <typename T>
+template <typename T, bool KEEP>
 __global__ __launch_bounds__(1024) void pack_long_kernel(const PackArgs a) {
   __shared__ uint32_t across[16];
   const int units = (a.dim + kVec<T> - 1) / kVec<T>;
   for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
     const T* from = static_cast<const T*>(a.x) + row * a.ld_x;
-    uint32_t most = 0;
+    Most<T> seen;
 #pragma unroll 4
-    for (int u = threadIdx.x; u < units; u += 1024) most = most_bits<T>(unit_load<T>(from, u, a.dim), most);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const uint32_t o = (uint32_t)__shfl_xor((int)most, d);
-      most = o > most ? o : most;
-    }
+    for (int u = threadIdx.x; u < units; u += 1024) seen.add(unit_load<T>(from, u, a.dim));
+    uint32_t most = most_across<64>(seen.bits());
     __syncthreads();
     if (threadIdx.x % 64 == 0) across[threadIdx.x / 64] = most;
     __syncthreads();
@@ -172,7 +183,7 @@ __global__ __launch_bounds__(1024) void pack_long_kernel(const PackArgs a) {
     const Scale s(most);
 #pragma unroll 4
     for (int u = threadIdx.x; u < units; u += 1024)
-      put_codes<T>(a.codes + row * a.ld_codes, u, a.dim, unit_load<T>(from, u, a.dim), s, a.keep != 0);
+      put_codes<T, KEEP>(a.codes + row * a.ld_codes, u, a.dim, unit_load<T>(from, u, a.dim), s);
     if (threadIdx.x == 0) a.scale[row] = s.scale;
   }
 }
@@ -650,7 +661,9 @@ hipError_t launch_type(const RowArgs& a, const PackedScales& p, int shape, hipSt
 
 template <typename T, int L, int N, int R>
 hipError_t pack_rows(const PackArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((pack_kernel<T, L, N, R>), dim3(blocks_of(a.n, 256 / L * R)), dim3(256), 0, s, a);
+  const dim3 grid(blocks_of(a.n, 256 / L * R)), block(256);
+  if (a.keep) hipLaunchKernelGGL((pack_kernel<T, L, N, R, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((pack_kernel<T, L, N, R, false>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 // R rows at once where there are enough to fill the card so; single ones otherwise.
@@ -669,7 +682,8 @@ hipError_t pack(const PackArgs& a, hipStream_t s) {
   if (units <= 128) return pack_some<T, 64, 2, 2>(a, s);
   if (units <= 256) return pack_rows<T, 64, 4, 1>(a, s);
   if (units <= 512) return pack_rows<T, 64, 8, 1>(a, s);
-  hipLaunchKernelGGL(pack_long_kernel<T>, dim3(blocks_of(a.n, 1)), dim3(1024), 0, s, a);
+  if (a.keep) hipLaunchKernelGGL((pack_long_kernel<T, true>), dim3(blocks_of(a.n, 1)), dim3(1024), 0, s, a);
+  else hipLaunchKernelGGL((pack_long_kernel<T, false>), dim3(blocks_of(a.n, 1)), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 template <typename T>
