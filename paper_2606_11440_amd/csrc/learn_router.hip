@@ -294,7 +294,10 @@ __device__ __forceinline__ void logits4(const RouterArgs& a, int64_t row, int j,
     z[i] = fminf(fmaxf(z[i], -INFINITY), kLargest);   // NaN: -infinity
   if (a.valid) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) z[i] = (ok >> i) & 1u ? z[i] : -INFINITY;
+    for (int i = 0; i < 4; ++i) {   // its bit as a mask of all: a bit select
+      const uint32_t m = (uint32_t)((int32_t)(ok << (31 - i)) >> 31);
+      z[i] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, z[i]) & m) | (0xff800000u & ~m));
+    }
   }
 }
 
@@ -684,7 +687,7 @@ __global__ __launch_bounds__(256) void router_backward_kernel(const RouterArgs a
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         // of bf16 logits the gradient is rounded to 2^-8: an exponential off by |z - top| 2^-23 will do
-        q[v] = sizeof(T) == 2 ? exp_(fmaxf(q[v] - top, kLeastE)) : exp_near(q[v] - top);
+        q[v] = sizeof(T) == 2 ? exp_(q[v] - top) : exp_near(q[v] - top);
         total += q[v];
       }
       total = sum_of<L>(total);
