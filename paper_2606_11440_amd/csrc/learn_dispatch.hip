@@ -233,37 +233,49 @@ __device__ __forceinline__ u32x4 narrow_to(const float (&f)[kVec<T>]) {
 
 constexpr int kTogether = 4;   // choices whose rows are on their way at once
 
-// to_i = sum_c weight_ic from[slot_ic], by T lanes a row.
-template <typename E, int T>
+// to_i = sum_c weight_ic from[slot_ic], by T lanes a row, N units a lane at once.
+template <typename E, int T, int N>
 __global__ __launch_bounds__(256) void gather_kernel(const ExchangeArgs a) {
   const int l = (int)threadIdx.x % T, units = (a.dim + kVec<E> - 1) / kVec<E>;
   constexpr int kRows = 256 / T;
   bool wrong = false;
   for (int64_t row = (int64_t)blockIdx.x * kRows + (int)threadIdx.x / T; row < a.n; row += (int64_t)gridDim.x * kRows) {
-    for (int u = l; u < units; u += T) {
-      const Piece<E> p(u, a.dim);
-      float sum[kVec<E>];
+    for (int u0 = l; u0 < units; u0 += T * N) {
+      float sum[N][kVec<E>];
 #pragma unroll
-      for (int i = 0; i < kVec<E>; ++i) sum[i] = 0.f;
+      for (int m = 0; m < N; ++m)
+#pragma unroll
+        for (int i = 0; i < kVec<E>; ++i) sum[m][i] = 0.f;
       for (int c0 = 0; c0 < a.k; c0 += kTogether) {
-        u32x4 v[kTogether];
+        u32x4 v[kTogether][N];
         float w[kTogether];
 #pragma unroll
         for (int j = 0; j < kTogether; ++j) {
           const int s = slot_of(a, row, c0 + j, wrong);
           w[j] = s < 0 ? 0.f : (a.weight ? a.weight[row * a.k + c0 + j] : 1.f);
-          v[j] = u32x4{0, 0, 0, 0};
-          if (s >= 0) v[j] = p.load(static_cast<const E*>(a.from) + s * a.ld_from, a.dim);
+#pragma unroll
+          for (int m = 0; m < N; ++m) v[j][m] = u32x4{0, 0, 0, 0};
+          if (s >= 0) {
+            const E* from = static_cast<const E*>(a.from) + s * a.ld_from;
+#pragma unroll
+            for (int m = 0; m < N; ++m)   // past the row's units its last one, which is not stored
+              v[j][m] = Piece<E>(u0 + m * T < units ? u0 + m * T : units - 1, a.dim).load(from, a.dim);
+          }
         }
 #pragma unroll
-        for (int j = 0; j < kTogether; ++j) {
-          float f[kVec<E>];
-          widen<E>(v[j], f);
+        for (int j = 0; j < kTogether; ++j)
 #pragma unroll
-          for (int i = 0; i < kVec<E>; ++i) sum[i] = fmaf(w[j], f[i], sum[i]);
-        }
+          for (int m = 0; m < N; ++m) {
+            float f[kVec<E>];
+            widen<E>(v[j][m], f);
+#pragma unroll
+            for (int i = 0; i < kVec<E>; ++i) sum[m][i] = fmaf(w[j], f[i], sum[m][i]);
+          }
       }
-      p.store(static_cast<E*>(a.to) + row * a.ld_to, a.dim, narrow_to<E>(sum));
+#pragma unroll
+      for (int m = 0; m < N; ++m)
+        if (u0 + m * T < units)
+          Piece<E>(u0 + m * T, a.dim).store(static_cast<E*>(a.to) + row * a.ld_to, a.dim, narrow_to<E>(sum[m]));
     }
   }
   if (wrong && a.error) atomicOr(a.error, IM_ERR_ACTION);
@@ -342,8 +354,13 @@ struct Kernels {
   }
   static void gather(const ExchangeArgs& a, int e, hipStream_t s) {
     const dim3 grid(blocks_of(a.n, 256 / T)), block(256);
-    if (e == 2) hipLaunchKernelGGL((gather_kernel<__bf16, T>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((gather_kernel<float, T>), grid, block, 0, s, a);
+    if (T == 64 && (int64_t)a.dim * e > 1024) {   // more units than lanes
+      if (e == 2) hipLaunchKernelGGL((gather_kernel<__bf16, T, 2>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((gather_kernel<float, T, 2>), grid, block, 0, s, a);
+    } else {
+      if (e == 2) hipLaunchKernelGGL((gather_kernel<__bf16, T, 1>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((gather_kernel<float, T, 1>), grid, block, 0, s, a);
+    }
   }
   static void backward(const ExchangeArgs& a, int e, hipStream_t s) {
     const dim3 grid(blocks_of(a.n, 256 / T)), block(256);
