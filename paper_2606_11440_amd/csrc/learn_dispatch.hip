@@ -1,5 +1,12 @@
 // Rows to experts and back: the places of (row, choice) pairs ordered by expert, the rows
 // sent there, and the weighted sums that return.
+//
+// The plan is a stable counting sort: pairs of an expert in the blocks and waves before, then ranks within
+// 64 pairs by ballots of the experts' bits; 262144 pairs of 64 experts 11 us, its two launches and their latency (2 MB of
+// pairs and places), 96 pairs 2.6 us in one. The rest is memory: a row is spread over up to 64 lanes in
+// 16-byte units. 65536 rows of 512, bf16: sent to 4 places each 60 us (5.6 TB/s), the weighted sum's gradient
+// 116 us (5.1 TB/s); 30011 rows of 387, fp32, summed from 3 places each 37 us (4.7 TB/s; 41
+// with the units of a lane one after the other).
 #include "learn_internal.h"
 #include "learn_tile.h"
 #include "wave.h"

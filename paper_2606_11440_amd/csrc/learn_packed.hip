@@ -1,6 +1,7 @@
 // Rows in 8 bits: packing, unpacking, and the product of packed rows with packed weights.
 //
-// Pack and unpack are one pass over memory: 262144 rows of 512, bf16, 82 us (4.9 TB/s).
+// Pack and unpack are one pass over memory: 262144 rows of 512, bf16, 76 us (5.3 TB/s; 101
+// with one row a wave at a time).
 // The product goes as that of bf16 rows does (tiles, stages of 128 bytes, blocks that keep taking tiles), on
 // v_mfma_i32_16x16x64_i8: twice the operations a byte of LDS, and an exact sum (127^2 65536 is below
 // 2^31), which the scales of its row and column multiply once. Large tiles of aligned rows have a kernel

@@ -3,7 +3,7 @@
 //
 // A row's experts are spread over few lanes (16 a lane where there are as many), so that most of the
 // work is within lanes and a wave has several rows. What bounds it is the number of operations: 262144 rows of
-// 64 experts in 8 sets, fp32, sigmoid and bias, 45 us (75 MB: 14 us at the rate of a copy), of some 1100
+// 64 experts in 8 sets, fp32, sigmoid and bias, 45 us (75 MB: 14 us at the rate of a copy), of some 1150
 // instructions for 16 rows; 8 lanes of 8 experts took 61 us, a wave a row in 64 bits throughout 332. The gradient
 // of 100003 rows of 193 experts, bf16, dense softmax: 30 us (85 MB: 16 us); adding the choices' parts
 // to every lane's experts in registers took 39.

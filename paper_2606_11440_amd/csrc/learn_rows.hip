@@ -120,7 +120,8 @@ struct Row {
   }
 };
 
-// The layer's input that a gradient passes: a unit of T, or of as many int8 codes.
+// The layer's input that a gradient passes: a unit of T, or of as many int8 codes (dx of 64 groups, 262144
+// rows, 512 x 512, bf16: 235 us with the mask from codes, 256 from bf16 rows).
 template <typename T, bool CODES>
 struct InputMask {
   using element = T;

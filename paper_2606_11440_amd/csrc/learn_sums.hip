@@ -41,7 +41,9 @@ __device__ __forceinline__ void store_some(T* p, f32x4 v, int left) {
   }
 }
 
-// CODES: Q is int8 codes with a scale a row.
+// CODES: Q is int8 codes with a scale a row, decoded on their way to LDS: 64 ragged groups of 262144 rows, 512 x
+// 512, bf16, 190 us where bf16 rows take 170; the conversions (five operations for two values) are more than
+// the half as many bytes save.
 template <typename T, class S, bool CODES>
 __global__ __launch_bounds__(S::NT, S::MI * S::NJ >= 32 ? 2 : 3) void sums_kernel(const SumArgs a) {
   using P = ColTile<T, S::BM, S::NT, S::D, S::SB>;
