@@ -30,7 +30,7 @@ class Policy:
                       b1=normal(E, H, t=f, scale=0.1), W2=normal(E, D2, H, scale=H ** -0.5),
                       b2=normal(E, D2, t=f, scale=0.1), Wh=normal(V, D2, scale=D2 ** -0.5), bh=normal(V, t=f, scale=0.1))
         self.target = torch.randint(0, V, (n,), device="cuda", generator=g, dtype=i)
-        self.dlogp = normal(n, t=f, scale=1 / n)
+        self.dlogp = normal(n, t=f, scale=1 / max(n, 1))
         self.bias = normal(E, t=f, scale=0.02)
         self.z, self.e, self.w = empty(n, E), empty(n, K, t=i), empty(n, K, t=f)
         self.off, self.slot = empty(E + 1, t=i), empty(n, K, t=i)
@@ -236,3 +236,46 @@ def test_the_same_bits_again():
         c.backward()
         for a, b in zip(c.out(), first):
             assert bool((a == b).all())
+
+
+def test_captured_plan_and_long_sums():
+    """What takes workspaces (a plan in blocks, a product in runs of k), captured and replayed on other inputs."""
+    note("[experts: captured workspaces]")
+    import paper_2606_11440_amd as P
+    torch = need_gpu()
+    n, k, e = 30000, 2, 50
+    expert = torch.zeros(n, k, dtype=torch.int32, device="cuda")
+    off, slot = torch.zeros(e + 1, dtype=torch.int32, device="cuda"), torch.zeros_like(expert)
+    q, s = torch.zeros(20, 9000, dtype=torch.int8, device="cuda"), torch.ones(20, device="cuda")
+    W, y = torch.randint(-127, 128, (33, 9000), dtype=torch.int8, device="cuda"), torch.zeros(20, 33, device="cuda")
+    Ws = torch.rand(33, device="cuda")
+
+    def run(off, slot, y):
+        P.im_dispatch_plan(expert, off, slot)
+        P.im_linear_forward_packed(q, s, W, Ws, None, y)
+    run(off, slot, y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(off, slot, y)
+    for r in range(4):
+        expert.copy_(torch.randint(-1, e, (n, k), dtype=torch.int32, generator=torch.Generator().manual_seed(r)))
+        q.copy_(torch.randint(-127, 128, q.shape, dtype=torch.int8, generator=torch.Generator().manual_seed(r)))
+        graph.replay()
+        a = [torch.zeros_like(t) for t in (off, slot, y)]
+        run(*a)
+        torch.cuda.synchronize()
+        assert all(bool((x == z).all()) for x, z in zip(a, (off, slot, y))), r
+        assert bool((slot.cpu() == X.plan(expert.cpu(), e)[1]).all())
+
+
+def test_no_rows_anywhere():
+    """Every call without rows."""
+    note("[experts: none]")
+    c = Policy("float32", n=0)
+    for t in list(c.g.values()):
+        t.fill_(7.0)
+    c.forward()
+    c.backward()
+    assert int(c.error) == 0 and c.off.tolist() == [0] * (E + 1)
+    assert all(bool((t == 0).all()) for t in c.g.values())

@@ -193,6 +193,33 @@ def test_large_tiles(n, k, m, sizes, dtype):
     check_forward(wide, relu=True)
 
 
+def test_large_tiles_and_rows_that_are_not_finite():
+    """In large tiles too a row's NaN scale is its own, and one behind the last group reaches nothing."""
+    note("[packed large: NaN]")
+    import paper_2606_11440_amd as P
+    c = make(70000, 64, 512, [33000, 36990], BF16, seed=3)
+    torch = c["torch"]
+    bad = torch.tensor([0, 255, 256, 33000, 69989], device="cuda")
+    c["s"][bad] = float("nan")
+    c["s"][69990:] = float("nan")
+    y = torch.full((70000, 512), 77.0, dtype=torch.bfloat16, device="cuda")
+    P.im_linear_forward_packed(c["q"], c["s"], c["Wq"], c["Ws"], c["b"], y, offsets=c["dev"], relu=True)
+    rows = torch.isnan(y).all(1)
+    assert int(rows.sum()) == 5 and bool(rows[bad].all()) and int(torch.isnan(y).sum()) == 5 * 512
+    assert bool((y[69990:] == 77.0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_many_groups(dtype):
+    """1024 groups, most of them empty or of some rows, one of most rows."""
+    note(f"[packed groups] {dtype}")
+    sizes = [(7 * g) % 5 if g % 3 else 0 for g in range(1024)]
+    sizes[500] = 9000
+    c = make(sum(sizes) + 11, 80, 48, sizes, dtype, seed=6, relu=True)
+    check_forward(c, relu=True)
+    check_backward(c, relu_in=True)
+
+
 @pytest.mark.parametrize("some", [("dx",), ("dW",), ("db",), ("dW", "db")])
 def test_some_gradients(some):
     note(f"[packed: some gradients] {some}")
