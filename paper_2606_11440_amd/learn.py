@@ -22,7 +22,9 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
+from . import _lib
 from ._lib import HERE, IM_BF16, IM_EINVAL, IM_F32, IM_OK, IMError, _stream
 
 LEARN_PATH = os.path.join(HERE, "libinframind_learn.so")
@@ -142,22 +144,20 @@ class _On:
             torch.cuda.set_device(self.was)
 
 
-_device = None   # torch's accessor of the current device's number
+_device = _raw = None   # torch's accessors of the current device's number and of its current stream's handle
 
 
-def _run(index, call, *args):
-    """A call of the library on device `index`, with torch's current stream of it where the last
-    argument is None."""
-    global _device
+def _run(index, stream, call, *args):
+    """A call of the library on device `index` and on `stream`, or torch's current stream of that device."""
+    global _device, _raw
     if _device is None:
-        import torch
-        torch.cuda.init()
-        _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        _stream(None)
+        _raw, _device = _lib._current
     if _device() == index:
-        status = call(*args[:-1], _stream(args[-1]))
+        status = call(*args, _raw(index) if stream is None else int(stream))
     else:
         with _On(index):
-            status = call(*args[:-1], _stream(args[-1]))
+            status = call(*args, _stream(stream))
     if status != IM_OK:
         raise IMError(status, im_learn_last_error())
 
@@ -392,13 +392,56 @@ def im_head_backward(h, W, b, target, lse, dlogp, dh=None, dW=None, db=None, val
                                  _stream(stream)))
 
 
-def _mask(valid, n, classes, dev):
+# The calls below check a tensor in the order that passes soonest; what does not pass is looked at again by
+# _flat and _matrix, which say why. Descriptions are packed as the C structures lie.
+_LINEAR, _ROUTER, _DISPATCH, _ROWS = (struct.Struct(f) for f in ("=8i3q", "=9if2q", "=6i3q", "=4i2q"))
+
+
+def _desc(form, *values):
+    try:
+        return form.pack(*values)
+    except (struct.error, OverflowError) as e:
+        _bad(f"an argument is out of range: {e}")
+
+
+def _cuda(index):
+    import torch
+    return torch.device("cuda", index)
+
+
+def _first(t, name):
+    """im_dtype and device number of a tensor on a GPU."""
+    if not _KINDS:
+        _kinds()
+    kind = _KINDS.get(t.dtype) if t.is_cuda else None
+    return (_kind(t, name) if kind is None else kind), t.get_device()
+
+
+def _at(t, name, dtype, index, count):
+    """Pointer of a contiguous tensor of `count` elements, or None."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.get_device() == index and t.numel() == count and t.is_contiguous():
+        return t.data_ptr()
+    return _flat(t, name, dtype, _cuda(index), count)
+
+
+def _ld(t, name, dtype, index, rows, cols):
+    """Row stride of a [rows, cols] tensor whose columns are contiguous."""
+    if rows > 1 and t.dtype is dtype and t.get_device() == index and t.shape == (rows, cols):
+        ld, inner = t.stride()
+        if inner == 1 and ld >= cols:
+            return ld
+    return _matrix(t, name, dtype, _cuda(index), rows, cols)
+
+
+def _mask(valid, n, classes, index):
     """Pointer of the words of a mask [n, ceil(classes / 32)], or None."""
     if valid is None:
         return None
     if valid.dtype is not _KINDS["i32"] and str(valid.dtype) != "torch.uint32":
         _bad(f"valid is {valid.dtype}: int32 (or uint32) words expected")
-    return _flat(valid, "valid", valid.dtype, dev, n * ((classes + 31) // 32))
+    return _at(valid, "valid", valid.dtype, index, n * ((classes + 31) // 32))
 
 
 def _matrix_of(t, name):
@@ -407,9 +450,8 @@ def _matrix_of(t, name):
 
 
 def _score(score):
-    if score not in SCORES:
-        _bad(f"score is {score!r}: 'softmax' or 'sigmoid' expected")
-    return SCORES[score]
+    at = SCORES.get(score)
+    return _bad(f"score is {score!r}: 'softmax' or 'sigmoid' expected") if at is None else at
 
 
 def im_router_forward(z, expert, weight, bias=None, valid=None, score="softmax", renorm=True, scale=1.0, n_sets=1,
@@ -419,33 +461,28 @@ def im_router_forward(z, expert, weight, bias=None, valid=None, score="softmax",
     the choice goes by score + bias (float32 [experts]) within the top_sets best of
     n_sets equal sets, valued by their set_best (1 or 2) best; weights are scale times the
     scores, divided by their sum with renorm. valid: as for im_head_forward."""
-    kind, dev, dt = _kind(z, "z"), z.device, z.dtype
+    kind, on = _first(z, "z")
     n, E = _matrix_of(z, "z")
-    ld = _matrix(z, "z", dt, dev, n, E)
     k = _matrix_of(expert, "expert")[1]
-    f32, i32 = _KINDS["f32"], _KINDS["i32"]
-    L = _learn or load_learn()
-    d = ImRouterDesc(n, E, k, n_sets, n_sets if top_sets is None else top_sets, set_best, kind, _score(score),
-                     1 if renorm else 0, scale, ld, 0)
-    _run(dev.index, L.im_router_forward, ctypes.byref(d), z.data_ptr(), _flat(bias, "bias", f32, dev, E),
-         _mask(valid, n, E, dev), _flat(expert, "expert", i32, dev, n * k),
-         _flat(weight, "weight", f32, dev, n * k), stream)
+    f32 = _KINDS["f32"]
+    d = _desc(_ROUTER, n, E, k, n_sets, n_sets if top_sets is None else top_sets, set_best, kind, _score(score),
+              1 if renorm else 0, scale, _ld(z, "z", z.dtype, on, n, E), 0)
+    _run(on, stream, (_learn or load_learn()).im_router_forward, d, z.data_ptr(), _at(bias, "bias", f32, on, E),
+         _mask(valid, n, E, on), _at(expert, "expert", _KINDS["i32"], on, n * k), _at(weight, "weight", f32, on, n * k))
 
 
 def im_router_backward(z, expert, dweight, dz, valid=None, score="softmax", renorm=True, scale=1.0, error=None,
                        stream=None):
     """Gradient dz [n, experts] of the logits from dweight (float32 [n, top_k]), for the
     experts that im_router_forward chose. Rows of z and dz may be strided."""
-    kind, dev, dt = _kind(z, "z"), z.device, z.dtype
+    kind, on = _first(z, "z")
     n, E = _matrix_of(z, "z")
-    ld, ld_dz = _matrix(z, "z", dt, dev, n, E), _matrix(dz, "dz", dt, dev, n, E)
-    k = _matrix_of(expert, "expert")[1]
-    f32, i32 = _KINDS["f32"], _KINDS["i32"]
-    L = _learn or load_learn()
-    d = ImRouterDesc(n, E, k, 1, 1, 1, kind, _score(score), 1 if renorm else 0, scale, ld, ld_dz)
-    _run(dev.index, L.im_router_backward, ctypes.byref(d), z.data_ptr(), _mask(valid, n, E, dev),
-         _flat(expert, "expert", i32, dev, n * k), _flat(dweight, "dweight", f32, dev, n * k),
-         dz.data_ptr(), _flat(error, "error", i32, dev, 1), stream)
+    k, dt, i32 = _matrix_of(expert, "expert")[1], z.dtype, _KINDS["i32"]
+    d = _desc(_ROUTER, n, E, k, 1, 1, 1, kind, _score(score), 1 if renorm else 0, scale, _ld(z, "z", dt, on, n, E),
+              _ld(dz, "dz", dt, on, n, E))
+    _run(on, stream, (_learn or load_learn()).im_router_backward, d, z.data_ptr(), _mask(valid, n, E, on),
+         _at(expert, "expert", i32, on, n * k), _at(dweight, "dweight", _KINDS["f32"], on, n * k), dz.data_ptr(),
+         _at(error, "error", i32, on, 1))
 
 
 def _dispatch_size(desc, backward, out):
@@ -461,66 +498,67 @@ def im_dispatch_workspace(n_rows, top_k, n_experts, device=None):
 def im_dispatch_plan(expert, offsets, slot, workspace=None, error=None, stream=None):
     """Places of the pairs of expert (int32 [n, top_k], -1: none) ordered by expert: slot
     like expert, and offsets int32 [experts + 1], the groups of the layers that follow."""
-    if expert.device.type != "cuda":
+    if not expert.is_cuda:
         _bad(f"expert is on {expert.device}, a GPU is expected")
     if not _KINDS:
         _kinds()
-    dev, i32 = expert.device, _KINDS["i32"]
+    on, i32 = expert.get_device(), _KINDS["i32"]
     n, k = _matrix_of(expert, "expert")
     E = offsets.numel() - 1
-    L = _learn or load_learn()
-    d = ImDispatchDesc(n, k, E, 0, 1, 0, 1, 1, 1)
-    ws, at, size = _workspace(lambda desc, backward, out: L.im_dispatch_workspace(desc, out), d,
-                                  (4, dev.index, n, k, E), 0, workspace, dev, stream)
-    _run(dev.index, L.im_dispatch_plan, ctypes.byref(d), _flat(expert, "expert", i32, dev, n * k),
-         _flat(offsets, "offsets", i32, dev, E + 1), _flat(slot, "slot", i32, dev, n * k), at,
-         size, _flat(error, "error", i32, dev, 1), stream)
+    d, key = _desc(_DISPATCH, n, k, E, 0, 1, 0, 1, 1, 1), (4, on, n, k, E)
+    ws, at, size = None, None, 0
+    if _SIZES.get(key) != 0:
+        ws, at, size = _workspace(_dispatch_size, ImDispatchDesc.from_buffer_copy(d), key, 0, workspace, expert.device,
+                                  stream)
+    _run(on, stream, (_learn or load_learn()).im_dispatch_plan, d, _at(expert, "expert", i32, on, n * k),
+         _at(offsets, "offsets", i32, on, E + 1), _at(slot, "slot", i32, on, n * k), at, size,
+         _at(error, "error", i32, on, 1))
 
 
 def _exchange(rows, rows_name, slots, slots_name, slot, dslots=None, codes=False):
-    """Description of an exchange between rows [n, dim] and slots' rows [n_slots, dim]."""
-    if codes and str(rows.dtype) == "torch.int8" and rows.device.type == "cuda":
-        kind = IM_CODES
-    else:
-        kind = _kind(rows, rows_name)
-    dev, dt = rows.device, rows.dtype
-    n, dim = _matrix_of(rows, rows_name)
-    ld = _matrix(rows, rows_name, dt, dev, n, dim)
-    if slots is None:
-        slots, slots_name = dslots, "dys"
-    m, ld_slot = 0, dim
-    if slots is not None:
-        m = _matrix_of(slots, slots_name)[0]
-        ld_slot = _matrix(slots, slots_name, dt, dev, m, dim)
-    ld_dslot = dim if dslots is None else _matrix(dslots, "dys", dt, dev, m, dim)
-    k = _matrix_of(slot, "slot")[1]
+    """Description of an exchange between rows [n, dim] and slots' rows [n_slots, dim], the device's
+    number and the slots' pointer."""
+    dt = rows.dtype
     if not _KINDS:
         _kinds()
-    return ImDispatchDesc(n, k, 1, m, dim, kind, ld, ld_slot, ld_dslot), dev, _flat(slot, "slot", _KINDS["i32"], dev,
-        n * k)
+    if codes and dt is _KINDS["i8"] and rows.is_cuda:
+        kind, on = IM_CODES, rows.get_device()
+    else:
+        kind, on = _first(rows, rows_name)
+    n, dim = _matrix_of(rows, rows_name)
+    k = _matrix_of(slot, "slot")[1]
+    if slots is None:
+        slots, slots_name = dslots, "dys"
+    m, ld_slot, ld_dslot = 0, dim, dim
+    if slots is not None:
+        m = _matrix_of(slots, slots_name)[0]
+        ld_slot = _ld(slots, slots_name, dt, on, m, dim)
+    if dslots is not None:
+        ld_dslot = _ld(dslots, "dys", dt, on, m, dim)
+    d = _desc(_DISPATCH, n, k, 1, m, dim, kind, _ld(rows, rows_name, dt, on, n, dim), ld_slot, ld_dslot)
+    return d, on, _at(slot, "slot", _KINDS["i32"], on, n * k)
 
 
 def im_dispatch_forward(x, slot, xs, error=None, stream=None):
     """xs[slot[i, c]] = x[i]: rows to their places (float32, bfloat16, or the int8 codes of
     packed rows; rows of xs that no slot names stay as they are). Rows may be strided."""
-    d, dev, ps = _exchange(x, "x", xs, "xs", slot, codes=True)
-    _run(dev.index, (_learn or load_learn()).im_dispatch_forward, ctypes.byref(d), x.data_ptr(), ps, xs.data_ptr(),
-         _flat(error, "error", _KINDS["i32"], dev, 1), stream)
+    d, on, ps = _exchange(x, "x", xs, "xs", slot, codes=True)
+    _run(on, stream, (_learn or load_learn()).im_dispatch_forward, d, x.data_ptr(), ps, xs.data_ptr(),
+         _at(error, "error", _KINDS["i32"], on, 1))
 
 
 def im_dispatch_backward(dxs, slot, dx, error=None, stream=None):
     """dx[i] = sum of dxs[slot[i, c]] over c."""
-    d, dev, ps = _exchange(dx, "dx", dxs, "dxs", slot)
-    _run(dev.index, (_learn or load_learn()).im_dispatch_backward, ctypes.byref(d), dxs.data_ptr(), ps, dx.data_ptr(),
-         _flat(error, "error", _KINDS["i32"], dev, 1), stream)
+    d, on, ps = _exchange(dx, "dx", dxs, "dxs", slot)
+    _run(on, stream, (_learn or load_learn()).im_dispatch_backward, d, dxs.data_ptr(), ps, dx.data_ptr(),
+         _at(error, "error", _KINDS["i32"], on, 1))
 
 
 def im_combine_forward(ys, slot, weight, y, error=None, stream=None):
     """y[i] = sum of weight[i, c] ys[slot[i, c]] over c (weight float32 like slot)."""
-    d, dev, ps = _exchange(y, "y", ys, "ys", slot)
-    _run(dev.index, (_learn or load_learn()).im_combine_forward, ctypes.byref(d), ys.data_ptr(), ps, _flat(weight,
-         "weight", _KINDS["f32"], dev, slot.numel()), y.data_ptr(),
-         _flat(error, "error", _KINDS["i32"], dev, 1), stream)
+    d, on, ps = _exchange(y, "y", ys, "ys", slot)
+    _run(on, stream, (_learn or load_learn()).im_combine_forward, d, ys.data_ptr(), ps,
+         _at(weight, "weight", _KINDS["f32"], on, slot.numel()), y.data_ptr(), _at(error, "error", _KINDS["i32"], on, 1))
 
 
 def im_combine_backward(dy, ys, slot, weight, dys=None, dweight=None, error=None, stream=None):
@@ -528,35 +566,34 @@ def im_combine_backward(dy, ys, slot, weight, dys=None, dweight=None, error=None
     (float32 like slot); None skips one."""
     if dweight is not None and ys is None:
         _bad("dweight needs ys")
-    d, dev, ps = _exchange(dy, "dy", ys, "ys", slot, dys)
-    f32 = _KINDS["f32"]
-    _run(dev.index, (_learn or load_learn()).im_combine_backward, ctypes.byref(d), dy.data_ptr(),
-         None if ys is None else ys.data_ptr(), ps,
-         _flat(weight, "weight", f32, dev, slot.numel()), None if dys is None else dys.data_ptr(),
-         _flat(dweight, "dweight", f32, dev, slot.numel()), _flat(error, "error", _KINDS["i32"], dev, 1), stream)
+    d, on, ps = _exchange(dy, "dy", ys, "ys", slot, dys)
+    f32, pairs = _KINDS["f32"], slot.numel()
+    _run(on, stream, (_learn or load_learn()).im_combine_backward, d, dy.data_ptr(),
+         None if ys is None else ys.data_ptr(), ps, _at(weight, "weight", f32, on, pairs),
+         None if dys is None else dys.data_ptr(), _at(dweight, "dweight", f32, on, pairs),
+         _at(error, "error", _KINDS["i32"], on, 1))
 
 
 def _rows(x, codes, scale, keep):
-    kind, dev = _kind(x, "x"), x.device
+    kind, on = _first(x, "x")
     n, dim = _matrix_of(x, "x")
-    d = ImRowsDesc(n, dim, kind, 1 if keep else 0, _matrix(x, "x", x.dtype, dev, n, dim),
-                   _matrix(codes, "codes", _KINDS["i8"], dev, n, dim))
-    return d, dev, _flat(scale, "scale", _KINDS["f32"], dev, n)
+    d = _desc(_ROWS, n, dim, kind, 1 if keep else 0, _ld(x, "x", x.dtype, on, n, dim),
+              _ld(codes, "codes", _KINDS["i8"], on, n, dim))
+    return d, on, _at(scale, "scale", _KINDS["f32"], on, n)
 
 
 def im_rows_pack(x, codes, scale, keep=False, stream=None):
     """Rows in 8 bits: codes int8 [n, dim] and scale float32 [n] of x [n, dim] (float32 or
     bfloat16), x = scale code up to half a scale. keep: what is not zero gets a code
     that is not. Rows of x and codes may be strided."""
-    d, dev, ps = _rows(x, codes, scale, keep)
-    _run(dev.index, (_learn or load_learn()).im_rows_pack, ctypes.byref(d), x.data_ptr(), codes.data_ptr(), ps, stream)
+    d, on, ps = _rows(x, codes, scale, keep)
+    _run(on, stream, (_learn or load_learn()).im_rows_pack, d, x.data_ptr(), codes.data_ptr(), ps)
 
 
 def im_rows_unpack(codes, scale, x, stream=None):
     """x = scale code in float32, rounded to its type."""
-    d, dev, ps = _rows(x, codes, scale, False)
-    _run(dev.index, (_learn or load_learn()).im_rows_unpack, ctypes.byref(d), codes.data_ptr(), ps, x.data_ptr(),
-         stream)
+    d, on, ps = _rows(x, codes, scale, False)
+    _run(on, stream, (_learn or load_learn()).im_rows_unpack, d, codes.data_ptr(), ps, x.data_ptr())
 
 
 def im_linear_workspace_packed(n_rows, in_dim, out_dim, dtype, n_groups=1, backward=False, device=None):
@@ -565,51 +602,64 @@ def im_linear_workspace_packed(n_rows, in_dim, out_dim, dtype, n_groups=1, backw
     return _size_of((_learn or load_learn()).im_linear_workspace_packed, d, backward, device)
 
 
+def _groups_of(W, dtype, index, cols):
+    """Groups and rows of contiguous weights [groups, rows, cols] or [rows, cols]."""
+    if W.dtype is dtype and W.get_device() == index and W.is_contiguous():
+        shape = W.shape
+        if len(shape) == 3 and shape[2] == cols:
+            return shape[0], shape[1]
+    return _weights(W, dtype, _cuda(index), cols)
+
+
+def _offsets_at(offsets, G, index):
+    if offsets is None and G != 1:
+        _bad("offsets are needed for more than one group")
+    return _at(offsets, "offsets", _KINDS["i32"], index, G + 1)
+
+
 def im_linear_forward_packed(x, x_scale, W, W_scale, b, y, offsets=None, relu=False, workspace=None, error=None,
                              stream=None):
     """y = act(x_scale W_scale (x W_g^T) + b_g) from packed rows x (int8 [n, in], x_scale
     float32 [n]) and packed weights W (int8 [groups, out, in] or [out, in], W_scale float32
     [groups, out]); y float32 or bfloat16 [n, out]. Rows of x and y may be strided."""
-    kind, dev, dt = _kind(y, "y"), y.device, y.dtype
-    f32, i32, i8 = _KINDS["f32"], _KINDS["i32"], _KINDS["i8"]
+    kind, on = _first(y, "y")
+    f32, i8 = _KINDS["f32"], _KINDS["i8"]
     n, k = _matrix_of(x, "x")
-    ld_x = _matrix(x, "x", i8, dev, n, k)
-    G, m = _weights(W, i8, dev, k)
-    ld_y = _matrix(y, "y", dt, dev, n, m)
-    L = _learn or load_learn()
-    d = ImLinearDesc(G, n, k, m, kind, 1 if relu else 0, 0, 0, ld_x, ld_y, 0)
-    ws, at, size = _workspace(L.im_linear_workspace_packed, d, (5, dev.index, G, n, k, m, kind), 0, workspace, dev,
-        stream)
-    _run(dev.index, L.im_linear_forward_packed, ctypes.byref(d), _offsets(offsets, G, dev), x.data_ptr(),
-         _flat(x_scale, "x_scale", f32, dev, n), W.data_ptr(),
-         _flat(W_scale, "W_scale", f32, dev, G * m), _flat(b, "b", f32, dev, G * m),
-         y.data_ptr(), at, size, _flat(error, "error", i32, dev, 1), stream)
+    G, m = _groups_of(W, i8, on, k)
+    d = _desc(_LINEAR, G, n, k, m, kind, 1 if relu else 0, 0, 0, _ld(x, "x", i8, on, n, k),
+              _ld(y, "y", y.dtype, on, n, m), 0)
+    L, key = _learn or load_learn(), (5, on, G, n, k, m, kind)
+    ws, at, size = None, None, 0
+    if _SIZES.get(key) != 0:
+        ws, at, size = _workspace(L.im_linear_workspace_packed, ImLinearDesc.from_buffer_copy(d), key, 0, workspace,
+                                  y.device, stream)
+    _run(on, stream, L.im_linear_forward_packed, d, _offsets_at(offsets, G, on), x.data_ptr(),
+         _at(x_scale, "x_scale", f32, on, n), W.data_ptr(), _at(W_scale, "W_scale", f32, on, G * m),
+         _at(b, "b", f32, on, G * m), y.data_ptr(), at, size, _at(error, "error", _KINDS["i32"], on, 1))
 
 
 def im_linear_backward_packed(dy, x, x_scale, W, dx=None, dW=None, db=None, offsets=None, relu_in=False,
                               workspace=None, error=None, stream=None):
     """Gradients of a layer as im_linear_backward's, with its input x kept as packed rows
     (int8 [n, in], x_scale float32 [n]). relu_in: dx is zero where x's code is not above 0."""
-    kind, dev, dt = _kind(dy, "dy"), dy.device, dy.dtype
-    f32, i32 = _KINDS["f32"], _KINDS["i32"]
+    kind, on = _first(dy, "dy")
+    dt, f32 = dy.dtype, _KINDS["f32"]
     n, m = _matrix_of(dy, "dy")
     k = _matrix_of(x, "x")[1]
-    ld_y = _matrix(dy, "dy", dt, dev, n, m)
-    ld_x = _matrix(x, "x", _KINDS["i8"], dev, n, k)
-    G, rows = _weights(W, dt, dev, k)
+    G, rows = _groups_of(W, dt, on, k)
     if rows != m:
         _bad(f"W has {rows} outputs, dy {m}")
-    ld_dx = k if dx is None else _matrix(dx, "dx", dt, dev, n, k)
-    L = _learn or load_learn()
-    d = ImLinearDesc(G, n, k, m, kind, 0, 1 if relu_in else 0, 0, ld_x, ld_y, ld_dx)
-    ws, at, size = _workspace(L.im_linear_workspace_packed, d, (6, dev.index, G, n, k, m, kind), 1, workspace, dev,
-        stream)
-    _run(dev.index, L.im_linear_backward_packed, ctypes.byref(d), _offsets(offsets, G, dev), dy.data_ptr(),
-         x.data_ptr(),
-         _flat(x_scale, "x_scale", f32, dev, n), W.data_ptr(),
-         None if dx is None else dx.data_ptr(), _flat(dW, "dW", dt, dev, G * m * k),
-         _flat(db, "db", f32, dev, G * m), at, size,
-         _flat(error, "error", i32, dev, 1), stream)
+    d = _desc(_LINEAR, G, n, k, m, kind, 0, 1 if relu_in else 0, 0, _ld(x, "x", _KINDS["i8"], on, n, k),
+              _ld(dy, "dy", dt, on, n, m), k if dx is None else _ld(dx, "dx", dt, on, n, k))
+    L, key = _learn or load_learn(), (6, on, G, n, k, m, kind)
+    ws, at, size = None, None, 0
+    if _SIZES.get(key) != 0:
+        ws, at, size = _workspace(L.im_linear_workspace_packed, ImLinearDesc.from_buffer_copy(d), key, 1, workspace,
+                                  dy.device, stream)
+    _run(on, stream, L.im_linear_backward_packed, d, _offsets_at(offsets, G, on), dy.data_ptr(), x.data_ptr(),
+         _at(x_scale, "x_scale", f32, on, n), W.data_ptr(), None if dx is None else dx.data_ptr(),
+         _at(dW, "dW", dt, on, G * m * k), _at(db, "db", f32, on, G * m), at, size,
+         _at(error, "error", _KINDS["i32"], on, 1))
 
 
 # Plans whose AdamW was dropped. To free one synchronises the device, which would spoil a graph

@@ -199,3 +199,15 @@ def test_python_refuses_before_the_library():
         with pytest.raises(P.IMError):
             call()
     assert P.im_dispatch_workspace(10, 2, 8) == 0 and P.im_dispatch_workspace(100000, 2, 8) > 0
+
+
+def test_descriptions_lie_as_the_structures_do():
+    for form, cls in ((learn._LINEAR, learn.ImLinearDesc), (learn._ROUTER, learn.ImRouterDesc),
+                      (learn._DISPATCH, learn.ImDispatchDesc), (learn._ROWS, learn.ImRowsDesc)):
+        values = [i + 1 for i in range(len(cls._fields_))]
+        assert form.size == ctypes.sizeof(cls)
+        d = cls.from_buffer_copy(form.pack(*values))
+        assert [getattr(d, name) for name, _ in cls._fields_] == values
+        values[0] = 1 << 31
+        with pytest.raises(P.IMError):
+            learn._desc(form, *values)
