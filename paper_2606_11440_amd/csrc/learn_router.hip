@@ -477,7 +477,9 @@ __global__ __launch_bounds__(256) void router_kernel(const RouterArgs a, int sco
         }
         if (l < 4) mine[a.sets + l] = -INFINITY;   // the last four are read whole
         lds_order();
-        int rank[V / 4];   // sets that come before the lane's
+        // sets that come before the lane's; by scores those of a larger value, and of equal ones all are taken: where
+        // they are too many then, the row is unsure
+        int rank[V / 4], count = 0;
 #pragma unroll
         for (int q = 0; q < V / 4; ++q) rank[q] = 0;
 #pragma unroll 2
@@ -496,9 +498,12 @@ __global__ __launch_bounds__(256) void router_kernel(const RouterArgs a, int sco
           const bool chosen = rank[q] < a.top_sets;
           taken = chosen ? fminf(taken, value[q]) : taken;
           left = chosen ? left : fmaxf(left, value[q]);
+          if constexpr (SCORES) count += chosen && value[q] > -INFINITY;
 #pragma unroll
           for (int i = 0; i < 4; ++i) key[4 * q + i] = chosen ? key[4 * q + i] : -INFINITY;
         }
+        if constexpr (SCORES)   // each set counts in its lanes
+          unsure = across<L>(count, [](int32_t a, int32_t b) { return a + b; }) > a.top_sets << shift;
       } else {
 #pragma unroll
         for (int v = 0; v < V; ++v)
@@ -554,7 +559,7 @@ __global__ __launch_bounds__(256) void router_kernel(const RouterArgs a, int sco
       if constexpr (SCORES) {   // a sum of two is off by twice as much
         taken = -most_of<L>(-taken);
         left = most_of<L>(left);
-        unsure = left > -INFINITY && !(taken - left > 3.f * near + most_of<L>(large) * 0x1p-21f);
+        unsure |= left > -INFINITY && !(taken - left > 3.f * near + most_of<L>(large) * 0x1p-21f);
       }
     }
     // The keys as integers in their order. Scores' low bits become the number within the lane, and the
