@@ -589,7 +589,10 @@ __global__ __launch_bounds__(256) void router_kernel(const RouterArgs a, int sco
       best = most_of<L>(best);
       int j;
       if constexpr (SCORES) {
-        const float value = from_ordered(best);   // NaN where none is left: it counts in neither
+        // without the place, whose bits would count as up to V - 1 units more: a lower bound, so that what lies between
+        // two is too large by as much at most. NaN where none is left, which counts in neither; a key of infinity
+        // makes the size infinite and the row unsure.
+        const float value = from_ordered(best & ~(V - 1));
         if (c > 0) apart = fminf(apart, before - value);
         size = fmaxf(size, fabsf(value));
         before = value;
@@ -614,7 +617,7 @@ __global__ __launch_bounds__(256) void router_kernel(const RouterArgs a, int sco
 #pragma unroll
       for (int t = 0; t < C; ++t) choice[t] = c == t * L + l ? j : choice[t];
     }
-    // a sum with a bias is rounded to 2^-24 of itself, and its low bits are not its own
+    // a sum with a bias is rounded to 2^-24 of itself, and its low bits are taken as zeros
     if constexpr (SCORES) unsure |= !(apart > near + (0x1p-22f + V * 0x1p-23f) * size);
     float z[C], w[C];
 #pragma unroll

@@ -65,3 +65,64 @@ def test_sets_whose_sums_fp32_cannot_tell_apart(E, sets, top_sets):
     z[:, :, 1] = torch.logit(s)
     z[:, :, 3] = torch.logit(0.9 - s)
     check(torch, z.reshape(n, E).float().cuda(), None, min(4, 2 * top_sets), "sigmoid", True, None, sets, top_sets, 2)
+
+
+@pytest.mark.parametrize("score", SCORES)
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("E,sets,top_sets", [(8, 1, 1), (8, 2, 1), (24, 1, 1), (64, 1, 1), (64, 8, 3), (100, 10, 2),
+                                             (200, 1, 1), (1024, 1, 1)])
+def test_biases_of_infinity(E, sets, top_sets, dtype, score):
+    """Two of them, and more than can be chosen: equal c, the lowest index first."""
+    note(f"[infinite biases] E={E} sets={sets} {dtype} {score}")
+    torch = need_gpu()
+    g = torch.Generator().manual_seed(E)
+    z = torch.randn(90, E, generator=g).to(getattr(torch, dtype)).cuda()
+    for where in ([1, 4], [E - 1, 0], [0, 1, 2, 3], list(range(E // 2, E)), list(range(E))):
+        for k in (1, 2, 4):
+            for best in (1, 2):
+                b = torch.randn(E, generator=g) * 0.1
+                b[where] = INF
+                check(torch, z, None, k, score, True, b, sets, top_sets, best)
+    ok = (torch.rand(90, E, generator=g) < 0.6).numpy()
+    b[:] = torch.where(torch.rand(E, generator=g) < 0.5, INF, -INF)
+    check(torch, z, ok, 2, score, False, b, sets, top_sets, 2)
+
+
+@pytest.mark.parametrize("score", SCORES)
+@pytest.mark.parametrize("E", [16, 32, 64, 256, 1024])
+def test_scores_next_to_large_biases(E, score):
+    """Two experts whose c, a bias of 64 or so + a score of 1 / 2 or 1 / 4, lie some 1e-8 apart where fp32 rounds (half
+    its unit of 2^-17 under a multiple of 16): what it makes of them is a unit apart, either way."""
+    note(f"[large biases] E={E} {score}")
+    torch = need_gpu()
+    n, r = 20000 if E <= 64 else 3000, np.random.default_rng(E)
+    unit, apart = 2.0 ** -17, 30000                  # of the biases, in units
+    V = 4 if E <= 16 else (8 if E <= 32 else 16)
+    L = E // V                                       # lanes of a row
+    pair = [0, (V // 4 - 1) * 4 * L + 3]             # the first and the last number of the first lane
+    for first, second in (pair, pair[::-1]):
+        c = 0.5 - unit / 2 + r.uniform(-4e-8, 4e-8, (n, 2))
+        s = c - np.array([0, apart * unit])
+        z = torch.full((n, E), -60.0, dtype=torch.float64)
+        z[:, [first, second]] = torch.from_numpy(np.log(s / (1 - s) if score == "sigmoid" else s))
+        if score == "softmax":
+            z[:, 5] = torch.from_numpy(np.log(1 - s.sum(1)))
+        b = torch.full((E,), -100.0)
+        b[first], b[second] = 64.0, 64.0 + apart * unit
+        check(torch, z.float().cuda(), None, 1, score, True, b)
+
+
+@pytest.mark.parametrize("score", SCORES)
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_no_expert_is_left(dtype, score):
+    """Rows with as many experts to choose as are chosen, or fewer."""
+    note(f"[none left] {dtype} {score}")
+    torch = need_gpu()
+    g = torch.Generator().manual_seed(8)
+    for E, sets, top_sets, k in ((8, 1, 1, 8), (8, 2, 1, 4), (64, 8, 1, 8), (64, 16, 4, 16), (200, 1, 1, 32), (30, 10, 2, 6)):
+        z = torch.randn(150, E, generator=g).to(getattr(torch, dtype)).cuda()
+        ok = (torch.rand(150, E, generator=g) < 0.2).numpy()
+        b = torch.randn(E, generator=g) * 0.1
+        for mask in (None, ok):
+            check(torch, z, mask, k, score, True, b, sets, top_sets, 2)
+            check(torch, z, mask, k, score, False, None, sets, top_sets, 2)
