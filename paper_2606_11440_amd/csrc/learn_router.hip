@@ -442,8 +442,9 @@ __global__ __launch_bounds__(256) void router_kernel(const RouterArgs a, int sco
           for (int v = 0; v < V; ++v) key[v] = (out >> v) & 1u ? -INFINITY : key[v];
         }
         // the exponential is off by (1.25 |z| + 2) 2^-24 of itself, which counts by the score times
-        // (1 - score); the sum and the reciprocal add 3 2^-24 of the score; both for two scores
-        near = most * (0x1p-20f + 0x1p-21f * fmaxf(-top, 0.f));
+        // (1 - score); the sum and the reciprocal add 3 2^-24 of the score; both for two scores. Below the normal
+        // floats the reciprocal gives 0: 2^-126 more of each.
+        near = most * (0x1p-20f + 0x1p-21f * fmaxf(-top, 0.f)) + 0x1p-124f;
       }
       if (a.bias) {
 #pragma unroll

@@ -126,3 +126,16 @@ def test_no_expert_is_left(dtype, score):
         for mask in (None, ok):
             check(torch, z, mask, k, score, True, b, sets, top_sets, 2)
             check(torch, z, mask, k, score, False, None, sets, top_sets, 2)
+
+
+@pytest.mark.parametrize("E,sets,top_sets", [(8, 2, 1), (64, 8, 3), (100, 10, 2), (256, 8, 4)])
+def test_sigmoids_below_the_normal_floats(E, sets, top_sets):
+    """Sums and biases of about the smallest normal float, which scores of logits near -88 have."""
+    note(f"[tiny sigmoids] E={E} sets={sets}")
+    torch = need_gpu()
+    g = torch.Generator().manual_seed(E)
+    z = (-86.3 - 2.5 * torch.rand(500, E, generator=g)).cuda()
+    check(torch, z, None, 3, "sigmoid", True, None, sets, top_sets, 2)
+    check(torch, z, None, 3, "sigmoid", True, torch.randn(E, generator=g) * 1e-38)
+    check(torch, z, None, 3, "sigmoid", True, torch.randn(E, generator=g) * 1e-38, sets, top_sets, 2)
+    check(torch, z, None, 3, "sigmoid", True, torch.randn(E, generator=g) * 1e-39, sets, top_sets, 1)
