@@ -565,13 +565,15 @@ __global__ __launch_bounds__(256) void router_kernel(const RouterArgs a, int sco
     }
     // The keys as integers in their order. Scores' low bits become the number within the lane, and the
     // lower half of a bf16 logit what tells the lower index: such keys are sorted within the lane,
-    // and each choice takes one from a lane's front. fp32 logits are looked through.
+    // and each choice takes one from a lane's front. An infinite one counts as the largest float, which no bf16 number
+    // is: the factor of 1 + 2^-23 takes that to infinity, and of others changes the lower half only. fp32 logits are
+    // looked through.
     constexpr bool kSorted = SCORES || sizeof(T) == 2;
     int32_t at[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if constexpr (SCORES) at[v] = (ordered(key[v]) & ~(V - 1)) | (V - 1 - v);   // of -infinity: kNone at most
-      else if constexpr (kSorted) at[v] = (ordered(key[v] + 0.f) & ~0xffff) | (0xffff - place<L>(v) - 4 * l);
+      else if constexpr (kSorted) at[v] = (ordered(fmaf(key[v], 1.f + 0x1p-23f, 0.f)) & ~0xffff) | (0xffff - place<L>(v) - 4 * l);
       else at[v] = ordered(key[v] + 0.f);   // -0 as +0
     }
     if constexpr (kSorted) sort_down<V>(at);

@@ -139,3 +139,22 @@ def test_sigmoids_below_the_normal_floats(E, sets, top_sets):
     check(torch, z, None, 3, "sigmoid", True, torch.randn(E, generator=g) * 1e-38)
     check(torch, z, None, 3, "sigmoid", True, torch.randn(E, generator=g) * 1e-38, sets, top_sets, 2)
     check(torch, z, None, 3, "sigmoid", True, torch.randn(E, generator=g) * 1e-39, sets, top_sets, 1)
+
+
+@pytest.mark.parametrize("score", SCORES)
+@pytest.mark.parametrize("E,sets,top_sets", [(8, 1, 1), (30, 1, 1), (64, 1, 1), (64, 8, 4), (193, 1, 1), (1000, 10, 9)])
+def test_infinity_is_above_the_largest_bf16(E, sets, top_sets, score):
+    """A logit of +infinity counts as the largest float, which no bf16 number reaches."""
+    note(f"[bf16 infinity] E={E} sets={sets} {score}")
+    torch = need_gpu()
+    g = torch.Generator().manual_seed(E)
+    z = torch.randn(60, E, generator=g).bfloat16()
+    top = torch.finfo(torch.bfloat16).max
+    z[:30, 1], z[:30, 5] = top, INF
+    z[30:, :4], z[30:, 4:7] = top, INF
+    z[45:, 0], z[45:, 3] = -top, -INF
+    z[50:, 2], z[50:, 7] = 0.0, -0.0
+    z[55:, 8 - E:] = -top
+    for k in (1, 2, 4):
+        for renorm in (True, False):
+            check(torch, z.cuda(), None, k, score, renorm, None, sets, top_sets, 1)
