@@ -720,8 +720,15 @@ __global__ __launch_bounds__(256) void router_backward_kernel(const RouterArgs a
       }
     }
     const float each = dense ? -dot / total : 0.f;
+    // no zero times NaN or infinity where the expert is not valid
+    const bool odd = !(fabsf(each) <= kLargest);
+    if (ballot(odd) != 0) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) q[v] *= each;
+      for (int v = 0; v < V; ++v) q[v] = q[v] == 0.f ? 0.f : q[v] * each;
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) q[v] *= each;
+    }
     // The choices' parts are added in LDS: a row's listed experts are as a rule no two the same, which
     // each place's last writer tells. Where they are, they are added in their order, one by one.
     float* const mine = lds[threadIdx.x / 64] + ((int)threadIdx.x % 64) / L * (L * V);

@@ -158,3 +158,36 @@ def test_infinity_is_above_the_largest_bf16(E, sets, top_sets, score):
     for k in (1, 2, 4):
         for renorm in (True, False):
             check(torch, z.cuda(), None, k, score, renorm, None, sets, top_sets, 1)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("E", [8, 40, 193, 1000])
+def test_gradients_that_are_not_finite_stay_with_valid_experts(E, dtype):
+    """dweight of NaN or infinity: dz of experts that are not valid is zero all the same, and other rows do not see it."""
+    note(f"[dz of no expert] E={E} {dtype}")
+    import paper_2606_11440_amd as P
+    torch = need_gpu()
+    g = torch.Generator().manual_seed(E)
+    n, k = 70, 3
+    z = torch.randn(n, E, generator=g).to(getattr(torch, dtype))
+    ok = (torch.rand(n, E, generator=g) < 0.6).numpy()
+    ok[:, 0] = True
+    z[:, E // 2], z[:, E - 1] = -INF, float("nan")
+    valid = torch.from_numpy(ok) & (z > -INF)
+    for score in SCORES:
+        for renorm in (False, True):
+            ref = X.Router(z, score, ok)
+            e = ref.choose(k)
+            dw = torch.randn(n, k, generator=g)
+            clean, tol = ref.grad(e, dw, renorm)
+            bad = {4: float("nan"), 9: INF, 30: -INF, 69: float("nan")}
+            for row, x in bad.items():
+                dw[row, 0] = x
+            dz = torch.full((n, E), 77.0, dtype=z.dtype, device="cuda")
+            P.im_router_backward(z.cuda(), torch.from_numpy(e).int().cuda(), dw.cuda(), dz, valid=X.words(ok).cuda(),
+                                 score=score, renorm=renorm)
+            dz = dz.cpu()
+            assert bool((dz[~valid] == 0).all()), (score, renorm)
+            assert all(not bool(torch.isfinite(dz[row]).all()) for row in bad), (score, renorm)
+            rows = [i for i in range(n) if i not in bad]
+            X.same_or_close(dz[rows], clean[rows], tol[rows], (score, renorm))
