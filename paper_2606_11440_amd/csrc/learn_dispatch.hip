@@ -391,8 +391,7 @@ int element(int dtype) { return dtype == IM_CODES ? 1 : (dtype == IM_BF16 ? 2 : 
 
 }  // namespace
 
-int64_t plan_blocks(int64_t pairs, int64_t E, int cus, int64_t& each) {
-  (void)E;
+int64_t plan_blocks(int64_t pairs, int cus, int64_t& each) {
   // one block, and one launch, for few pairs (4096: 4.1 us); more take blocks of 1024 each until a block a CU
   // (262144 pairs, 64 experts: 16 us in blocks of 4096)
   int64_t blocks = pairs <= 4096 ? 1 : (pairs + 1023) / 1024;

@@ -73,9 +73,9 @@ PlanWork plan_work(const im_dispatch_desc& d, void* ws) {
   PlanArgs& a = w.args;
   a.pairs = (int64_t)d.n_rows * d.top_k;
   a.E = d.n_experts;
-  a.blocks = (int32_t)plan_blocks(a.pairs, a.E, compute_units(), a.each);
+  a.blocks = (int32_t)plan_blocks(a.pairs, compute_units(), a.each);
   Sections s(ws);
-  a.count = s.take<int32_t>(a.blocks > 1 ? (int64_t)a.blocks * a.E : 0);
+  a.count = a.blocks > 1 ? s.take<int32_t>((int64_t)a.blocks * a.E) : nullptr;
   w.bytes = s.used;
   return w;
 }

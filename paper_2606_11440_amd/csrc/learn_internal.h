@@ -149,14 +149,13 @@ struct PlanArgs {
   const int32_t* expert;
   int64_t pairs;
   int32_t E, blocks;          // blocks that share the pairs
-  int64_t each;               // pairs of a block, a multiple of 64
-  int32_t* count;             // [blocks][E]: pairs of an expert in a block, then in the blocks before it
-  int32_t* total;             // [E]
+  int64_t each;               // pairs of a block, a multiple of 512 (its waves' runs are whole groups of 64)
+  int32_t* count;             // [blocks][E]: pairs of an expert in a block; NULL with one block
   int32_t* offsets;
   int32_t* slot;
   int32_t* error;
 };
-int64_t plan_blocks(int64_t pairs, int64_t E, int cus, int64_t& each);
+int64_t plan_blocks(int64_t pairs, int cus, int64_t& each);
 hipError_t launch_dispatch_plan(const PlanArgs& a, hipStream_t s);
 
 struct ExchangeArgs {
