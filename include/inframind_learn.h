@@ -289,7 +289,8 @@ im_status im_combine_backward(const im_dispatch_desc* desc, const void* dy, cons
  * A packed row is int8 codes in [-127, 127] and a scale: x_j = scale code_j.
  *   scale = max |x_j| / 127 (at least 2^-126), code = x_j (1 / scale), rounded to
  *   nearest even, every operation in fp32
- * so that |x_j - scale code_j| <= scale / 2 (and a few units of fp32). keep: what is not
+ * so that |x_j - scale code_j| <= scale / 2 (and a few units of fp32; the largest float itself comes back as
+ * infinity, which 127 scales are then). keep: what is not
  * zero gets the code 1 or -1 at least, so that a kept ReLU output says where it was above
  * zero (off by less than a scale there). A row with a value that is not finite has
  * the scale NaN and codes 0.
@@ -309,7 +310,8 @@ im_status im_rows_unpack(const im_rows_desc* desc, const int8_t* codes, const fl
  * is not packed (y; dy, W, dx, dW) and ld_x the row stride of the codes.
  * forward: y_i = act(x_scale_i W_scale_gj (sum_k x_ik W_gjk) + b_gj), a product of
  * 8-bit integers whose sum is exact; x and W are codes, W [n_groups x out_dim x in_dim]
- * contiguous, W_scale fp32 [n_groups x out_dim].
+ * contiguous, W_scale fp32 [n_groups x out_dim]. In fp32 the sum is multiplied by x_scale first: where that
+ * passes the largest float, y is infinite however small W_scale is.
  * backward: the gradients of im_linear_backward with x in 8 bits, as it was kept
  * (IM_BF16: scale code is rounded to bf16 where it enters the product of dW, 2^-8 of it at
  * most, which rounding to the code left already of the largest); relu_in: dx is zero where the code is not above 0. */

@@ -3,7 +3,7 @@
 //
 // A row's experts are spread over few lanes (16 a lane where there are as many), so that most of the
 // work is within lanes and a wave has several rows. What bounds it is the number of operations: 262144 rows of
-// 64 experts in 8 sets, fp32, sigmoid and bias, 45 us (75 MB: 14 us at the rate of a copy), of some 1150
+// 64 experts in 8 sets, fp32, sigmoid and bias, 46 us (75 MB: 14 us at the rate of a copy), of some 1170
 // instructions for 16 rows; 8 lanes of 8 experts took 61 us, a wave a row in 64 bits throughout 332. The gradient
 // of 100003 rows of 193 experts, bf16, dense softmax: 30 us (85 MB: 16 us); adding the choices' parts
 // to every lane's experts in registers took 39.
@@ -362,8 +362,8 @@ __device__ __forceinline__ void two_best_with(float& first, float& second, bool 
 // SCORES: the choice goes by scores (a bias, or sets by the sum of their best), which fp32 knows
 // up to `near` only. Where two that decide something (neighbours in the order of the chosen and the
 // first that is not, or the last set taken and the first left) are no further apart, the
-// row is done again in 64 bits: one row of some thousand. The order is then found on integers whose low bits
-// are the number within the lane. Otherwise the choice goes by the logits themselves, exactly.
+// row is done again in 64 bits: one row of some thousand, and every row with scores that are equal there. The
+// order is then found on integers whose low bits are the number within the lane. Otherwise the choice goes by the logits themselves, exactly.
 // SETS: 0 none, 1 sets of 4, 8, .. experts within the lanes' fours, 2 any.
 template <typename T, int L, int V, int C, bool SCORES, int SETS>
 __global__ __launch_bounds__(256) void router_kernel(const RouterArgs a, int score) {
