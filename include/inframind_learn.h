@@ -209,7 +209,8 @@ void im_adamw_destroy(im_adamw* opt);
  *   or the sum of its two best, of s + bias or of s (set_best = 2; a set with
  *   one valid expert has that one's)
  *   weight = scale s of the chosen experts, with renorm divided by the sum of theirs
- * c is compared as computed in 64 bits; of equal ones the lowest index is best.
+ * c and the sets' values are compared as computed in 64 bits; of equal ones the lowest index is best, and what
+ * lies nearer to one another than a 64-bit number's rounding may come in either order.
  * Experts come in the order of their c. An expert is valid where `valid` (uint32
  * [n_rows x ceil(n_experts / 32)], as for the softmax head, or NULL) has its bit and
  * its z is neither NaN nor -infinity; +infinity counts as the largest float. One
